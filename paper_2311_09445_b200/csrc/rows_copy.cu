@@ -1,0 +1,278 @@
+// Rows to the experts and back: dispatch, combine and the gradient of combine.
+#include "rows_internal.cuh"
+
+namespace {
+
+constexpr uint32_t kThreads = 256;
+
+// How a block of threads covers rows of `cols` accesses each: `across` threads along a row, `down` rows; where a row has more
+// than a block's threads the grid's y covers its parts, all of one length within an access.
+struct Tiling {
+    uint32_t across, down, parts;
+    dim3 grid, block;
+};
+Tiling tile(uint32_t rows, uint32_t cols)
+{
+    Tiling t;
+    t.parts = (cols + kThreads - 1) / kThreads;
+    t.across = (cols + t.parts - 1) / t.parts;
+    t.down = kThreads / t.across;
+    t.grid = dim3((rows + t.down - 1) / t.down, t.parts);
+    t.block = dim3((t.across * t.down + 31) / 32 * 32);
+    return t;
+}
+
+// ---- dispatch --------------------------------------------------------------------------------------------------------
+// xs[place[t, j]] = x[t].  A thread reads its access of row t once and writes it k times: (1 + k) rows of traffic for k
+// copies, bound by the stores.
+template <int B, int KC>
+__global__ void __launch_bounds__(kThreads) dispatch_kernel(unsigned* status, uint32_t T, uint32_t k, uint32_t cols, uint32_t across,
+                                                            uint32_t down, const unsigned char* __restrict__ x, uint64_t ld_x,
+                                                            const int32_t* __restrict__ place, uint32_t sorted_rows,
+                                                            unsigned char* __restrict__ xs)
+{
+    typedef typename RowsRaw<B>::type R;
+    rows_begin();
+    const uint32_t in = threadIdx.x / across;
+    const uint32_t col = threadIdx.x - in * across + blockIdx.y * across;
+    const uint64_t t = (uint64_t)blockIdx.x * down + in;
+    if (in >= down || t >= T || col >= cols) return;
+    const R v = rows_load(reinterpret_cast<const R*>(x + t * ld_x) + col);
+    const int32_t* p = place + t * k;
+    for (uint32_t j0 = 0; j0 < k; j0 += KC) {
+        int32_t at[KC];
+#pragma unroll
+        for (int j = 0; j < KC; ++j) at[j] = j0 + j < k ? __ldg(p + j0 + j) : -1;
+#pragma unroll
+        for (int j = 0; j < KC; ++j) {
+            if (at[j] >= 0 && (uint32_t)at[j] < sorted_rows) rows_store(reinterpret_cast<R*>(xs) + (uint64_t)(uint32_t)at[j] * cols + col, v);
+            else if (at[j] != -1 && col == 0) atomicOr(status, PEARL_ST_BAD_INDEX);
+        }
+    }
+}
+
+// ---- combine ---------------------------------------------------------------------------------------------------------
+// y[t] = sum_j w[t, j] z[place[t, j]], j ascending, in binary32.  A thread holds the sums of N elements; the k reads do not
+// depend on one another and are issued together.
+template <typename E, int N, int KC, bool kWeights>
+__global__ void __launch_bounds__(kThreads) combine_kernel(unsigned* status, uint32_t T, uint32_t k, uint32_t cols, uint32_t across,
+                                                           uint32_t down, const E* __restrict__ z, uint32_t sorted_rows,
+                                                           const int32_t* __restrict__ place, const float* __restrict__ w,
+                                                           E* __restrict__ y, uint64_t ld_y)
+{
+    rows_begin();
+    const uint32_t in = threadIdx.x / across;
+    const uint32_t col = threadIdx.x - in * across + blockIdx.y * across;
+    const uint64_t t = (uint64_t)blockIdx.x * down + in;
+    if (in >= down || t >= T || col >= cols) return;
+    float sum[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum[i] = 0.0f;
+    for (uint32_t j0 = 0; j0 < k; j0 += KC) {
+        int32_t at[KC];
+        float wt[KC];
+        RowsVec<E, N> v[KC];
+#pragma unroll
+        for (int j = 0; j < KC; ++j) {
+            at[j] = j0 + j < k ? __ldg(place + t * k + j0 + j) : -1;
+            wt[j] = kWeights && j0 + j < k ? __ldg(w + t * k + j0 + j) : 1.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < KC; ++j) {
+            if ((at[j] >= 0 && (uint32_t)at[j] >= sorted_rows) || at[j] < -1) {
+                if (col == 0) atomicOr(status, PEARL_ST_BAD_INDEX);
+                at[j] = -1;
+            }
+            if (at[j] >= 0) v[j] = rows_load_vec<E, N>(z + ((uint64_t)(uint32_t)at[j] * cols + col) * N);
+        }
+#pragma unroll
+        for (int j = 0; j < KC; ++j) {
+            if (at[j] < 0) continue;
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                sum[i] = kWeights ? __fmaf_rn(wt[j], RowsElem<E>::up(v[j].e[i]), sum[i]) : __fadd_rn(sum[i], RowsElem<E>::up(v[j].e[i]));
+        }
+    }
+    RowsVec<E, N> out;
+#pragma unroll
+    for (int i = 0; i < N; ++i) out.e[i] = RowsElem<E>::down(sum[i]);
+    rows_store_vec<E, N>(y + t * ld_y + (uint64_t)col * N, out);
+}
+
+// ---- the gradient of combine -----------------------------------------------------------------------------------------
+// dz[place[t, j]] = w[t, j] dy[t], dw[t, j] = <dy[t], z[place[t, j]]>.  A team of `team` threads (a power of two, 32 .. 256) has one
+// row t: each thread reads its accesses of dy once for KC slots at a time and keeps one partial sum a slot; the partial sums are
+// added in a fixed order (a tree over the lanes, then the warps in turn).
+template <typename E, int N, int KC>
+__global__ void __launch_bounds__(kThreads) combine_grad_kernel(unsigned* status, uint32_t T, uint32_t k, uint32_t cols, uint32_t team,
+                                                                const E* __restrict__ dy, uint64_t ld_dy, const E* __restrict__ z,
+                                                                uint32_t sorted_rows, const int32_t* __restrict__ place,
+                                                                const float* __restrict__ w, E* __restrict__ dz, float* __restrict__ dw)
+{
+    __shared__ float part[kThreads / 32][KC];
+    rows_begin();
+    const uint32_t in = threadIdx.x / team, me = threadIdx.x % team;
+    const uint64_t t = (uint64_t)blockIdx.x * (kThreads / team) + in;
+    const bool row = t < T;
+    const E* g = dy + (row ? t : 0) * ld_dy;
+    for (uint32_t j0 = 0; j0 < k; j0 += KC) {
+        int32_t at[KC];
+        float wt[KC], dot[KC];
+#pragma unroll
+        for (int j = 0; j < KC; ++j) {
+            const bool slot = row && j0 + j < k;
+            at[j] = slot ? __ldg(place + t * k + j0 + j) : -1;
+            wt[j] = slot && w != nullptr ? __ldg(w + t * k + j0 + j) : 1.0f;
+            dot[j] = 0.0f;
+            if ((at[j] >= 0 && (uint32_t)at[j] >= sorted_rows) || at[j] < -1) {
+                if (me == 0) atomicOr(status, PEARL_ST_BAD_INDEX);
+                at[j] = -1;
+            }
+        }
+        for (uint32_t col = me; col < cols && row; col += team) {
+            const RowsVec<E, N> a = rows_load_vec<E, N>(g + (uint64_t)col * N);
+            RowsVec<E, N> v[KC];
+            if (dw != nullptr) {
+#pragma unroll
+                for (int j = 0; j < KC; ++j)
+                    if (at[j] >= 0) v[j] = rows_load_vec<E, N>(z + ((uint64_t)(uint32_t)at[j] * cols + col) * N);
+            }
+#pragma unroll
+            for (int j = 0; j < KC; ++j) {
+                if (at[j] < 0) continue;
+                if (dw != nullptr) {
+#pragma unroll
+                    for (int i = 0; i < N; ++i) dot[j] = __fmaf_rn(RowsElem<E>::up(a.e[i]), RowsElem<E>::up(v[j].e[i]), dot[j]);
+                }
+                if (dz != nullptr) {
+                    RowsVec<E, N> o;
+#pragma unroll
+                    for (int i = 0; i < N; ++i) o.e[i] = RowsElem<E>::down(__fmul_rn(wt[j], RowsElem<E>::up(a.e[i])));
+                    rows_store_vec<E, N>(dz + ((uint64_t)(uint32_t)at[j] * cols + col) * N, o);
+                }
+            }
+        }
+        if (dw == nullptr) continue;
+#pragma unroll
+        for (int j = 0; j < KC; ++j)
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) dot[j] = __fadd_rn(dot[j], __shfl_xor_sync(0xFFFFFFFFu, dot[j], d));
+        if (team > 32) {
+            const uint32_t warp = threadIdx.x / 32;
+            __syncthreads();                          // the sums of the slots before these have been read
+            if ((threadIdx.x & 31u) == 0) {
+#pragma unroll
+                for (int j = 0; j < KC; ++j) part[warp][j] = dot[j];
+            }
+            __syncthreads();
+            if (me < KC && row && j0 + me < k) {
+                float s = 0.0f;
+                for (uint32_t q = 0; q < team / 32; ++q) s = __fadd_rn(s, part[in * (team / 32) + q][me]);
+                dw[t * k + j0 + me] = s;
+            }
+        } else if (me == 0 && row) {
+#pragma unroll
+            for (int j = 0; j < KC; ++j)
+                if (j0 + j < k) dw[t * k + j0 + j] = dot[j];
+        }
+    }
+}
+
+// Runs CALL(N) with the elements per access that `granule` allows for elements of S bytes.
+#define ROWS_WITH_VEC(S, granule, CALL)                                         \
+    do {                                                                        \
+        if ((granule) >= 16) { CALL(16 / (S)); }                                \
+        else if ((granule) >= 8) { CALL(8 / (S)); }                             \
+        else if ((granule) >= 4) { CALL(4 / (S)); }                             \
+        else { CALL(1); }                                                       \
+    } while (0)
+
+// Runs CALL(KC): slots of a row that are handled together.
+#define ROWS_WITH_SLOTS(k, CALL)                                                \
+    do {                                                                        \
+        if ((k) <= 2) { CALL(2); } else if ((k) <= 4) { CALL(4); } else { CALL(8); } \
+    } while (0)
+
+}  // namespace
+
+int rows_launch_dispatch(unsigned* status, uint32_t T, uint32_t k, uint32_t row_bytes, const void* x, uint64_t ld_x,
+                         const int32_t* place, uint32_t sorted_rows, void* xs, cudaStream_t s)
+{
+    if (T == 0) return 0;
+    const uint32_t g = rows_granule(row_bytes, ld_x, (uintptr_t)x, (uintptr_t)xs);
+    const uint32_t cols = row_bytes / g;
+    const Tiling t = tile(T, cols);
+    if (t.grid.y > 65535u) return -1;
+    int rc = -1;
+#define ROWS_GO(B, KC)                                                                                                      \
+    rc = rows_launch(dispatch_kernel<B, KC>, t.grid, t.block, 0, s, 0, status, T, k, cols, t.across, t.down, (const unsigned char*)x, ld_x, \
+                     place, sorted_rows, (unsigned char*)xs)
+#define ROWS_K(KC)                                                                                     \
+    switch (g) {                                                                                       \
+    case 16: ROWS_GO(16, KC); break;                                                                   \
+    case 8: ROWS_GO(8, KC); break;                                                                     \
+    case 4: ROWS_GO(4, KC); break;                                                                     \
+    case 2: ROWS_GO(2, KC); break;                                                                     \
+    default: ROWS_GO(1, KC); break;                                                                    \
+    }
+    ROWS_WITH_SLOTS(k, ROWS_K);
+#undef ROWS_K
+#undef ROWS_GO
+    return rc;
+}
+
+int rows_launch_combine(unsigned* status, uint32_t T, uint32_t k, uint32_t D, uint32_t dtype, const void* z, uint32_t sorted_rows,
+                        const int32_t* place, const float* w, void* y, uint64_t ld_y, cudaStream_t s)
+{
+    if (T == 0) return 0;
+    const uint32_t S = rows_elem_bytes(dtype);
+    const uint32_t g = rows_granule((uint64_t)D * S, ld_y * S, (uintptr_t)z, (uintptr_t)y);
+    int rc = -1;
+#define ROWS_GO(E, N, KC)                                                                                                           \
+    do {                                                                                                                            \
+        const uint32_t cols = D / (N);                                                                                              \
+        const Tiling t = tile(T, cols);                                                                                             \
+        if (t.grid.y > 65535u) break;                                                                                               \
+        if (w) rc = rows_launch(combine_kernel<E, N, KC, true>, t.grid, t.block, 0, s, 0, status, T, k, cols, t.across, t.down, (const E*)z, \
+                                sorted_rows, place, w, (E*)y, ld_y);                                                                \
+        else rc = rows_launch(combine_kernel<E, N, KC, false>, t.grid, t.block, 0, s, 0, status, T, k, cols, t.across, t.down, (const E*)z,   \
+                              sorted_rows, place, w, (E*)y, ld_y);                                                                  \
+    } while (0)
+#define ROWS_TYPE(E)                                                                  \
+    do {                                                                              \
+        constexpr int kSize = sizeof(E);                                              \
+        ROWS_WITH_VEC(kSize, g, ROWS_N_##E);                                          \
+    } while (0)
+#define ROWS_N(E, N)                                                                  \
+    do {                                                                              \
+        if (k <= 2) ROWS_GO(E, N, 2); else if (k <= 4) ROWS_GO(E, N, 4); else ROWS_GO(E, N, 8); \
+    } while (0)
+#define ROWS_N_float(N) ROWS_N(float, N)
+#define ROWS_N___half(N) ROWS_N(__half, N)
+#define ROWS_N___nv_bfloat16(N) ROWS_N(__nv_bfloat16, N)
+    ROWS_WITH_TYPE(dtype, ROWS_TYPE);
+#undef ROWS_GO
+    return rc;
+}
+
+int rows_launch_combine_grad(unsigned* status, uint32_t T, uint32_t k, uint32_t D, uint32_t dtype, const void* dy, uint64_t ld_dy,
+                             const void* z, uint32_t sorted_rows, const int32_t* place, const float* w, void* dz, float* dw,
+                             cudaStream_t s)
+{
+    if (T == 0) return 0;
+    const uint32_t S = rows_elem_bytes(dtype);
+    const uint32_t g = rows_granule((uint64_t)D * S, ld_dy * S, (uintptr_t)dy, dw ? (uintptr_t)z : 0, dz ? (uintptr_t)dz : 0);
+    int rc = -1;
+#define ROWS_GO(E, N, KC)                                                                                                  \
+    do {                                                                                                                   \
+        const uint32_t cols = D / (N);                                                                                     \
+        uint32_t team = 32;                                                                                                \
+        while (team < kThreads && team * 4 < cols) team *= 2;                                                              \
+        const uint32_t each = kThreads / team;                                                                             \
+        rc = rows_launch(combine_grad_kernel<E, N, KC>, dim3((T + each - 1) / each), dim3(kThreads), 0, s, 0, status, T, k, cols, team, \
+                         (const E*)dy, ld_dy, (const E*)z, sorted_rows, place, w, (E*)dz, dw);                             \
+    } while (0)
+    ROWS_WITH_TYPE(dtype, ROWS_TYPE);
+#undef ROWS_GO
+    return rc;
+}
