@@ -433,7 +433,6 @@ constexpr uint32_t kMoveThreads = 256;
 template <int B, int M>
 __global__ void __launch_bounds__(kMoveThreads) reorder_kernel(const ReorderArgs a)
 {
-    typedef typename RowsRaw<B>::type R;
     rows_begin();
     const uint64_t og = blockIdx.x / a.col_blocks;
     const uint32_t g = (uint32_t)(og % a.G);
@@ -448,21 +447,21 @@ __global__ void __launch_bounds__(kMoveThreads) reorder_kernel(const ReorderArgs
     }
     const unsigned char* src = a.src + o * a.sp.block_pitch + (uint64_t)g * a.W * a.sp.state_pitch + piece * a.sp.piece_pitch + in * B;
     unsigned char* dst = a.dst + o * a.dp.block_pitch + (uint64_t)g * a.W * a.dp.state_pitch + piece * a.dp.piece_pitch + in * B;
-    R v[M];
-    uint32_t moves = 0;
+    RowsRaw<B> v[M];
+    int32_t from[M];
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < M; ++i) from[i] = (uint32_t)i < a.W ? __ldg(a.parent + (uint64_t)g * a.W + i) : -1;
 #pragma unroll
     for (int i = 0; i < M; ++i) {
-        const int32_t p = (uint32_t)i < a.W ? a.parent[(uint64_t)g * a.W + i] : -1;
-        if (p < -1 || p >= (int32_t)a.W) {
-            if (col == 0) atomicOr(a.status, PEARL_ST_BAD_INDEX);
-        } else if (p >= 0 && !(a.in_place && p == i)) {
-            v[i] = *reinterpret_cast<const R*>(src + (uint64_t)(uint32_t)p * a.sp.state_pitch);
-            moves |= 1u << i;
-        }
+        bad |= from[i] < -1 || from[i] >= (int32_t)a.W;
+        if ((uint32_t)from[i] >= a.W || (a.in_place && from[i] == i)) from[i] = -1;
+        rows_load_if<true>(from[i] >= 0, v[i], src + (uint64_t)(uint32_t)from[i] * a.sp.state_pitch);
     }
 #pragma unroll
     for (int i = 0; i < M; ++i)
-        if (moves >> i & 1u) *reinterpret_cast<R*>(dst + (uint64_t)i * a.dp.state_pitch) = v[i];
+        if (from[i] >= 0) rows_store(dst + (uint64_t)i * a.dp.state_pitch, v[i]);
+    if (bad && col == 0) atomicOr(a.status, PEARL_ST_BAD_INDEX);
 }
 
 template <int B>
@@ -514,7 +513,8 @@ int rows_launch_beam_reorder(unsigned* status, uint32_t blocks, uint32_t G, uint
     uint64_t all = piece_bytes | (uintptr_t)src | (uintptr_t)dst | sp.state_pitch | dp.state_pitch;
     if (pieces > 1) all |= sp.piece_pitch | dp.piece_pitch;
     if (blocks > 1) all |= sp.block_pitch | dp.block_pitch;
-    const uint32_t g = rows_granule(all);
+    uint32_t g = rows_granule(all);
+    if (g == 32 && W > 16) g = 16;          // (32 states of 32 bytes are more than a thread's registers)
     a.piece_cols = piece_bytes / g;
     a.cols = a.piece_cols * pieces;
     a.col_blocks = (a.cols + kMoveThreads - 1) / kMoveThreads;
@@ -522,6 +522,7 @@ int rows_launch_beam_reorder(unsigned* status, uint32_t blocks, uint32_t G, uint
     if (a.col_blocks > 0x7FFFFFFFull / og) return -1;
     const dim3 grid((uint32_t)(a.col_blocks * og));
     switch (g) {
+    case 32: return launch_reorder<32>(a, grid, s);
     case 16: return launch_reorder<16>(a, grid, s);
     case 8: return launch_reorder<8>(a, grid, s);
     case 4: return launch_reorder<4>(a, grid, s);

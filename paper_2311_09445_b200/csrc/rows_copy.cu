@@ -22,6 +22,23 @@ Tiling tile(uint32_t rows, uint32_t cols)
     return t;
 }
 
+// The places of KC slots from `first` on, -1 where there is none or it is out of range (which is reported once a slot).
+template <int KC>
+__device__ __forceinline__ void load_places(unsigned* status, const int32_t* __restrict__ place, uint32_t n, uint32_t sorted_rows, bool report,
+                                            int32_t (&at)[KC])
+{
+    bool bad = false;
+#pragma unroll
+    for (int j = 0; j < KC; ++j) at[j] = (uint32_t)j < n ? __ldg(place + j) : -1;
+#pragma unroll
+    for (int j = 0; j < KC; ++j)
+        if ((uint32_t)at[j] >= sorted_rows) {
+            bad |= at[j] != -1;
+            at[j] = -1;
+        }
+    if (bad && report) atomicOr(status, PEARL_ST_BAD_INDEX);
+}
+
 // ---- dispatch --------------------------------------------------------------------------------------------------------
 // xs[place[t, j]] = x[t].  A thread reads its access of row t once and writes it k times: (1 + k) rows of traffic for k
 // copies, bound by the stores.
@@ -31,23 +48,19 @@ __global__ void __launch_bounds__(kThreads) dispatch_kernel(unsigned* status, ui
                                                             const int32_t* __restrict__ place, uint32_t sorted_rows,
                                                             unsigned char* __restrict__ xs)
 {
-    typedef typename RowsRaw<B>::type R;
     rows_begin();
     const uint32_t in = threadIdx.x / across;
     const uint32_t col = threadIdx.x - in * across + blockIdx.y * across;
     const uint64_t t = (uint64_t)blockIdx.x * down + in;
     if (in >= down || t >= T || col >= cols) return;
-    const R v = rows_load(reinterpret_cast<const R*>(x + t * ld_x) + col);
-    const int32_t* p = place + t * k;
+    RowsRaw<B> v;
+    rows_load_if<false>(true, v, x + t * ld_x + (uint64_t)col * B);
     for (uint32_t j0 = 0; j0 < k; j0 += KC) {
         int32_t at[KC];
+        load_places<KC>(status, place + t * k + j0, k - j0, sorted_rows, col == 0, at);
 #pragma unroll
-        for (int j = 0; j < KC; ++j) at[j] = j0 + j < k ? __ldg(p + j0 + j) : -1;
-#pragma unroll
-        for (int j = 0; j < KC; ++j) {
-            if (at[j] >= 0 && (uint32_t)at[j] < sorted_rows) rows_store(reinterpret_cast<R*>(xs) + (uint64_t)(uint32_t)at[j] * cols + col, v);
-            else if (at[j] != -1 && col == 0) atomicOr(status, PEARL_ST_BAD_INDEX);
-        }
+        for (int j = 0; j < KC; ++j)
+            if (at[j] >= 0) rows_store(xs + ((uint64_t)(uint32_t)at[j] * cols + col) * B, v);
     }
 }
 
@@ -72,30 +85,24 @@ __global__ void __launch_bounds__(kThreads) combine_kernel(unsigned* status, uin
         int32_t at[KC];
         float wt[KC];
         RowsVec<E, N> v[KC];
+        load_places<KC>(status, place + t * k + j0, k - j0, sorted_rows, col == 0, at);
+#pragma unroll
+        for (int j = 0; j < KC; ++j) wt[j] = kWeights && j0 + j < k ? __ldg(w + t * k + j0 + j) : 1.0f;
 #pragma unroll
         for (int j = 0; j < KC; ++j) {
-            at[j] = j0 + j < k ? __ldg(place + t * k + j0 + j) : -1;
-            wt[j] = kWeights && j0 + j < k ? __ldg(w + t * k + j0 + j) : 1.0f;
-        }
-#pragma unroll
-        for (int j = 0; j < KC; ++j) {
-            if ((at[j] >= 0 && (uint32_t)at[j] >= sorted_rows) || at[j] < -1) {
-                if (col == 0) atomicOr(status, PEARL_ST_BAD_INDEX);
-                at[j] = -1;
-            }
-            if (at[j] >= 0) v[j] = rows_load_vec<E, N>(z + ((uint64_t)(uint32_t)at[j] * cols + col) * N);
+            v[j].clear();
+            rows_load_if<false>(at[j] >= 0, v[j].raw, z + ((uint64_t)(uint32_t)at[j] * cols + col) * N);
         }
 #pragma unroll
         for (int j = 0; j < KC; ++j) {
             if (at[j] < 0) continue;
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-                sum[i] = kWeights ? __fmaf_rn(wt[j], RowsElem<E>::up(v[j].e[i]), sum[i]) : __fadd_rn(sum[i], RowsElem<E>::up(v[j].e[i]));
+            for (int i = 0; i < N; ++i) sum[i] = kWeights ? __fmaf_rn(wt[j], v[j].get(i), sum[i]) : __fadd_rn(sum[i], v[j].get(i));
         }
     }
     RowsVec<E, N> out;
 #pragma unroll
-    for (int i = 0; i < N; ++i) out.e[i] = RowsElem<E>::down(sum[i]);
+    for (int i = 0; i < N; ++i) out.put(i, sum[i]);
     rows_store_vec<E, N>(y + t * ld_y + (uint64_t)col * N, out);
 }
 
@@ -118,36 +125,32 @@ __global__ void __launch_bounds__(kThreads) combine_grad_kernel(unsigned* status
     for (uint32_t j0 = 0; j0 < k; j0 += KC) {
         int32_t at[KC];
         float wt[KC], dot[KC];
+        load_places<KC>(status, place + (row ? t : 0) * k + j0, row ? k - j0 : 0u, sorted_rows, me == 0, at);
 #pragma unroll
         for (int j = 0; j < KC; ++j) {
-            const bool slot = row && j0 + j < k;
-            at[j] = slot ? __ldg(place + t * k + j0 + j) : -1;
-            wt[j] = slot && w != nullptr ? __ldg(w + t * k + j0 + j) : 1.0f;
+            wt[j] = row && j0 + j < k && w != nullptr ? __ldg(w + t * k + j0 + j) : 1.0f;
             dot[j] = 0.0f;
-            if ((at[j] >= 0 && (uint32_t)at[j] >= sorted_rows) || at[j] < -1) {
-                if (me == 0) atomicOr(status, PEARL_ST_BAD_INDEX);
-                at[j] = -1;
-            }
         }
         for (uint32_t col = me; col < cols && row; col += team) {
             const RowsVec<E, N> a = rows_load_vec<E, N>(g + (uint64_t)col * N);
-            RowsVec<E, N> v[KC];
             if (dw != nullptr) {
+                RowsVec<E, N> v[KC];
 #pragma unroll
-                for (int j = 0; j < KC; ++j)
-                    if (at[j] >= 0) v[j] = rows_load_vec<E, N>(z + ((uint64_t)(uint32_t)at[j] * cols + col) * N);
-            }
+                for (int j = 0; j < KC; ++j) rows_load_if<false>(at[j] >= 0, v[j].raw, z + ((uint64_t)(uint32_t)at[j] * cols + col) * N);
 #pragma unroll
-            for (int j = 0; j < KC; ++j) {
-                if (at[j] < 0) continue;
-                if (dw != nullptr) {
+                for (int j = 0; j < KC; ++j) {
+                    if (at[j] < 0) continue;
 #pragma unroll
-                    for (int i = 0; i < N; ++i) dot[j] = __fmaf_rn(RowsElem<E>::up(a.e[i]), RowsElem<E>::up(v[j].e[i]), dot[j]);
+                    for (int i = 0; i < N; ++i) dot[j] = __fmaf_rn(a.get(i), v[j].get(i), dot[j]);
                 }
-                if (dz != nullptr) {
+            }
+            if (dz != nullptr) {
+#pragma unroll
+                for (int j = 0; j < KC; ++j) {
+                    if (at[j] < 0) continue;
                     RowsVec<E, N> o;
 #pragma unroll
-                    for (int i = 0; i < N; ++i) o.e[i] = RowsElem<E>::down(__fmul_rn(wt[j], RowsElem<E>::up(a.e[i])));
+                    for (int i = 0; i < N; ++i) o.put(i, __fmul_rn(wt[j], a.get(i)));
                     rows_store_vec<E, N>(dz + ((uint64_t)(uint32_t)at[j] * cols + col) * N, o);
                 }
             }
@@ -181,7 +184,8 @@ __global__ void __launch_bounds__(kThreads) combine_grad_kernel(unsigned* status
 // Runs CALL(N) with the elements per access that `granule` allows for elements of S bytes.
 #define ROWS_WITH_VEC(S, granule, CALL)                                         \
     do {                                                                        \
-        if ((granule) >= 16) { CALL(16 / (S)); }                                \
+        if ((granule) >= 32) { CALL(32 / (S)); }                                \
+        else if ((granule) >= 16) { CALL(16 / (S)); }                           \
         else if ((granule) >= 8) { CALL(8 / (S)); }                             \
         else if ((granule) >= 4) { CALL(4 / (S)); }                             \
         else { CALL(1); }                                                       \
@@ -209,6 +213,7 @@ int rows_launch_dispatch(unsigned* status, uint32_t T, uint32_t k, uint32_t row_
                      place, sorted_rows, (unsigned char*)xs)
 #define ROWS_K(KC)                                                                                     \
     switch (g) {                                                                                       \
+    case 32: ROWS_GO(32, KC); break;                                                                   \
     case 16: ROWS_GO(16, KC); break;                                                                   \
     case 8: ROWS_GO(8, KC); break;                                                                     \
     case 4: ROWS_GO(4, KC); break;                                                                     \

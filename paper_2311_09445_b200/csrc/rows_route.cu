@@ -38,7 +38,7 @@ __device__ __forceinline__ bool load_logits(const E* row, uint32_t first, uint32
         for (int a = 0; a < N; a += M) {
             const RowsVec<E, M> v = rows_load_vec<E, M>(row + first + a);
 #pragma unroll
-            for (int i = 0; i < M; ++i) x[a + i] = RowsElem<E>::up(v.e[i]);
+            for (int i = 0; i < M; ++i) x[a + i] = v.get(i);
         }
     } else {
 #pragma unroll
@@ -170,7 +170,7 @@ __global__ void __launch_bounds__(kThreads) route_grad_kernel(unsigned* status, 
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const float v = over_chosen ? g[i] : __fmul_rn(__fmul_rn(__expf(__fsub_rn(x[i], shift)), p_scale), __fsub_rn(g[i], mean));
-        out[i / M].e[i % M] = RowsElem<E>::down(v);
+        out[i / M].put(i % M, v);
     }
     E* row = dlogits + t * ld_d;
     if (wide_d && lane * N + N <= experts) {
@@ -179,7 +179,7 @@ __global__ void __launch_bounds__(kThreads) route_grad_kernel(unsigned* status, 
     } else {
 #pragma unroll
         for (int i = 0; i < N; ++i)
-            if (lane * N + i < experts) row[lane * N + i] = out[i / M].e[i % M];
+            if (lane * N + i < experts) row[lane * N + i] = RowsElem<E>::down(out[i / M].get(i % M));
     }
 }
 
