@@ -9,26 +9,27 @@ namespace {
 
 constexpr float kInf = __builtin_huge_valf();
 constexpr float kLowest = -3.402823466e+38f;
-constexpr uint32_t kMostParts = 16;
 constexpr float kLog2e = 1.44269504f;
 
 // ---- selection -------------------------------------------------------------------------------------------------------
 // One thread-block cluster has a group.  A unit of work is a run of one beam's logits (the whole row, or a part of it where the
-// cluster has more CTAs than the group has beams).  A unit is read once:
-//   statistics   a thread keeps a reference value, the sum of exp(x - reference) and its largest logit.  The reference
-//                follows the largest logit only when that is more than 8 above it (e^8 terms fit a binary32 sum easily), so a
-//                logit costs one subtraction, one product, one exponential, one addition and one comparison;
-//   the best C   the threads form kTeams teams.  The C-th largest of the teams' largest logits is a bound that at least C logits
-//                reach, and only logits of the (at most C) teams whose largest reaches it can do so: those teams' logits -- a few
-//                per cent of the unit, still in L2 -- are read again and the ones that reach the bound are sorted.
+// cluster has more CTAs than the group has beams).  A unit is read once, through a ring of 16-byte slots in shared memory that
+// each thread fills and reads by itself (no barrier, 128 KB in flight on an SM with 64 registers a thread):
+//   statistics   a thread keeps a reference value, the sum of exp(x - reference), and the largest logits of its three best pairs
+//                of accesses.  The reference follows the largest logit only when that is more than 8 above
+//                it (e^8 terms fit a binary32 sum easily), so a logit costs one subtraction, one product, one exponential, one
+//                addition (two logits an instruction but for the exponential) and one comparison;
+//   the best C   in each of A warps the r-th largest of the lanes' largest logits, r = ceil(C / A), is reached by r logits, so the
+//                smallest of these bounds is reached by C.  Only threads whose largest logit reaches it can have such logits; they
+//                read their two best pairs again (from L2), and all their logits where the third-best pair reaches the bound, too.
+//                What reaches the bound -- some three times C logits -- is sorted.
 // Offers carry (logit, token) as one 64-bit key, all different, so nothing depends on the order threads arrive in.
-// The CTAs then exchange row sums and sorted lists through each other's shared memory, and the rank of an offer among the
-// group's is the sum over the lists of how many entries precede it: binary searches, one writer for each result.
-constexpr uint32_t kThreads = 256;
-constexpr uint32_t kTeams = 128;                 // >= PEARL_ROWS_MAX_BEST
-constexpr uint32_t kPerTeam = kThreads / kTeams;
-constexpr uint32_t kRoom = 2048;                 // offers that are sorted
-constexpr uint32_t kUnroll = 4;                  // accesses a thread has in flight
+// Each CTA writes its row sums and sorted lists into the shared memory of all CTAs of the cluster; after one barrier, the rank of
+// an offer among the group's is the sum over the lists of how many entries precede it: binary searches, one writer for each result.
+constexpr uint32_t kThreads = 256, kWarps = kThreads / 32;
+constexpr uint32_t kRoom = 4096;                 // offers that are sorted
+constexpr uint32_t kSlots = 8;                   // of the ring, per thread
+constexpr uint32_t kMostCtas = 16;
 
 // Keys that order like (larger logit, lower token); 0 stands for no offer.
 __device__ __forceinline__ uint32_t rising(float x)
@@ -37,10 +38,7 @@ __device__ __forceinline__ uint32_t rising(float x)
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float from_rising(uint32_t r) { return __uint_as_float(r & 0x80000000u ? r ^ 0x80000000u : ~r); }
-__device__ __forceinline__ uint64_t key_of(float x, uint32_t token)
-{
-    return x == -kInf ? 0ull : ((uint64_t)rising(x) << 32) | (0xFFFFFFFFu - token);
-}
+__device__ __forceinline__ uint64_t key_of(float x, uint32_t token) { return ((uint64_t)rising(x) << 32) | (0xFFFFFFFFu - token); }
 __device__ __forceinline__ uint64_t rising64(double x)
 {
     const uint64_t b = (uint64_t)__double_as_longlong(x + 0.0);
@@ -51,107 +49,375 @@ __device__ __forceinline__ double from_rising64(uint64_t r)
     return __longlong_as_double((long long)(r >> 63 ? r ^ 0x8000000000000000ull : ~r));
 }
 
-// Access v (N elements from element v*N of the run on) of a run of n elements at `run`, whose address is `off` bytes past a
-// 16-byte boundary: one 16-byte load where that is 0, else the two that hold it, shifted together.  The accesses are counted from
-// the run's start, not from the boundary: what a thread adds up does not depend on where the row lies in memory.  The last
-// access, and the first of a shifted run, go element by element so that nothing outside the run is read.
+__device__ __forceinline__ float exp2_of(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// log(x), x >= 1, by Tang's table-driven method (1990): x = 2^e m, c near 1/m from a table of 32, r = m c - 1 (|r| <= 2^-6), log x =
+// e log 2 - log c + log(1 + r); beyond r the series is below 2^-12 and runs in binary32.  Within 3e-11.  A few binary64 operations
+// in a row where the library's logarithm is some twenty.
+__device__ __constant__ const double kLogOf[32] = {
+    0.015748356968139168, 0.045962135564635756, 0.07500982100486657, 0.10275973395776894,
+    0.1313017372972535, 0.15839142994391764, 0.18388527877013736, 0.21004610480880948,
+    0.23443755793296864, 0.2594388601383859, 0.2824872555746769, 0.30607943759149703,
+    0.33024168687057687, 0.3522205935893521, 0.3746934494414107, 0.394780208008148,
+    0.415278729556489, 0.43620624966244487, 0.4575811092471784, 0.47627324225933093,
+    0.4953214372300254, 0.514739523087127, 0.5312143602906321, 0.5513492686996879,
+    0.5684437020589881, 0.5858354447708572, 0.6035350218702582, 0.6215535273729365,
+    0.6362058041598069, 0.6548283162578087, 0.6699801212784109, 0.6853650401178903,
+};        // -log of the numbers below
+__device__ __constant__ const float kNear[32] = {
+    504.0f / 512, 489.0f / 512, 475.0f / 512, 462.0f / 512, 449.0f / 512, 437.0f / 512, 426.0f / 512, 415.0f / 512,
+    405.0f / 512, 395.0f / 512, 386.0f / 512, 377.0f / 512, 368.0f / 512, 360.0f / 512, 352.0f / 512, 345.0f / 512,
+    338.0f / 512, 331.0f / 512, 324.0f / 512, 318.0f / 512, 312.0f / 512, 306.0f / 512, 301.0f / 512, 295.0f / 512,
+    290.0f / 512, 285.0f / 512, 280.0f / 512, 275.0f / 512, 271.0f / 512, 266.0f / 512, 262.0f / 512, 258.0f / 512,
+};        // 1 / (1 + (i + 1/2) / 32) to 9 bits
+__device__ __forceinline__ double log_of(double x)
+{
+    const uint64_t bits = (uint64_t)__double_as_longlong(x);
+    const int e = (int)(bits >> 52) - 1023;
+    const double m = __longlong_as_double((long long)((bits & 0x000FFFFFFFFFFFFFull) | 0x3FF0000000000000ull));
+    const uint32_t i = (uint32_t)(bits >> 47) & 31u;
+    const double r = fma(m, (double)kNear[i], -1.0);
+    const float f = (float)r;
+    const float tail = __fmul_rn(__fmul_rn(f, f), __fmaf_rn(f, __fmaf_rn(f, __fmaf_rn(f, 0.2f, -0.25f), 0.333333343f), -0.5f));
+    return fma((double)e, 0.693147180559945309417, kLogOf[i]) + (r + (double)tail);
+}
+
+// What an access of 16 bytes holds: words of one or two logits.
+template <typename E> struct Word;
+template <> struct Word<float> {
+    static constexpr uint32_t kMinusInf = 0xFF800000u;
+    static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }
+    static __device__ __forceinline__ float largest(uint32_t a) { return __uint_as_float(a); }
+    static __device__ __forceinline__ uint32_t bits_of(const float* p) { return __float_as_uint(*p); }
+    static __device__ __forceinline__ float get(const uint32_t (&r)[4], int i) { return __uint_as_float(r[i]); }
+    static __device__ __forceinline__ void set(uint32_t (&r)[4], int i, uint32_t bits) { r[i] = bits; }
+};
+// (i is known to the compiler: the words stay in registers)
+__device__ __forceinline__ void set_half(uint32_t (&r)[4], int i, uint32_t bits)
+{
+    r[i / 2] = i % 2 ? (r[i / 2] & 0x0000FFFFu) | bits << 16 : (r[i / 2] & 0xFFFF0000u) | (bits & 0xFFFFu);
+}
+template <> struct Word<__half> {
+    static constexpr uint32_t kMinusInf = 0xFC00FC00u;
+    static __device__ __forceinline__ __half2 as(uint32_t a) { return *reinterpret_cast<const __half2*>(&a); }
+    static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b)
+    {
+        const __half2 m = __hmax2(as(a), as(b));
+        return *reinterpret_cast<const uint32_t*>(&m);
+    }
+    static __device__ __forceinline__ float2 both(uint32_t a) { return __half22float2(as(a)); }
+    static __device__ __forceinline__ float largest(uint32_t a) { const float2 f = both(a); return fmaxf(f.x, f.y); }
+    static __device__ __forceinline__ uint32_t bits_of(const __half* p) { return __half_as_ushort(*p); }
+    static __device__ __forceinline__ float get(const uint32_t (&r)[4], int i) { const float2 f = both(r[i / 2]); return i % 2 ? f.y : f.x; }
+    static __device__ __forceinline__ void set(uint32_t (&r)[4], int i, uint32_t bits) { set_half(r, i, bits); }
+};
+template <> struct Word<__nv_bfloat16> {
+    static constexpr uint32_t kMinusInf = 0xFF80FF80u;
+    static __device__ __forceinline__ __nv_bfloat162 as(uint32_t a) { return *reinterpret_cast<const __nv_bfloat162*>(&a); }
+    static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b)
+    {
+        const __nv_bfloat162 m = __hmax2(as(a), as(b));
+        return *reinterpret_cast<const uint32_t*>(&m);
+    }
+    static __device__ __forceinline__ float2 both(uint32_t a) { return make_float2(__uint_as_float(a << 16), __uint_as_float(a & 0xFFFF0000u)); }
+    static __device__ __forceinline__ float largest(uint32_t a) { const float2 f = both(a); return fmaxf(f.x, f.y); }
+    static __device__ __forceinline__ uint32_t bits_of(const __nv_bfloat16* p) { return __bfloat16_as_ushort(*p); }
+    static __device__ __forceinline__ float get(const uint32_t (&r)[4], int i) { const float2 f = both(r[i / 2]); return i % 2 ? f.y : f.x; }
+    static __device__ __forceinline__ void set(uint32_t (&r)[4], int i, uint32_t bits) { set_half(r, i, bits); }
+};
+
+// A run of n logits.  Its accesses (N logits each, from logit v*N on) are counted from its start, not from a 16-byte boundary:
+// what a thread adds up does not depend on where a row lies in memory.  Where the start is `off` bytes past a boundary, an
+// access is the two 16-byte words that hold it, shifted together; those may hold logits of the rows beside this one, and stay
+// within [the first row's start, the last row's end): an access that would leave that is read logit by logit.
 template <typename E>
 struct Run {
     static constexpr int N = 16 / (int)sizeof(E);
     const E* run;
-    uint32_t n, off, accesses;
-    __device__ __forceinline__ void load(uint32_t v, float (&x)[N]) const
+    uint32_t n, off;
+    uint32_t accesses, full;        // ceil and floor of n / N
+    uint32_t from, upto;            // accesses from .. upto - 1 may be read as 16-byte words
+
+    __device__ __forceinline__ Run(const E* start, uint32_t count, const E* all, const E* all_end) : run(start), n(count)
     {
-        const uint64_t at = (uint64_t)v * 16u;
-        if (off == 0 ? at + 16u <= (uint64_t)n * sizeof(E) : (v > 0 && at + 32u - off <= (uint64_t)n * sizeof(E))) {
-            uint32_t q[8];
-            const uint4* p = reinterpret_cast<const uint4*>(reinterpret_cast<const unsigned char*>(run) + at - off);
-            const uint4 a = __ldg(p);
-            q[0] = a.x; q[1] = a.y; q[2] = a.z; q[3] = a.w;
-            if (off) {
-                const uint4 b = __ldg(p + 1);
-                q[4] = b.x; q[5] = b.y; q[6] = b.z; q[7] = b.w;
-                if (off & 8u) {
-#pragma unroll
-                    for (int i = 0; i < 6; ++i) q[i] = q[i + 2];
-                }
-                if (off & 4u) {
-#pragma unroll
-                    for (int i = 0; i < 5; ++i) q[i] = q[i + 1];
-                }
-                if (sizeof(E) == 2 && (off & 2u)) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) q[i] = __funnelshift_r(q[i], q[i + 1], 16);
-                }
-            }
-            const E* e = reinterpret_cast<const E*>(q);
-#pragma unroll
-            for (int i = 0; i < N; ++i) x[i] = RowsElem<E>::up(e[i]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i) x[i] = (uint64_t)v * N + i < n ? RowsElem<E>::up(run[(uint64_t)v * N + i]) : -kInf;
+        off = (uint32_t)((uintptr_t)start & 15u);
+        accesses = (n + N - 1) / N;
+        full = n / N;
+        from = (uintptr_t)start - off < (uintptr_t)all ? 1u : 0u;
+        const uint64_t room = ((uintptr_t)all_end - ((uintptr_t)start - off)) / 16u;       // 16-byte words that may be read
+        const uint64_t last = off ? (room ? room - 1 : 0) : room;
+        upto = last < accesses ? (uint32_t)last : accesses;
+    }
+    __device__ __forceinline__ bool readable(uint32_t v) const { return v >= from && v < upto; }
+    __device__ __forceinline__ const unsigned char* words(uint32_t v) const
+    {
+        return reinterpret_cast<const unsigned char*>(run) + (uint64_t)v * 16u - off;
+    }
+    // The access's logits in order, in lo, from the two words that hold it.
+    __device__ __forceinline__ void shift(RowsRaw<16>& lo, RowsRaw<16>& hi) const
+    {
+        if (off & 8u) { lo.r[0] = lo.r[2]; lo.r[1] = lo.r[3]; lo.r[2] = hi.r[0]; lo.r[3] = hi.r[1]; hi.r[0] = hi.r[2]; hi.r[1] = hi.r[3]; }
+        if (off & 4u) { lo.r[0] = lo.r[1]; lo.r[1] = lo.r[2]; lo.r[2] = lo.r[3]; lo.r[3] = hi.r[0]; hi.r[0] = hi.r[1]; }
+        if (sizeof(E) == 2 && (off & 2u)) {
+            lo.r[0] = __funnelshift_r(lo.r[0], lo.r[1], 16);
+            lo.r[1] = __funnelshift_r(lo.r[1], lo.r[2], 16);
+            lo.r[2] = __funnelshift_r(lo.r[2], lo.r[3], 16);
+            lo.r[3] = __funnelshift_r(lo.r[3], hi.r[0], 16);
         }
     }
+    // An access at an end of the run, or behind it: -infinity where there is no logit.
+    __device__ __forceinline__ void mend(uint32_t v, RowsRaw<16>& w) const
+    {
+        const bool there = readable(v);
+        const uint32_t past = v < accesses ? n - v * N : 0u;
+        if (past == 0) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w.r[i] = Word<E>::kMinusInf;
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if ((uint32_t)i >= past) Word<E>::set(w.r, i, Word<E>::kMinusInf);
+            else if (!there) Word<E>::set(w.r, i, Word<E>::bits_of(run + (uint64_t)v * N + i));
+        }
+    }
+    __device__ __forceinline__ bool whole(uint32_t v) const { return readable(v) && v < full; }
 };
 
-template <int N> __device__ __forceinline__ bool clean(float (&x)[N])
+// NaN and +infinity become -infinity; true if there were any.
+template <typename E> __device__ __forceinline__ bool clean(RowsRaw<16>& w)
 {
     bool bad = false;
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-        if (!(x[i] < kInf)) { bad = true; x[i] = -kInf; }
+    for (int i = 0; i < 16 / (int)sizeof(E); ++i)
+        if (!(Word<E>::get(w.r, i) < kInf)) { bad = true; Word<E>::set(w.r, i, Word<E>::kMinusInf); }
     return bad;
 }
+template <typename E> __device__ __forceinline__ float largest_of(const RowsRaw<16>& w)
+{
+    return Word<E>::largest(Word<E>::larger(Word<E>::larger(w.r[0], w.r[1]), Word<E>::larger(w.r[2], w.r[3])));
+}
+// The sum of exp(x - ref) over an access.  (x log2e - ref log2e as one fused operation would be off by the rounding of the second
+// product, and overflows where x - ref does not.)
+template <typename E> __device__ __forceinline__ float exp_sum(const RowsRaw<16>& w, float ref)
+{
+    constexpr int N = 16 / (int)sizeof(E);
+    float e[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) e[i] = exp2_of(__fmul_rn(__fsub_rn(Word<E>::get(w.r, i), ref), kLog2e));
+#pragma unroll
+    for (int d = N / 2; d > 0; d >>= 1)
+#pragma unroll
+        for (int i = 0; i < d; ++i) e[i] = __fadd_rn(e[i], e[i + d]);
+    return e[0];
+}
 
+// What a thread knows of its part of a run.  Its accesses are taken in pairs.  (Four at a time need a quarter fewer instructions, and
+// more than the 64 registers that let four CTAs share an SM.)
 struct Stats {
-    double sum;          // of exp(x - ref)
-    float ref, best;     // best: the largest logit, first seen in access best_at
-    uint32_t best_at;
+    double sum;                     // of exp(x - ref)
+    float ref;
+    float best, second, third;      // the largest logits of the three pairs that have the largest
+    uint32_t best_at, second_at;    // best_at: the access that has the largest logit first; second_at: any of the second pair's
     bool bad;
 };
-template <int N> __device__ __forceinline__ void take(Stats& s, float (&x)[N], uint32_t v)
+template <typename E> __device__ __forceinline__ void take(Stats& s, RowsRaw<16>& a, RowsRaw<16>& b, uint32_t v)
 {
+    float top = 0.0f, sum = 0.0f;
+    uint32_t m = 0;
 #pragma unroll 1
-    for (int again = 0; again < 2; ++again) {
-        float top = x[0];
-#pragma unroll
-        for (int i = 1; i < N; ++i) top = fmaxf(top, x[i]);
+    for (uint32_t tries = 0; tries < 2; ++tries) {
+        m = Word<E>::larger(Word<E>::larger(a.r[0], a.r[1]), Word<E>::larger(a.r[2], a.r[3]));
+        top = Word<E>::largest(Word<E>::larger(m, Word<E>::larger(Word<E>::larger(b.r[0], b.r[1]), Word<E>::larger(b.r[2], b.r[3]))));
+        sum = kInf;
         if (top < kInf) {
             if (top > __fadd_rn(s.ref, 8.0f)) {
-                s.sum *= (double)exp2f(__fmul_rn(__fsub_rn(s.ref, top), kLog2e));
+                s.sum *= (double)exp2_of(__fmul_rn(__fsub_rn(s.ref, top), kLog2e));
                 s.ref = top;
             }
-            float e[N];
+            sum = __fadd_rn(exp_sum<E>(a, s.ref), exp_sum<E>(b, s.ref));
+        }
+        if (sum < kInf) break;                       // (a NaN among the logits makes the sum one)
+        s.bad |= clean<E>(a);
+        s.bad |= clean<E>(b);
+    }
+    s.sum += (double)sum;
+    s.third = fmaxf(s.third, fminf(s.second, top));
+    if (top > s.best) {
+        s.second_at = s.best_at;
+        s.best_at = Word<E>::largest(m) == top ? v : v + kThreads;
+    } else if (top > s.second) {
+        s.second_at = v;
+    }
+    s.second = fmaxf(s.second, fminf(s.best, top));
+    s.best = fmaxf(s.best, top);
+}
+
+__device__ __forceinline__ void copy_16(uint32_t to, const unsigned char* from)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ RowsRaw<16> ring_word(uint32_t at)
+{
+    RowsRaw<16> w;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w.r[0]), "=r"(w.r[1]), "=r"(w.r[2]), "=r"(w.r[3]) : "r"(at) : "memory");
+    return w;
+}
+
+// A thread's way through a run: pair p is accesses tid + 2p * kThreads and the next one.  kDepth pairs are in the ring at a time;
+// `ring` is the shared address of the thread's slot 0, slots are kThreads * 16 bytes apart.  Two accesses are added up at a time
+// however the run lies in memory, so that equal rows have equal sums.
+template <bool kShifted, typename E>
+struct Stream {
+    static constexpr uint32_t kWords = kShifted ? 2u : 1u, kDepth = kSlots / 2 / kWords, kStep = kWords * kThreads * 16u;
+    static constexpr uint32_t kPairBytes = 2u * kThreads * 16u;
+    static __device__ __forceinline__ uint32_t pairs(const Run<E>& r) { return (r.accesses + 2 * kThreads - 1) / (2 * kThreads); }
+    // Pairs from .. plain() - 1 are whole accesses for every thread of the block.
+    static __device__ __forceinline__ uint32_t plain(const Run<E>& r) { return (r.upto < r.full ? r.upto : r.full) / (2 * kThreads); }
+    // Pair p, whose first word is at `at`, on its way into the ring (in a group of copies of its own, which may be empty).
+    static __device__ __forceinline__ void issue(const Run<E>& r, uint32_t slot, uint32_t p, const unsigned char* at, bool both)
+    {
 #pragma unroll
-            for (int i = 0; i < N; ++i) e[i] = exp2f(__fmul_rn(__fsub_rn(x[i], s.ref), kLog2e));
-#pragma unroll
-            for (int d = N / 2; d > 0; d >>= 1)
-#pragma unroll
-                for (int i = 0; i < d; ++i) e[i] = __fadd_rn(e[i], e[i + d]);
-            if (e[0] < kInf) {                       // (a NaN among the logits makes this one)
-                s.sum += (double)e[0];
-                if (top > s.best) { s.best = top; s.best_at = v; }
-                return;
+        for (uint32_t i = 0; i < 2; ++i) {
+            if (both || r.readable(threadIdx.x + (2 * p + i) * kThreads)) {
+                copy_16(slot + i * kStep, at + i * kThreads * 16u);
+                if (kShifted) copy_16(slot + i * kStep + kThreads * 16u, at + i * kThreads * 16u + 16);
             }
         }
-        s.bad |= clean<N>(x);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    static __device__ __forceinline__ void start(const Run<E>& r, uint32_t ring)
+    {
+        const unsigned char* at = r.words(threadIdx.x);
+#pragma unroll 1
+        for (uint32_t p = 0; p < kDepth; ++p) issue(r, ring + p * 2 * kStep, p, at + p * kPairBytes, p >= r.from && p < plain(r));
+    }
+    static __device__ __forceinline__ void finish() { asm volatile("cp.async.wait_group 0;" ::: "memory"); }
+    // (a function of its own: inlined, the registers of what follows it in the kernel are spilled inside this loop)
+    static __device__ __noinline__ Stats run(const Run<E> r, uint32_t ring)
+    {
+        Stats s{0.0, kLowest, -kInf, -kInf, -kInf, 0u, 0u, false};
+        const uint32_t all = pairs(r), plain_pairs = plain(r), last = ring + (kDepth - 1) * 2 * kStep;
+        const unsigned char* at = r.words(threadIdx.x) + kDepth * kPairBytes;
+        uint32_t slot = ring;
+#pragma unroll 1
+        for (uint32_t p = 0; p < all; ++p) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
+            RowsRaw<16> a = ring_word(slot), b = ring_word(slot + kStep);
+            if (kShifted) {
+                RowsRaw<16> a_hi = ring_word(slot + kThreads * 16u), b_hi = ring_word(slot + kStep + kThreads * 16u);
+                r.shift(a, a_hi);
+                r.shift(b, b_hi);
+            }
+            const uint32_t v = threadIdx.x + 2 * p * kThreads;
+            if (p >= plain_pairs || p < r.from) {
+                if (!r.whole(v)) r.mend(v, a);
+                if (!r.whole(v + kThreads)) r.mend(v + kThreads, b);
+            }
+            take<E>(s, a, b, v);
+            issue(r, slot, p + kDepth, at, p + kDepth < plain_pairs);          // (into the slots that have just been read)
+            at += kPairBytes;
+            slot = slot == last ? ring : slot + 2 * kStep;
+        }
+        finish();
+        return s;
+    }
+};
+
+// The logits of the pair of accesses that `access` is one of that reach the bound, appended to `offers`.
+template <typename E>
+__device__ __noinline__ void collect(const Run<E> r, uint32_t access, uint64_t at_least, uint32_t first, uint64_t* offers, uint32_t* n_offers)
+{
+    constexpr int N = Run<E>::N;
+    access -= access / kThreads % 2u * kThreads;
+    RowsRaw<16> w[2], hi[2];
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+        rows_load_if<false>(r.readable(access + m * kThreads), w[m], r.words(access + m * kThreads));
+        if (r.off) rows_load_if<false>(r.readable(access + m * kThreads), hi[m], r.words(access + m * kThreads) + 16);
+    }
+    const bool every = at_least == 1u;
+    const float low = every ? 0.0f : from_rising((uint32_t)(at_least >> 32));
+    const uint32_t last = 0xFFFFFFFFu - (uint32_t)at_least;               // of equal logits those up to this token
+    uint32_t reach = 0;                                                   // bit m * N + j: logit j of access m reaches the bound
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+        if (r.off) r.shift(w[m], hi[m]);
+        if (!r.whole(access + m * kThreads)) r.mend(access + m * kThreads, w[m]);
+        if (!every && largest_of<E>(w[m]) < low) continue;
+        const uint32_t token = first + (access + m * kThreads) * N, equals = token <= last ? last - token + 1u : 0u;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const float x = Word<E>::get(w[m].r, j);
+            if (x < kInf && x > -kInf && (every || x > low || (x == low && (uint32_t)j < equals))) reach |= 1u << (m * N + j);
+        }
+    }
+    uint32_t to = reach ? atomicAdd(n_offers, (uint32_t)__popc(reach)) : 0u;
+    for (; reach; reach &= reach - 1u) {
+        const uint32_t at = __ffs(reach) - 1u;
+        uint32_t word = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (at / (N / 4) == (uint32_t)i) word = w[i / 4].r[i % 4];
+        float x;
+        if constexpr (N == 4) x = __uint_as_float(word);
+        else { const float2 f = Word<E>::both(word); x = at & 1u ? f.y : f.x; }
+        if (to < kRoom) offers[to] = key_of(x, first + (access + at / N * kThreads) * N + at % N);
+        ++to;
     }
 }
 
-// What the CTAs of a cluster leave for one another, one entry per unit of the CTA.
+// What the CTAs of a cluster tell one another of a unit.
 struct UnitSum {
     double sum;
     float ref;
     uint32_t offers;
 };
 
-// The sorted list's place of `key` (entries that precede it): the list falls.
+// A transfer into the shared memory of CTA `rank`: value to where this CTA has `to`, counted by that CTA's barrier.
+__device__ __forceinline__ uint32_t in_cta(uint32_t at, uint32_t rank)
+{
+    uint32_t there;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(rank));
+    return there;
+}
+__device__ __forceinline__ void send(uint32_t to, uint32_t barrier, uint32_t rank, uint64_t value)
+{
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b64 [%0], %1, [%2];"
+                 ::"r"(in_cta(to, rank)), "l"(value), "r"(in_cta(barrier, rank)) : "memory");
+}
+__device__ __forceinline__ void send(uint32_t to, uint32_t barrier, uint32_t rank, const UnitSum& s)
+{
+    const uint64_t ref_offers = (uint64_t)__float_as_uint(s.ref) | (uint64_t)s.offers << 32;
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.b64 [%0], {%1, %2}, [%3];"
+                 ::"r"(in_cta(to, rank)), "l"((uint64_t)__double_as_longlong(s.sum)), "l"(ref_offers), "r"(in_cta(barrier, rank)) : "memory");
+}
+// Waits until all of them are here; the barrier's one phase.  Every CTA of the cluster sends a fixed number of bytes, so this
+// ends; should it not, the limit ends it (PEARL_ST_INTERNAL, the group's results are missing).
+constexpr uint32_t kPolls = 1u << 22;
+__device__ __forceinline__ bool arrived(uint32_t barrier)
+{
+    for (uint32_t i = 0; i < kPolls; ++i) {
+        uint32_t ok;
+        asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], 0; selp.u32 %0, 1, 0, p; }"
+                     : "=r"(ok) : "r"(barrier) : "memory");
+        if (ok) return true;
+    }
+    return false;
+}
+
+// The entries of a falling list that precede `key`.
 __device__ __forceinline__ uint32_t preceding(const uint64_t* list, uint32_t n, uint64_t key, bool equal_precedes)
 {
+    const uint64_t bar = key - (equal_precedes ? 1u : 0u);                // (keys are not 0)
     uint32_t lo = 0, hi = n;
     while (lo < hi) {
         const uint32_t mid = (lo + hi) / 2;
-        if (list[mid] > key || (equal_precedes && list[mid] == key)) lo = mid + 1;
+        if (list[mid] > bar) lo = mid + 1;
         else hi = mid;
     }
     return lo;
@@ -159,9 +425,9 @@ __device__ __forceinline__ uint32_t preceding(const uint64_t* list, uint32_t n, 
 
 struct SelectArgs {
     unsigned* status;
-    uint32_t W, V, C;
+    uint32_t G, W, V, C;
     uint32_t parts;             // runs a row is cut into
-    uint32_t run;               // elements of a run (a multiple of 8)
+    uint32_t run;               // logits of a run (a multiple of 8)
     uint32_t units_per_cta;
     const void* logits;
     uint64_t ld;
@@ -173,124 +439,133 @@ struct SelectArgs {
     int32_t* best_token;
 };
 
-// Dynamic shared memory: keys[units_per_cta][C] and sums[units_per_cta] (this CTA's, read by the others), then the workspace:
-// kRoom offers, later all_totals[units][C], all_keys[units][C].
+// Dynamic shared memory: all_keys[units][C], which every CTA of the cluster writes its lists to, and a workspace that is the ring,
+// then the offers to be sorted (kRoom), then all_totals[units][C].
 template <typename E>
-__global__ void __launch_bounds__(kThreads) select_kernel(const SelectArgs a)
+__global__ void __launch_bounds__(kThreads, 4) select_kernel(const SelectArgs a)
 {
     extern __shared__ __align__(16) unsigned char shared[];
-    __shared__ uint64_t team_best[kTeams];
-    __shared__ uint32_t picked[kTeams];
-    __shared__ uint32_t n_picked, n_offers;
-    __shared__ uint64_t bound;
-    __shared__ double warp_sum[kThreads / 32];
-    __shared__ float warp_ref[kThreads / 32];
+    __shared__ uint64_t barrier;
+    __shared__ __align__(16) UnitSum all_sums[PEARL_ROWS_MAX_BEAMS];
+    __shared__ uint64_t warp_bound[kWarps];
+    __shared__ uint64_t warp_sum[kWarps];
+    __shared__ float warp_ref[kWarps];
+    __shared__ uint2 deep[kThreads];
+    __shared__ uint32_t n_deep, n_offers, n_all;
+    __shared__ float score_of[PEARL_ROWS_MAX_BEAMS];
+    __shared__ uint8_t done_of[PEARL_ROWS_MAX_BEAMS];
+    __shared__ double lse[PEARL_ROWS_MAX_BEAMS];
     constexpr int N = Run<E>::N;
     cg::cluster_group cluster = cg::this_cluster();
     const uint32_t ctas = cluster.num_blocks(), cta = cluster.block_rank(), g = blockIdx.x / ctas;
     const uint32_t units = a.W * a.parts, C = a.C, tid = threadIdx.x, lane = tid & 31u, warp = tid / 32;
-    uint64_t* keys = reinterpret_cast<uint64_t*>(shared);
-    UnitSum* sums = reinterpret_cast<UnitSum*>(keys + a.units_per_cta * C);
-    uint64_t* work = reinterpret_cast<uint64_t*>(sums + a.units_per_cta);
+    uint64_t* all_keys = reinterpret_cast<uint64_t*>(shared);
+    uint64_t* work = all_keys + (units * C + 1) / 2 * 2;
+    const uint32_t keys_at = (uint32_t)__cvta_generic_to_shared(all_keys), sums_at = (uint32_t)__cvta_generic_to_shared(all_sums);
+    const uint32_t bar = (uint32_t)__cvta_generic_to_shared(&barrier), ring = (uint32_t)__cvta_generic_to_shared(work) + tid * 16u;
+    if (tid == 0) {
+        asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar) : "memory");
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(units * (C * 8u + (uint32_t)sizeof(UnitSum))) : "memory");
+        n_all = 0;
+    }
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     rows_begin();
 
+    const E* all = reinterpret_cast<const E*>(a.logits);
+    const E* all_end = all + ((uint64_t)a.G * a.W - 1) * a.ld + a.V;
     for (uint32_t q = 0; q < a.units_per_cta; ++q) {
         const uint32_t u = cta * a.units_per_cta + q;
-        uint64_t* mine = keys + q * C;
-        if (u >= units) break;
-        const uint32_t b = u / a.parts, part = u % a.parts;
-        const uint64_t row = (uint64_t)g * a.W + b;
-        float score = a.scores[row];
-        if (!(score < kInf)) {
-            if (tid == 0 && part == 0) atomicOr(a.status, PEARL_ST_BAD_SCORE);
-            score = -kInf;
-        }
-        const bool done = a.done != nullptr && a.done[row] != 0;
+        const uint32_t b = u < units ? u / a.parts : 0u, part = u < units ? u - b * a.parts : 0u;
         const uint64_t first = (uint64_t)part * a.run;
-        if (score == -kInf || done || first >= a.V) {
-            // no logits are read; a finished beam has one offer, whose key only has to be valid
-            const uint32_t n = done && score > -kInf && part == 0 ? 1u : 0u;
-            for (uint32_t i = tid; i < C; i += kThreads) mine[i] = i < n ? key_of(0.0f, 0u) : 0ull;
-            if (tid == 0) sums[q] = UnitSum{0.0, kLowest, n};
+        const bool any = u < units && first < a.V;
+        const Run<E> r(all + ((uint64_t)g * a.W + b) * a.ld + (any ? first : 0), any ? (uint32_t)(a.V - first < a.run ? a.V - first : a.run) : 0u, all,
+                       all_end);
+        if (r.off) Stream<true, E>::start(r, ring);
+        else Stream<false, E>::start(r, ring);
+        if (q == 0) {
+            // (the first logits are on their way while the scores are read)
+            if (tid < a.W) {
+                const uint64_t row = (uint64_t)g * a.W + tid;
+                float score = a.scores[row];
+                done_of[tid] = a.done != nullptr && a.done[row] != 0;
+                if (!(score < kInf)) {
+                    if (cta == 0) atomicOr(a.status, PEARL_ST_BAD_SCORE);
+                    score = -kInf;
+                }
+                score_of[tid] = score;
+            }
+            __syncwarp();
+            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");      // the others' barriers may be used from here on
+            __syncthreads();
+        }
+        if (u >= units) {
+            Stream<false, E>::finish();
+            break;
+        }
+        const uint32_t mine = keys_at + u * C * 8u;
+        if (score_of[b] == -kInf || done_of[b] || !any) {
+            // the logits do not matter; a finished beam has one offer, whose key only has to be valid
+            Stream<false, E>::finish();
+            const uint32_t n = done_of[b] && score_of[b] > -kInf && part == 0 ? 1u : 0u;
+            for (uint32_t i = tid; i < C * ctas; i += kThreads) send(mine + i % C * 8u, bar, i / C, i % C < n ? key_of(0.0f, 0u) : 0ull);
+            if (tid < ctas) send(sums_at + u * (uint32_t)sizeof(UnitSum), bar, tid, UnitSum{0.0, kLowest, n});
             continue;
         }
-        Run<E> r;
-        r.run = reinterpret_cast<const E*>(a.logits) + row * a.ld + first;
-        r.n = (uint32_t)(a.V - first < a.run ? a.V - first : a.run);
-        r.off = (uint32_t)((uintptr_t)r.run & 15u);
-        r.accesses = (r.n + N - 1) / N;
-
-        Stats s{0.0, kLowest, -kInf, 0u, false};
-        uint32_t v = tid;
-        for (; v + (kUnroll - 1) * kThreads < r.accesses; v += kUnroll * kThreads) {
-            float x[kUnroll][N];
-#pragma unroll
-            for (int i = 0; i < (int)kUnroll; ++i) r.load(v + i * kThreads, x[i]);
-#pragma unroll
-            for (int i = 0; i < (int)kUnroll; ++i) take<N>(s, x[i], v + i * kThreads);
-        }
-        for (; v < r.accesses; v += kThreads) {
-            float x[N];
-            r.load(v, x);
-            take<N>(s, x, v);
-        }
+        const Stats s = r.off ? Stream<true, E>::run(r, ring) : Stream<false, E>::run(r, ring);
         if (s.bad) atomicOr(a.status, PEARL_ST_BAD_SCORE);
 
-        // the unit's sum: relative to the largest reference, added in a fixed order
-        float ref = s.ref;
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) ref = fmaxf(ref, __shfl_xor_sync(0xFFFFFFFFu, ref, d));
-        if (lane == 0) warp_ref[warp] = ref;
-        // a team's largest logit, as the smallest key that a logit of its access can have
-        uint64_t key = s.best == -kInf ? 0ull : key_of(s.best, (uint32_t)first + s.best_at * N + N - 1);
-#pragma unroll
-        for (uint32_t d = 1; d < kPerTeam; d <<= 1) {
-            const uint64_t o = __shfl_xor_sync(0xFFFFFFFFu, key, d);
-            key = o > key ? o : key;
+        // a bound that C logits reach: the smallest key that the logit of its access can have stands for it
+        const uint64_t key = s.best == -kInf ? 0ull : key_of(s.best, (uint32_t)first + s.best_at * N + N - 1);
+        const uint32_t full_warps = r.accesses / 32u;
+        const uint32_t active = full_warps < 1u ? 1u : full_warps < kWarps ? full_warps : kWarps;
+        const uint32_t need = (C + active - 1) / active;
+        uint64_t mark = ~0ull;
+        if (warp < active) {
+            uint32_t left = (uint32_t)(key >> 32), top = 0, had = 0;
+            do {
+                top = __reduce_max_sync(0xFFFFFFFFu, left);
+                had += __popc(__ballot_sync(0xFFFFFFFFu, left == top));
+                if (had < need && left == top) left = 0;
+            } while (had < need && top);
+            const uint32_t low = __reduce_min_sync(0xFFFFFFFFu, (uint32_t)(key >> 32) == top ? (uint32_t)key : 0xFFFFFFFFu);
+            mark = top ? ((uint64_t)top << 32) | low : 1ull;                 // (too few lanes have a logit: every logit is an offer)
         }
-        if (tid % kPerTeam == 0) team_best[tid / kPerTeam] = key;
-        if (tid == 0) { n_picked = 0; n_offers = 0; bound = 1ull; }
-        __syncthreads();
-        ref = warp_ref[0];
-#pragma unroll
-        for (uint32_t i = 1; i < kThreads / 32; ++i) ref = fmaxf(ref, warp_ref[i]);
-        double sum = s.sum > 0.0 ? s.sum * exp((double)s.ref - (double)ref) : 0.0;
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
-        if (lane == 0) warp_sum[warp] = sum;
-        // the C-th largest of the teams' keys (teams without a logit have none: the bound stays at the lowest key)
-        if (tid < kTeams) {
-            const uint64_t k = team_best[tid];
-            uint32_t ahead = 0;
-            for (uint32_t i = 0; i < kTeams; ++i) ahead += team_best[i] > k || (team_best[i] == k && i < tid);
-            if (ahead == C - 1 && k) bound = k;
+        // the warp's sum relative to its largest reference, in fixed point (30 bits behind the point: the sum is 1 at least if there
+        // is a logit, and 2^60 of these at most): whole numbers add up in any order, three limbs of 22 bits at a time
+        {
+            const float ref = from_rising(__reduce_max_sync(0xFFFFFFFFu, rising(s.ref)));
+            const double scaled = s.sum * (double)exp2_of(__fmul_rn(__fsub_rn(s.ref, ref), kLog2e));
+            const uint64_t fixed = (uint64_t)__double2ull_rn(scaled * 1073741824.0);
+            const uint64_t sum = (uint64_t)__reduce_add_sync(0xFFFFFFFFu, (uint32_t)fixed & 0x3FFFFFu) +
+                                 ((uint64_t)__reduce_add_sync(0xFFFFFFFFu, (uint32_t)(fixed >> 22) & 0x3FFFFFu) << 22) +
+                                 ((uint64_t)__reduce_add_sync(0xFFFFFFFFu, (uint32_t)(fixed >> 44)) << 44);
+            if (lane == 0) { warp_bound[warp] = mark; warp_sum[warp] = sum; warp_ref[warp] = ref; }
         }
+        if (tid == 0) { n_deep = 0; n_offers = 0; }
         __syncthreads();
-        if (tid < kTeams && team_best[tid] && (team_best[tid] | (uint64_t)(N - 1)) >= bound) picked[atomicAdd(&n_picked, 1u)] = tid;
-        __syncthreads();
+        uint64_t lowest = warp_bound[0];
+#pragma unroll
+        for (uint32_t i = 1; i < kWarps; ++i) lowest = warp_bound[i] < lowest ? warp_bound[i] : lowest;
 
-        // the picked teams' logits that reach the bound.  Should they be more than there is room for, the bound is searched by
-        // halving (`low`: too many reach it, `high`: fewer than C do; the keys are all different, so some key has a number between).
-        const uint32_t rounds = (r.accesses + kThreads - 1) / kThreads;
-        const uint64_t lowest = bound;
+        // The logits that reach the bound.  Should they be more than there is room for, the bound is searched by halving (`low`: too
+        // many reach it, `high`: fewer than C do; the keys are all different, so some key has a number between).
         uint64_t low = lowest, high = ~0ull, at_least = lowest;
         for (;;) {
-            for (uint32_t p = warp; p < n_picked; p += kThreads / 32) {
-                for (uint32_t i = lane; i < rounds * kPerTeam; i += 32) {
-                    const uint32_t at = picked[p] * kPerTeam + i % kPerTeam + i / kPerTeam * kThreads;
-                    if (at >= r.accesses) continue;
-                    float x[N];
-                    r.load(at, x);
-                    clean<N>(x);
-#pragma unroll
-                    for (int j = 0; j < N; ++j) {
-                        const uint64_t k = key_of(x[j], (uint32_t)first + at * N + j);
-                        if (k >= at_least) {
-                            const uint32_t to = atomicAdd(&n_offers, 1u);
-                            if (to < kRoom) work[to] = k;
-                        }
-                    }
-                }
+            const float low_logit = from_rising((uint32_t)(at_least >> 32));              // (NaN for the lowest key)
+            if (s.best > -kInf && !(s.best < low_logit)) {          // (low_logit is NaN for the lowest key)
+                collect<E>(r, s.best_at, at_least, (uint32_t)first, work, &n_offers);
+                if (s.second > -kInf && !(s.second < low_logit)) collect<E>(r, s.second_at, at_least, (uint32_t)first, work, &n_offers);
+                if (s.third > -kInf && !(s.third < low_logit)) deep[atomicAdd(&n_deep, 1u)] = make_uint2(s.best_at, s.second_at);
+            }
+            __syncthreads();
+            const uint32_t a_thread = Stream<false, E>::pairs(r), all_deep = n_deep * a_thread;
+            for (uint32_t i = tid; i < all_deep; i += kThreads) {
+                const uint2 d = deep[i / a_thread];
+                const uint32_t p = i % a_thread;
+                if (p != d.x / (2 * kThreads) && p != d.y / (2 * kThreads))
+                    collect<E>(r, d.x % kThreads + 2 * p * kThreads, at_least, (uint32_t)first, work, &n_offers);
             }
             __syncthreads();
             const uint32_t n = n_offers;
@@ -299,19 +574,34 @@ __global__ void __launch_bounds__(kThreads) select_kernel(const SelectArgs a)
             else high = at_least;
             at_least = low + (high - low) / 2;
             __syncthreads();
-            if (tid == 0) n_offers = 0;
+            if (tid == 0) { n_deep = 0; n_offers = 0; }
             __syncthreads();
         }
         const uint32_t n = n_offers;
-        for (uint32_t i = tid; i < C; i += kThreads)
-            if (i >= n) mine[i] = 0ull;
+        if (warp == kWarps - 1) {
+            // the unit's sum, relative to the largest reference, added in a fixed order
+            const float mine_ref = lane < kWarps ? warp_ref[lane] : kLowest;
+            const float ref = from_rising(__reduce_max_sync(0xFFFFFFFFu, rising(mine_ref)));
+            double sum = lane < kWarps ? (double)warp_sum[lane] * (1.0 / 1073741824.0) * (double)exp2_of(__fmul_rn(__fsub_rn(mine_ref, ref), kLog2e)) : 0.0;
+#pragma unroll
+            for (uint32_t d = 1; d < kWarps; d <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
+            sum = __shfl_sync(0xFFFFFFFFu, sum, 0);
+            if (lane < ctas) send(sums_at + u * (uint32_t)sizeof(UnitSum), bar, lane, UnitSum{sum, ref, n < C ? n : C});
+        }
+        for (uint32_t i = n + tid; i < C; i += kThreads)
+            for (uint32_t c = 0; c < ctas; ++c) send(mine + i * 8u, bar, c, 0ull);
         if (n <= kThreads) {
-            if (tid < n) {
-                const uint64_t k = work[tid];
-                uint32_t ahead = 0;
-                for (uint32_t i = 0; i < n; ++i) ahead += work[i] > k;
-                if (ahead < C) mine[ahead] = k;
-            }
+            // 2^shift lanes count the offers ahead of one, and hand it to the CTAs
+            uint32_t shift = 5;
+            while (n << shift > kThreads) --shift;
+            const uint32_t each = 1u << shift, i = tid >> shift, sub = tid & (each - 1);
+            const uint64_t k = i < n ? work[i] : 0ull;
+            uint32_t ahead = 0;
+#pragma unroll 4
+            for (uint32_t o = sub; o < n; o += each) ahead += work[o] > k;
+            for (uint32_t d = 1; d < each; d *= 2) ahead += __shfl_xor_sync(0xFFFFFFFFu, ahead, d);
+            if (i < n && ahead < C)
+                for (uint32_t c = sub; c < ctas; c += each) send(mine + ahead * 8u, bar, c, k);
         } else {
             uint32_t size = kThreads;
             while (size < n) size *= 2;
@@ -320,96 +610,76 @@ __global__ void __launch_bounds__(kThreads) select_kernel(const SelectArgs a)
                 for (uint32_t step = span / 2; step > 0; step /= 2) {
                     __syncthreads();
                     for (uint32_t i = tid; i < size / 2; i += kThreads) {
-                        const uint32_t x = i / step * step * 2 + i % step, y = x + step;
+                        const uint32_t x = (i & ~(step - 1)) * 2 + (i & (step - 1)), y = x + step;
                         const uint64_t p = work[x], o = work[y];
                         if ((p < o) == ((x & span) == 0)) { work[x] = o; work[y] = p; }
                     }
                 }
             __syncthreads();
-            for (uint32_t i = tid; i < C; i += kThreads) mine[i] = work[i];
+            for (uint32_t i = tid; i < C * ctas; i += kThreads) send(mine + i % C * 8u, bar, i / C, work[i % C]);
         }
-        if (tid == 0) {
-            double total = 0.0;
-            for (uint32_t i = 0; i < kThreads / 32; ++i) total += warp_sum[i];
-            sums[q] = UnitSum{total, ref, n < C ? n : C};
-        }
-        __syncthreads();                  // (the next unit uses the same workspace)
+        if (q + 1 < a.units_per_cta) __syncthreads();                      // (the next unit uses the same workspace)
     }
-    cluster.sync();
-
-    // every CTA: the group's row sums and lists, copied from where they are
-    __shared__ double lse[PEARL_ROWS_MAX_BEAMS];
-    __shared__ uint32_t n_all;
-    uint64_t* all_keys = work;
-    uint64_t* all_totals = work + units * C;
-    if (tid == 0) n_all = 0;
+    if (!arrived(bar)) atomicOr(a.status, PEARL_ST_INTERNAL);
     __syncthreads();
+
     if (tid < a.W) {
-        UnitSum part[kMostParts];
         float ref = kLowest;
         uint32_t offers = 0;
-        for (uint32_t i = 0; i < a.parts; ++i) {
-            const uint32_t u = tid * a.parts + i;
-            part[i] = *cluster.map_shared_rank(sums + u % a.units_per_cta, u / a.units_per_cta);
-            ref = fmaxf(ref, part[i].ref);
-            offers += part[i].offers;
-        }
+        for (uint32_t i = 0; i < a.parts; ++i) ref = fmaxf(ref, all_sums[tid * a.parts + i].ref);
         double sum = 0.0;
-        for (uint32_t i = 0; i < a.parts; ++i)
-            if (part[i].sum > 0.0) sum += part[i].sum * exp((double)part[i].ref - (double)ref);
-        lse[tid] = (double)ref + log(sum);
+        for (uint32_t i = 0; i < a.parts; ++i) {
+            const UnitSum& p = all_sums[tid * a.parts + i];
+            sum += p.sum * (double)exp2_of(__fmul_rn(__fsub_rn(p.ref, ref), kLog2e));
+            offers += p.offers;
+        }
+        lse[tid] = (double)ref + log_of(sum);
         atomicAdd(&n_all, offers);
     }
-    for (uint32_t i = tid; i < units * C; i += kThreads) {
-        const uint32_t u = i / C;
-        all_keys[i] = cluster.map_shared_rank(keys + u % a.units_per_cta * C, u / a.units_per_cta)[i % C];
-    }
-    cluster.sync();                       // (nobody reads this CTA's memory from here on)
+    __syncthreads();
+    uint64_t* all_totals = work;
     for (uint32_t i = tid; i < units * C; i += kThreads) {
         const uint32_t b = i / C / a.parts;
-        const uint64_t row = (uint64_t)g * a.W + b, k = all_keys[i];
-        const double score = (double)a.scores[row];
-        const bool done = a.done != nullptr && a.done[row] != 0;
-        all_totals[i] = k == 0 ? 0ull : rising64(done ? score : score + ((double)from_rising((uint32_t)(k >> 32)) - lse[b]));
+        const uint64_t k = all_keys[i];
+        const double score = (double)score_of[b];
+        all_totals[i] = k == 0 ? 0ull : rising64(done_of[b] ? score : score + ((double)from_rising((uint32_t)(k >> 32)) - lse[b]));
     }
     __syncthreads();
 
-    // the place of each offer of this CTA's units: kLanes lanes share the lists that may hold offers before it
-    constexpr uint32_t kLanes = 8;
-    const uint32_t own = a.units_per_cta * C;
-    for (uint32_t i0 = 0; i0 < own; i0 += kThreads / kLanes) {
-        const uint32_t i = i0 + tid / kLanes;
-        const uint32_t u = cta * a.units_per_cta + i / C;
-        const bool there = i < own && u < units && all_keys[u * C + i % C] != 0;
-        const uint32_t b = u / a.parts;
-        uint32_t place = 0;
-        uint64_t key = 0, total = 0;
-        if (there) {
-            key = all_keys[u * C + i % C];
-            total = all_totals[u * C + i % C];
-            for (uint32_t o = tid % kLanes; o < units; o += kLanes) {
-                if (o / a.parts == b) place += preceding(all_keys + o * C, C, key, false);
-                else place += preceding(all_totals + o * C, C, total, o < u);
+    // the place of each offer of this CTA's units: 2^shift lanes share the lists that may hold offers before it
+    uint32_t shift = 5;
+    while (shift > 0 && C << shift > kThreads) --shift;
+    const uint32_t each = 1u << shift, sub = tid & (each - 1);
+    for (uint32_t q = 0; q < a.units_per_cta; ++q) {
+        const uint32_t u = cta * a.units_per_cta + q, b = u / a.parts, rows_from = b * a.parts, rows_to = rows_from + a.parts;
+        if (u >= units) break;
+        const uint64_t* mine = all_keys + u * C;
+        for (uint32_t i0 = 0; i0 < C; i0 += kThreads >> shift) {
+            const uint32_t i = i0 + (tid >> shift);
+            const uint64_t key = i < C ? mine[i] : 0ull, total = i < C ? all_totals[u * C + i] : 0ull;
+            uint32_t place = 0;
+            if (key)
+                for (uint32_t o = sub; o < units; o += each) {
+                    if (o == u) place += i;
+                    else if (o >= rows_from && o < rows_to) place += preceding(all_keys + o * C, C, key, false);
+                    else place += preceding(all_totals + o * C, C, total, o < u);
+                }
+            for (uint32_t d = 1; d < each; d *= 2) place += __shfl_xor_sync(0xFFFFFFFFu, place, d);
+            if (key && sub == 0 && place < C) {
+                const uint64_t to = (uint64_t)g * C + place;
+                a.best_score[to] = (float)from_rising64(total);
+                a.best_beam[to] = (int32_t)b;
+                a.best_token[to] = done_of[b] ? a.end_token : (int32_t)(0xFFFFFFFFu - (uint32_t)key);
             }
-        }
-#pragma unroll
-        for (uint32_t d = 1; d < kLanes; d <<= 1) place += __shfl_xor_sync(0xFFFFFFFFu, place, d);
-        if (there && tid % kLanes == 0 && place < C) {
-            const uint64_t row = (uint64_t)g * a.W + b, to = (uint64_t)g * C + place;
-            const bool done = a.done != nullptr && a.done[row] != 0;
-            a.best_score[to] = (float)from_rising64(total);
-            a.best_beam[to] = (int32_t)b;
-            a.best_token[to] = done ? a.end_token : (int32_t)(0xFFFFFFFFu - (uint32_t)key);
         }
     }
     if (cta == 0)
-        for (uint32_t i = tid; i < C; i += kThreads)
-            if (i >= n_all) {
-                const uint64_t to = (uint64_t)g * C + i;
-                a.best_score[to] = -kInf;
-                a.best_beam[to] = -1;
-                a.best_token[to] = -1;
-            }
+        for (uint32_t i = n_all + tid; i < C; i += kThreads) {
+            const uint64_t to = (uint64_t)g * C + i;
+            a.best_score[to] = -kInf;
+            a.best_beam[to] = -1;
+            a.best_token[to] = -1;
+        }
 }
 
 // ---- the states ------------------------------------------------------------------------------------------------------
@@ -480,21 +750,22 @@ int rows_launch_beam_select(unsigned* status, uint32_t G, uint32_t W, uint32_t V
                             int32_t* best_beam, int32_t* best_token, cudaStream_t s)
 {
     if (G == 0) return 0;
-    // Rows are cut into parts where there are too few of them to occupy the GPU; a part has 2048 logits at least.
+    // Rows are cut into parts where there are too few of them to occupy the GPU; a part has 1024 logits at least.
     SelectArgs a;
-    const uint32_t most = 8;
+    const uint32_t most = (uint64_t)G * kMostCtas <= (uint64_t)rows_sm_count() && W <= kMostCtas ? kMostCtas : 8u;
     a.units_per_cta = (W + most - 1) / most;
     a.parts = 1;
-    while ((a.parts + 1) * W <= most && (uint64_t)G * W * a.parts < 592 && V / (a.parts + 1) >= 2048) ++a.parts;
+    while ((a.parts + 1) * W <= most && (uint64_t)G * W * a.parts < 592 && V / (a.parts + 1) >= 1024) ++a.parts;
     a.run = ((V + a.parts - 1) / a.parts + 7) / 8 * 8;
     const uint32_t units = W * a.parts, ctas = (units + a.units_per_cta - 1) / a.units_per_cta;
     if ((uint64_t)G * ctas > 0x7FFFFFFFull) return -1;
-    a.status = status; a.W = W; a.V = V; a.C = C; a.logits = logits; a.ld = ld; a.scores = scores; a.done = done; a.end_token = end_token;
+    a.status = status; a.G = G; a.W = W; a.V = V; a.C = C; a.logits = logits; a.ld = ld; a.scores = scores; a.done = done; a.end_token = end_token;
     a.best_score = best_score; a.best_beam = best_beam; a.best_token = best_token;
-    const size_t lists = (size_t)units * C * 16, offers = kRoom * 8;
-    const size_t smem = a.units_per_cta * (C * 8 + sizeof(UnitSum)) + (lists > offers ? lists : offers);
+    const size_t keys = ((size_t)units * C + 1) / 2 * 16, ring = kThreads * kSlots * 16;         // (the ring is the largest use of the workspace)
     int rc = -1;
-#define ROWS_GO(E) rc = rows_launch(select_kernel<E>, dim3(G * ctas), dim3(kThreads), smem, s, ctas, a)
+#define ROWS_GO(E)                                                                                                                    \
+    if (rows_large_cluster(select_kernel<E>, (int)(PEARL_ROWS_MAX_BEAMS * PEARL_ROWS_MAX_BEST * 8 + ring)))                             \
+        rc = rows_launch(select_kernel<E>, dim3(G * ctas), dim3(kThreads), keys + ring, s, ctas, a)
     ROWS_WITH_TYPE(dtype, ROWS_GO);
 #undef ROWS_GO
     return rc;

@@ -47,6 +47,43 @@ inline uint32_t rows_granule(uint64_t a, uint64_t b = 0, uint64_t c = 0, uint64_
     return (uint32_t)(all & (~all + 1u));
 }
 
+// The current device (0 .. 63; -1 where it cannot be told) and its SMs.
+constexpr int kRowsMaxDevices = 64;
+inline int rows_device()
+{
+    int dev = 0;
+    return cudaGetDevice(&dev) == cudaSuccess && dev >= 0 && dev < kRowsMaxDevices ? dev : -1;
+}
+inline uint32_t rows_sm_count()
+{
+    static uint32_t known[kRowsMaxDevices];
+    const int dev = rows_device();
+    if (dev < 0) return 148;
+    if (known[dev] == 0) {
+        int n = 0;
+        known[dev] = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && n > 0 ? (uint32_t)n : 148u;
+    }
+    return known[dev];
+}
+// Lets a kernel be launched in clusters of more than 8 CTAs and, with smem, with that much shared memory (once per kernel and
+// device; one call site per kernel).
+template <typename... Params> inline bool rows_large_cluster(void (*kernel)(Params...), int smem = 0)
+{
+    struct Known { const void* kernel; bool done[kRowsMaxDevices]; };
+    static Known known[8];
+    const int dev = rows_device();
+    for (Known& k : known) {
+        if (k.kernel != nullptr && k.kernel != (const void*)kernel) continue;
+        if (dev >= 0 && k.kernel != nullptr && k.done[dev]) return true;
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return false;
+        if (smem && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return false;
+        k.kernel = (const void*)kernel;
+        if (dev >= 0) k.done[dev] = true;
+        return true;
+    }
+    return false;
+}
+
 // Launches a kernel as a programmatic dependent of the one before it on the stream: its blocks may be set up while that one
 // still runs; each of them waits (rows_begin) before it reads or writes anything.
 template <typename... Params, typename... Args>

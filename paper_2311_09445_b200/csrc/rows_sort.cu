@@ -153,20 +153,6 @@ __global__ void __launch_bounds__(kMostThreads) sort_kernel(unsigned* status, ui
     }
 }
 
-// Enables what a launch of the largest size needs, once per device.
-template <bool kLong> bool prepare_large()
-{
-    static bool done[64];
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return false;
-    if (dev < 64 && done[dev]) return true;
-    const int most = (int)(PEARL_ROWS_MAX_EXPERTS * (kPitch + 2) + 32) * 4;
-    if (cudaFuncSetAttribute(sort_kernel<kLong>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess) return false;
-    if (cudaFuncSetAttribute(sort_kernel<kLong>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return false;
-    if (dev < 64) done[dev] = true;
-    return true;
-}
-
 }  // namespace
 
 int rows_launch_sort(unsigned* status, uint32_t slots, uint32_t E, const int32_t* ids, int32_t* offsets, int32_t* order,
@@ -180,9 +166,9 @@ int rows_launch_sort(unsigned* status, uint32_t slots, uint32_t E, const int32_t
     while (ctas < kMostCtas && ctas * warps * 2 < groups) ctas *= 2;
     const bool is_long = groups > ctas * warps * kHeld;
     const size_t smem = ((size_t)E * (kPitch + 2) + 32) * sizeof(uint32_t);
-    if (smem > 48 * 1024 || ctas > 8) {
-        if (!(is_long ? prepare_large<true>() : prepare_large<false>())) return -1;
-    }
-    return rows_launch(is_long ? sort_kernel<true> : sort_kernel<false>, dim3(ctas), dim3(warps * 32), smem, s, ctas, status, slots, E,
+    const auto kernel = is_long ? sort_kernel<true> : sort_kernel<false>;
+    const int most = (int)(PEARL_ROWS_MAX_EXPERTS * (kPitch + 2) + 32) * (int)sizeof(uint32_t);
+    if ((smem > 48 * 1024 || ctas > 8) && !rows_large_cluster(kernel, most)) return -1;
+    return rows_launch(kernel, dim3(ctas), dim3(warps * 32), smem, s, ctas, status, slots, E,
                        ids, offsets, order, place);
 }

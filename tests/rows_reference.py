@@ -102,14 +102,16 @@ def offers(logits, scores, done, end_token):
 
 def check_selection(got_score, got_beam, got_token, logits, scores, done, end_token, C):
     """One group's selection against the definition.  Sums of different beams that are nearer to each other than the
-    32-bit terms of the row sums allow (8 roundings of a term's 2^-24, see below) may stand in either order."""
+    32-bit terms of the row sums allow (see below) may stand in either order."""
     lists = offers(logits, scores, done, end_token)
     best = sorted(((-total, b, r, token) for b, l in enumerate(lists) for r, (total, token) in enumerate(l[:C])))[:C]
     n = len(best)
     assert (got_beam[n:] == -1).all() and (got_token[n:] == -1).all() and np.isneginf(got_score[n:]).all()
-    # a row's sum: an exponential within 2 units of its last place (4 half steps), the product before it (1 at
-    # most, weighted by the term), three additions in 32 bits: 8 half steps of 2^-24, and two rows are compared
-    near = 16 * 2.0 ** -24
+    # a row's sum, in half steps of 2^-24 relative to it: a term is an exponential within 2 units of its last place (4) of a
+    # product (1) of a difference (x e^-x of one: 0.4), four additions in 32 bits (4), and three factors that bring sums to a
+    # common reference, each an exponential of a product with a product (3 * 5 + 0.6 for the differences): 25; the whole
+    # numbers that warps add up are off by 2^-26 at most.  Two rows are compared.
+    near = 2 * (25 * 2.0 ** -24 + 2.0 ** -26)
     taken = [0] * len(lists)
     for i in range(n):
         b = int(got_beam[i])
