@@ -1,8 +1,12 @@
 // The router: the k best of E experts with their softmax weights, and its gradient.
 //
-// L lanes have a row, N consecutive logits each, in registers.  The k choices are k rounds of "largest that is left": a
-// maximum over the lane's logits, one over the lanes by exchanges, the first lane that has it takes its first such
-// logit out.  Lanes and logits are in order, so the lower expert wins among equal ones.
+// Up to 8 choices (route_kernel): L lanes have a row, N consecutive logits each.  A logit and its expert are one whole number that
+// orders like (larger logit, lower expert): for 16-bit logits 32 bits, so that a comparison and exchange is one minimum and one
+// maximum.  A lane sorts its logits KP at a time by a network (KP: k rounded up to a power of two), keeps the KP best of them by
+// bitonic merges, and merges with the other lanes' lists by exchanges.  No branch depends on the data.  What bounds it are those
+// minima and maxima: 65521 rows of 128 bfloat16 logits, k = 8, 49 us by rounds (below), see the table of the measured cases for
+// this way.
+// More choices (rounds_kernel): k rounds of "largest that is left" over the row's lanes.
 #include "rows_internal.cuh"
 
 namespace {
@@ -52,7 +56,7 @@ __device__ __forceinline__ bool load_logits(const E* row, uint32_t first, uint32
 }
 
 template <typename E, int L, int N>
-__global__ void __launch_bounds__(kThreads) route_kernel(unsigned* status, uint32_t T, uint32_t experts, uint32_t k, const E* __restrict__ logits,
+__global__ void __launch_bounds__(kThreads) rounds_kernel(unsigned* status, uint32_t T, uint32_t experts, uint32_t k, const E* __restrict__ logits,
                                                          uint64_t ld, uint32_t wide, uint32_t over_chosen, float* __restrict__ w,
                                                          int32_t* __restrict__ ids)
 {
@@ -119,67 +123,336 @@ __global__ void __launch_bounds__(kThreads) route_kernel(unsigned* status, uint3
     }
 }
 
-// The gradient: each lane builds its N gradients from the row's k (id, weight, dw).
-template <typename E, int L, int N>
-__global__ void __launch_bounds__(kThreads) route_grad_kernel(unsigned* status, uint32_t T, uint32_t experts, uint32_t k,
-                                                              const E* __restrict__ logits, uint64_t ld, uint32_t wide, uint32_t over_chosen,
-                                                              const float* __restrict__ w, const int32_t* __restrict__ ids,
-                                                              const float* __restrict__ dw, E* __restrict__ dlogits, uint64_t ld_d,
-                                                              uint32_t wide_d)
+// ---- up to 8 choices -------------------------------------------------------------------------------------------------
+// Keys.  16-bit logits: the logit's bits made rising in the upper half, 0xFFFF - expert in the lower; binary32: the same in 64 bits.
+// Below -infinity's key (NaN with the sign set, and places behind the last expert) there is nothing to choose.
+template <typename E> struct Key;
+template <> struct Key<float> {
+    typedef uint64_t type;
+    static constexpr uint32_t kNothing = 0x007FFFFFu;          // of -infinity
+    static __device__ __forceinline__ uint32_t canonical(uint32_t w) { return __float_as_uint(__fadd_rn(__uint_as_float(w), 0.0f)); }
+    static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b)
+    {
+        float m;
+        asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(__uint_as_float(a)), "f"(__uint_as_float(b)));
+        return __float_as_uint(m);
+    }
+    static __device__ __forceinline__ bool bad(uint32_t largest) { return !(__uint_as_float(largest) < kInf); }
+    static __device__ __forceinline__ void mend(uint32_t& w) { if (!(__uint_as_float(w) < kInf)) w = 0xFF800000u; }
+    template <int I> static __device__ __forceinline__ type of(const uint32_t* w)
+    {
+        const uint32_t b = w[I];
+        return ((uint64_t)(b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u)) << 32) | (0xFFFFu - I);
+    }
+    static __device__ __forceinline__ type none(int i) { return 0xFFFFu - i; }
+    static __device__ __forceinline__ uint32_t rising(type k) { return (uint32_t)(k >> 32); }
+    static __device__ __forceinline__ float logit(type k)
+    {
+        const uint32_t r = rising(k);
+        return __uint_as_float(r & 0x80000000u ? r ^ 0x80000000u : ~r);
+    }
+    static __device__ __forceinline__ float value(const uint32_t* w, int i) { return __uint_as_float(w[i]); }
+};
+template <typename E> struct Key16 {
+    typedef uint32_t type;
+    // both halves at once: a set sign flips the other bits, too
+    static __device__ __forceinline__ uint32_t rising2(uint32_t w) { return w ^ (((w >> 15) & 0x00010001u) * 0x7FFFu | 0x80008000u); }
+    template <int I> static __device__ __forceinline__ type of(const uint32_t* w)
+    {
+        const uint32_t r = rising2(w[I / 2]);
+        return (I % 2 ? r & 0xFFFF0000u : r << 16) | (0xFFFFu - I);
+    }
+    static __device__ __forceinline__ type none(int i) { return 0xFFFFu - i; }
+    static __device__ __forceinline__ uint32_t rising(type k) { return k >> 16; }
+    static __device__ __forceinline__ uint16_t bits(type k) { return (uint16_t)((k >> 16) ^ (k & 0x80000000u ? 0x8000u : 0xFFFFu)); }
+};
+template <> struct Key<__half> : Key16<__half> {
+    static constexpr uint32_t kNothing = 0x03FFu;
+    static __device__ __forceinline__ __half2 as(uint32_t w) { return *reinterpret_cast<const __half2*>(&w); }
+    static __device__ __forceinline__ uint32_t word(__half2 h) { return *reinterpret_cast<const uint32_t*>(&h); }
+    static __device__ __forceinline__ uint32_t canonical(uint32_t w) { return word(__hadd2_rn(as(w), as(0u))); }
+    static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return word(__hmax2_nan(as(a), as(b))); }
+    static __device__ __forceinline__ bool bad(uint32_t largest) { const float2 f = __half22float2(as(largest)); return !(f.x < kInf) || !(f.y < kInf); }
+    static __device__ __forceinline__ void mend(uint32_t& w)
+    {
+        const float2 f = __half22float2(as(w));
+        if (!(f.x < kInf)) w = (w & 0xFFFF0000u) | 0xFC00u;
+        if (!(f.y < kInf)) w = (w & 0x0000FFFFu) | 0xFC000000u;
+    }
+    static __device__ __forceinline__ float logit(type k) { return __half2float(__ushort_as_half(bits(k))); }
+    static __device__ __forceinline__ float value(const uint32_t* w, int i) { const float2 f = __half22float2(as(w[i / 2])); return i % 2 ? f.y : f.x; }
+};
+template <> struct Key<__nv_bfloat16> : Key16<__nv_bfloat16> {
+    static constexpr uint32_t kNothing = 0x007Fu;
+    static __device__ __forceinline__ __nv_bfloat162 as(uint32_t w) { return *reinterpret_cast<const __nv_bfloat162*>(&w); }
+    static __device__ __forceinline__ uint32_t word(__nv_bfloat162 h) { return *reinterpret_cast<const uint32_t*>(&h); }
+    static __device__ __forceinline__ uint32_t canonical(uint32_t w) { return word(__hadd2_rn(as(w), as(0u))); }
+    static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return word(__hmax2_nan(as(a), as(b))); }
+    static __device__ __forceinline__ float2 both(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)); }
+    static __device__ __forceinline__ bool bad(uint32_t largest) { const float2 f = both(largest); return !(f.x < kInf) || !(f.y < kInf); }
+    static __device__ __forceinline__ void mend(uint32_t& w)
+    {
+        const float2 f = both(w);
+        if (!(f.x < kInf)) w = (w & 0xFFFF0000u) | 0xFF80u;
+        if (!(f.y < kInf)) w = (w & 0x0000FFFFu) | 0xFF800000u;
+    }
+    static __device__ __forceinline__ float logit(type k) { return __uint_as_float((uint32_t)bits(k) << 16); }
+    static __device__ __forceinline__ float value(const uint32_t* w, int i) { const float2 f = both(w[i / 2]); return i % 2 ? f.y : f.x; }
+};
+
+template <typename K> __device__ __forceinline__ void order(K& a, K& b)       // the larger first
 {
+    const K hi = a > b ? a : b, lo = a > b ? b : a;
+    a = hi;
+    b = lo;
+}
+// Batcher's merge exchange sort (Knuth, 5.2.2), falling: 19 exchanges for 8 keys.
+template <int P, typename K> __device__ __forceinline__ void sort_falling(K (&a)[P])
+{
+#pragma unroll
+    for (int p = 1; p < P; p *= 2)
+#pragma unroll
+        for (int q = p; q >= 1; q /= 2)
+#pragma unroll
+            for (int j = q % p; j + q < P; j += 2 * q)
+#pragma unroll
+                for (int i = 0; i < q; ++i)
+                    if (i + j + q < P && (i + j) / (2 * p) == (i + j + q) / (2 * p)) order(a[i + j], a[i + j + q]);
+}
+// The P largest of two falling lists (b is handed over reversed), falling.
+template <int P, typename K> __device__ __forceinline__ void merge_falling(K (&a)[P], const K (&reversed)[P])
+{
+#pragma unroll
+    for (int i = 0; i < P; ++i) a[i] = a[i] > reversed[i] ? a[i] : reversed[i];
+#pragma unroll
+    for (int d = P / 2; d > 0; d /= 2)
+#pragma unroll
+        for (int i = 0; i < P; ++i)
+            if ((i & d) == 0) order(a[i], a[i + d]);
+}
+template <typename E, int FROM, int P, int I = 0> struct KeysOf {
+    static __device__ __forceinline__ void get(const uint32_t* w, typename Key<E>::type* out)
+    {
+        out[I] = Key<E>::template of<FROM + I>(w);
+        if constexpr (I + 1 < P) KeysOf<E, FROM, P, I + 1>::get(w, out);
+    }
+};
+// The P best of a lane's logits FROM .. N - 1, merged into `best`.
+template <typename E, int N, int P, int FROM = 0> struct Choose {
+    typedef typename Key<E>::type K;
+    static __device__ __forceinline__ void run(const uint32_t* w, uint32_t there, K (&best)[P])
+    {
+        K group[P];
+        KeysOf<E, FROM, P>::get(w, group);
+#pragma unroll
+        for (int i = 0; i < P; ++i)
+            if ((uint32_t)(FROM + i) >= there) group[i] = Key<E>::none(FROM + i);
+        sort_falling<P>(group);
+        if constexpr (FROM == 0) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) best[i] = group[i];
+        } else {
+            K reversed[P];
+#pragma unroll
+            for (int i = 0; i < P; ++i) reversed[i] = group[P - 1 - i];
+            merge_falling<P>(best, reversed);
+        }
+        if constexpr (FROM + P < N) Choose<E, N, P, FROM + P>::run(w, there, best);
+    }
+};
+
+__device__ __forceinline__ uint32_t from_lane(uint32_t k, int d, int width) { return __shfl_xor_sync(0xFFFFFFFFu, k, d, width); }
+__device__ __forceinline__ uint64_t from_lane(uint64_t k, int d, int width) { return __shfl_xor_sync(0xFFFFFFFFu, k, d, width); }
+
+template <typename E, int L, int N, int P>
+__global__ void __launch_bounds__(kThreads) route_kernel(unsigned* status, uint32_t T, uint32_t experts, uint32_t k, const E* __restrict__ logits,
+                                                         uint64_t ld, uint32_t wide, uint32_t over_chosen, float* __restrict__ w,
+                                                         int32_t* __restrict__ ids)
+{
+    typedef Key<E> Q;
+    typedef typename Q::type K;
+    constexpr int kWords = N * (int)sizeof(E) / 4, kBytes = N * (int)sizeof(E), kAccess = kBytes < 16 ? kBytes : 16;
+    static_assert(N >= P && N % P == 0 && kWords >= 1, "whole groups");
     rows_begin();
-    const uint32_t lane = threadIdx.x % L;
+    const uint32_t lane = threadIdx.x % L, first = lane * N;
     const uint64_t t = (uint64_t)blockIdx.x * (kThreads / L) + threadIdx.x / L;
-    const bool there = t < T;
-    float x[N], g[N];
+    const uint32_t there = t < T && first < experts ? (experts - first < (uint32_t)N ? experts - first : (uint32_t)N) : 0u;
+    const E* row = logits + (t < T ? t : 0) * ld + first;
+    uint32_t x[kWords];
+    if (wide && there == (uint32_t)N) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) g[i] = 0.0f;
-    float p_scale = 0.0f, shift = 0.0f;
+        for (int i = 0; i < kBytes / kAccess; ++i) {
+            RowsRaw<kAccess> raw;
+            rows_load_if<false>(true, raw, reinterpret_cast<const unsigned char*>(row) + i * kAccess);
+#pragma unroll
+            for (int j = 0; j < kAccess / 4; ++j) x[i * (kAccess / 4) + j] = raw.r[j];
+        }
+    } else if constexpr (sizeof(E) == 4) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = (uint32_t)i < there ? __float_as_uint(row[i]) : 0xFF800000u;
+    } else {
+        const uint16_t minus_inf = RowsElem<E>::bits(RowsElem<E>::down(-kInf));
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+            const uint32_t lo = (uint32_t)(2 * i) < there ? RowsElem<E>::bits(row[2 * i]) : minus_inf;
+            const uint32_t hi = (uint32_t)(2 * i + 1) < there ? RowsElem<E>::bits(row[2 * i + 1]) : minus_inf;
+            x[i] = lo | hi << 16;
+        }
+    }
+    uint32_t largest = x[0];
+#pragma unroll
+    for (int i = 1; i < kWords; ++i) largest = Q::larger(largest, x[i]);
+    if (Q::bad(largest)) {
+        atomicOr(status, PEARL_ST_BAD_SCORE);
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) Q::mend(x[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) x[i] = Q::canonical(x[i]);           // (-0 becomes 0)
+
+    K best[P];
+    Choose<E, N, P>::run(x, there, best);
+#pragma unroll
+    for (int i = 0; i < P; ++i) best[i] -= first;                         // the expert's number in the row
+#pragma unroll
+    for (int d = 1; d < L; d *= 2) {
+        K reversed[P];
+#pragma unroll
+        for (int i = 0; i < P; ++i) reversed[i] = from_lane(best[P - 1 - i], d, L);
+        merge_falling<P>(best, reversed);
+    }
+    const float shift = Q::rising(best[0]) <= Q::kNothing ? 0.0f : Q::logit(best[0]);
+    float e[P], sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        e[i] = (uint32_t)i < k && Q::rising(best[i]) > Q::kNothing ? __expf(__fsub_rn(Q::logit(best[i]), shift)) : 0.0f;
+        sum = __fadd_rn(sum, e[i]);
+    }
     if (!over_chosen) {
-        if (load_logits<E, N>(logits + (there ? t : 0) * ld, lane * N, experts, there, wide != 0, x)) atomicOr(status, PEARL_ST_BAD_SCORE);
-        float best = x[0];
+        sum = 0.0f;
 #pragma unroll
-        for (int i = 1; i < N; ++i) best = fmaxf(best, x[i]);
-        const float top = over_lanes_max<L>(best);
-        shift = top == -kInf ? 0.0f : top;
-        float sum = 0.0f;
-#pragma unroll
-        for (int i = 0; i < N; ++i) sum = __fadd_rn(sum, __expf(__fsub_rn(x[i], shift)));
+        for (int i = 0; i < N; ++i) sum = __fadd_rn(sum, __expf(__fsub_rn(Q::value(x, i), shift)));
         sum = over_lanes_sum<L>(sum);
+    }
+    if (t >= T) return;
+    const float scale = sum > 0.0f ? sum : 1.0f;
+    // the lanes share the row's choices
+    constexpr int kEach = P / L > 0 ? P / L : 1;
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+        if ((uint32_t)i < k && (int)lane == i / kEach) {
+            ids[t * k + i] = Q::rising(best[i]) > Q::kNothing ? (int32_t)(0xFFFFu - (uint32_t)(best[i] & 0xFFFFu)) : -1;
+            w[t * k + i] = __fdiv_rn(e[i], scale);
+        }
+}
+
+// ---- the gradient ----------------------------------------------------------------------------------------------------
+// A warp has R rows at a time.  First a lane has one of a row's choices (KL lanes a row, k rounded up to a power of two): the mean
+// is a sum over those lanes, and the choices' parts are laid out by expert in shared memory.  Then 32 / R lanes have a row's
+// experts, 16 bytes at a time, and write the gradient: bound by the bytes of dlogits.
+// B logits of a row from c on, by accesses of M (which a row's length is a multiple of): -infinity behind the last expert, and for NaN
+// and +infinity, of which it tells.
+template <typename E, int M, int B>
+__device__ __forceinline__ bool load_block(const E* x, uint32_t c, uint32_t experts, float (&v)[B])
+{
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < B; i += M) {
+        if (c + i < experts) {
+            const RowsVec<E, M> a = rows_load_vec<E, M>(x + c + i);
+#pragma unroll
+            for (int m = 0; m < M; ++m) v[i + m] = a.get(m);
+        } else {
+#pragma unroll
+            for (int m = 0; m < M; ++m) v[i + m] = -kInf;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < B; ++i)
+        if (!(v[i] < kInf)) { bad = true; v[i] = -kInf; }
+    return bad;
+}
+constexpr uint32_t kRowFloats = 1024;                // of shared memory per warp: R rows of the experts, rounded up to 4
+template <typename E, int M, bool kChosen>
+__global__ void __launch_bounds__(kThreads) route_grad_kernel(unsigned* status, uint32_t T, uint32_t experts, uint32_t k, uint32_t log_kl,
+                                                              uint32_t log_r, const E* __restrict__ logits, uint64_t ld,
+                                                              const float* __restrict__ w, const int32_t* __restrict__ ids,
+                                                              const float* __restrict__ dw, E* __restrict__ dlogits, uint64_t ld_d)
+{
+    constexpr int B = 16 / (int)sizeof(E);
+    __shared__ __align__(16) float shared[kThreads / 32][kRowFloats];
+    rows_begin();
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x / 32, pitch = (experts + 3u) & ~3u, rows = 1u << log_r;
+    float* g = shared[warp];
+    const uint64_t t0 = ((uint64_t)blockIdx.x * (kThreads / 32) + warp) << log_r;
+    for (uint32_t i = lane * 4; i < rows * pitch; i += 128) *reinterpret_cast<float4*>(g + i) = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+
+    const uint32_t r = lane >> log_kl, j = lane & ((1u << log_kl) - 1u);
+    const bool slot = r < rows && t0 + r < T && j < k;
+    const uint64_t at = (t0 + r) * k + j;
+    int32_t id = slot ? __ldg(ids + at) : -1;
+    const float weight = slot ? __ldg(w + at) : 0.0f, d = slot ? __ldg(dw + at) : 0.0f;
+    if ((uint32_t)id >= experts) {
+        if (id != -1) atomicOr(status, PEARL_ST_BAD_INDEX);
+        id = -1;
+    }
+    float mean = id >= 0 ? __fmul_rn(weight, d) : 0.0f;
+    for (uint32_t q = 1; q < 1u << log_kl; q *= 2) mean = __fadd_rn(mean, __shfl_xor_sync(0xFFFFFFFFu, mean, q));
+    const float add = kChosen ? __fmul_rn(weight, __fsub_rn(d, mean)) : d;
+    const uint32_t to = id >= 0 ? r * pitch + (uint32_t)id : 0x80000000u | lane;
+    const bool alone = __popc(__match_any_sync(0xFFFFFFFFu, to)) == 1;
+    __syncwarp();
+    if (__all_sync(0xFFFFFFFFu, alone)) {
+        if (id >= 0) g[to] = add;
+    } else {
+        for (uint32_t q = 0; q < 1u << log_kl; ++q) {                     // (an expert named twice in a row: its parts in order)
+            if (j == q && id >= 0) g[to] = __fadd_rn(g[to], add);
+            __syncwarp();
+        }
+    }
+    __syncwarp();
+
+    // (a lane's experts do not depend on M, the width of an access: neither does the order of the sum)
+    const uint32_t log_lr = 5u - log_r, row = lane >> log_lr, step = B << log_lr, from = (lane & ((1u << log_lr) - 1u)) * B;
+    const uint64_t t = t0 + row;
+    mean = __shfl_sync(0xFFFFFFFFu, mean, (int)(row << log_kl));
+    const bool there = t < T;
+    float top = -kInf, sum = 0.0f, shift = 0.0f, p_scale = 0.0f;
+    const E* x = logits + (there ? t : 0) * ld;
+    if (!kChosen) {
+        bool bad = false;
+        for (uint32_t c = from; c < experts && there; c += step) {
+            float v[B];
+            bad |= load_block<E, M, B>(x, c, experts, v);
+#pragma unroll
+            for (int i = 0; i < B; ++i) top = fmaxf(top, v[i]);
+        }
+        if (bad) atomicOr(status, PEARL_ST_BAD_SCORE);
+        for (uint32_t q = 1; q < 1u << log_lr; q *= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, q));
+        shift = top == -kInf ? 0.0f : top;
+        for (uint32_t c = from; c < experts && there; c += step) {
+            float v[B];
+            load_block<E, M, B>(x, c, experts, v);
+#pragma unroll
+            for (int i = 0; i < B; ++i) sum = __fadd_rn(sum, __expf(__fsub_rn(v[i], shift)));
+        }
+        for (uint32_t q = 1; q < 1u << log_lr; q *= 2) sum = __fadd_rn(sum, __shfl_xor_sync(0xFFFFFFFFu, sum, q));
         p_scale = sum > 0.0f ? __fdiv_rn(1.0f, sum) : 0.0f;
     }
-    if (!there) return;                     // (no exchange between lanes from here on)
-    float mean = 0.0f;
-    for (uint32_t j = 0; j < k; ++j)
-        if ((uint32_t)ids[t * k + j] < experts) mean = __fmaf_rn(w[t * k + j], dw[t * k + j], mean);
-    for (uint32_t j = 0; j < k; ++j) {
-        const int32_t e = ids[t * k + j];
-        if (e < -1 || e >= (int32_t)experts) {
-            if (lane == 0) atomicOr(status, PEARL_ST_BAD_INDEX);
-            continue;
+    if (!there) return;
+    const float* mine = g + row * pitch;
+    for (uint32_t c = from; c < experts; c += step) {
+        float v[B];
+        if (!kChosen) load_block<E, M, B>(x, c, experts, v);
+        RowsVec<E, M> out;
+#pragma unroll
+        for (int i = 0; i < B; ++i) {
+            if (c + i < experts) {
+                const float p = kChosen ? 0.0f : __fmul_rn(__expf(__fsub_rn(v[i], shift)), p_scale);
+                out.put(i % M, kChosen ? mine[c + i] : __fmul_rn(p, __fsub_rn(mine[c + i], mean)));
+                if (i % M == M - 1) rows_store_vec<E, M>(dlogits + t * ld_d + c + i - (M - 1), out);
+            }
         }
-        const float d = dw[t * k + j];
-        const float add = over_chosen ? __fmul_rn(w[t * k + j], __fsub_rn(d, mean)) : d;
-        const uint32_t at = (uint32_t)e - lane * N;
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (e >= 0 && at == (uint32_t)i) g[i] = __fadd_rn(g[i], add);
-    }
-    constexpr int M = Access<E, N>::elements;
-    RowsVec<E, M> out[N / M];
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const float v = over_chosen ? g[i] : __fmul_rn(__fmul_rn(__expf(__fsub_rn(x[i], shift)), p_scale), __fsub_rn(g[i], mean));
-        out[i / M].put(i % M, v);
-    }
-    E* row = dlogits + t * ld_d;
-    if (wide_d && lane * N + N <= experts) {
-#pragma unroll
-        for (int a = 0; a < N / M; ++a) rows_store_vec<E, M>(row + lane * N + a * M, out[a]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (lane * N + i < experts) row[lane * N + i] = RowsElem<E>::down(out[i / M].get(i % M));
     }
 }
 
@@ -210,14 +483,48 @@ int rows_launch_route(unsigned* status, uint32_t T, uint32_t E, uint32_t k, uint
 {
     if (T == 0) return 0;
     int rc = -1;
+    if (k <= 8) {
+        // P choices; a lane has P .. 32 logits.  Few rows: fewer logits a lane, so that a row's way is shorter.
+        const uint32_t bytes = rows_elem_bytes(dtype);
+#define ROWS_GO(L, N, P)                                                                                                      \
+    do {                                                                                                                      \
+        const uint32_t rows = kThreads / (L);                                                                                 \
+        const uint32_t access = (N) * bytes < 16 ? (N) * bytes : 16;                                                          \
+        const uint32_t wide = (uintptr_t)logits % access == 0 && ld * bytes % access == 0 ? 1u : 0u;                          \
+        rc = rows_launch(route_kernel<ROWS_T, L, N, P>, dim3((T + rows - 1) / rows), dim3(kThreads), 0, s, 0, status, T, E, k, \
+                         (const ROWS_T*)logits, ld, wide, over_chosen ? 1u : 0u, w, ids);                                     \
+    } while (0)
+#define ROWS_P(P)                                                                                                             \
+    do {                                                                                                                      \
+        if (E <= 8) ROWS_GO(1, 8, P);                                                                                         \
+        else if (E <= 16) ROWS_GO(2, 8, P);                                                                                   \
+        else if (E <= 32) ROWS_GO(2, 16, P);                                                                                  \
+        else if (E <= 64) ROWS_GO(4, 16, P);                                                                                  \
+        else if (E <= 128) ROWS_GO(4, 32, P);                                                                                 \
+        else if (E <= 256) ROWS_GO(8, 32, P);                                                                                 \
+        else if (E <= 512) ROWS_GO(16, 32, P);                                                                                \
+        else ROWS_GO(32, 32, P);                                                                                              \
+    } while (0)
+#define ROWS_TYPE(X)                                                                                                          \
+    do {                                                                                                                      \
+        typedef X ROWS_T;                                                                                                     \
+        if (k <= 2) ROWS_P(2); else if (k <= 4) ROWS_P(4); else ROWS_P(8);                                                    \
+    } while (0)
+        ROWS_WITH_TYPE(dtype, ROWS_TYPE);
+#undef ROWS_TYPE
+#undef ROWS_P
+#undef ROWS_GO
+        return rc;
+    }
 #define ROWS_GO(L, N)                                                                                                        \
     do {                                                                                                                     \
         const uint32_t rows = kThreads / (L);                                                                                \
-        rc = rows_launch(route_kernel<ROWS_T, L, N>, dim3((T + rows - 1) / rows), dim3(kThreads), 0, s, 0, status, T, E, k,  \
+        rc = rows_launch(rounds_kernel<ROWS_T, L, N>, dim3((T + rows - 1) / rows), dim3(kThreads), 0, s, 0, status, T, E, k, \
                          (const ROWS_T*)logits, ld, wide_rows<ROWS_T, N>(logits, ld) ? 1u : 0u, over_chosen ? 1u : 0u, w, ids); \
     } while (0)
 #define ROWS_TYPE(X) do { typedef X ROWS_T; ROWS_WITH_SPREAD(E, ROWS_GO); } while (0)
     ROWS_WITH_TYPE(dtype, ROWS_TYPE);
+#undef ROWS_TYPE
 #undef ROWS_GO
     return rc;
 }
@@ -227,15 +534,26 @@ int rows_launch_route_grad(unsigned* status, uint32_t T, uint32_t E, uint32_t k,
                            cudaStream_t s)
 {
     if (T == 0) return 0;
+    uint32_t log_kl = 0;
+    while (1u << log_kl < k) ++log_kl;
+    uint32_t log_r = 5 - log_kl;
+    while (log_r > 0 && ((E + 3) / 4 * 4) << log_r > kRowFloats) --log_r;
+    const uint32_t bytes = rows_elem_bytes(dtype), rows = (kThreads / 32) << log_r;
+    const uint32_t granule = rows_granule((uint64_t)E * bytes, (uintptr_t)dlogits, ld_d * bytes, over_chosen ? 0 : (uintptr_t)logits,
+                                          over_chosen ? 0 : ld * bytes);
     int rc = -1;
-#define ROWS_GO(L, N)                                                                                                        \
-    do {                                                                                                                     \
-        const uint32_t rows = kThreads / (L);                                                                                \
-        rc = rows_launch(route_grad_kernel<ROWS_T, L, N>, dim3((T + rows - 1) / rows), dim3(kThreads), 0, s, 0, status, T, E, k, \
-                         (const ROWS_T*)logits, ld, wide_rows<ROWS_T, N>(logits, ld) ? 1u : 0u, over_chosen ? 1u : 0u, w, ids, dw, \
-                         (ROWS_T*)dlogits, ld_d, wide_rows<ROWS_T, N>(dlogits, ld_d) ? 1u : 0u);                             \
+#define ROWS_GO(M, CHOSEN)                                                                                                     \
+    rc = rows_launch(route_grad_kernel<ROWS_T, M, CHOSEN>, dim3((T + rows - 1) / rows), dim3(kThreads), 0, s, 0, status, T, E, k, log_kl, log_r, \
+                     (const ROWS_T*)logits, ld, w, ids, dw, (ROWS_T*)dlogits, ld_d)
+#define ROWS_TYPE(X)                                                                                                           \
+    do {                                                                                                                       \
+        typedef X ROWS_T;                                                                                                      \
+        constexpr int kWide = 16 / (int)sizeof(ROWS_T);                                                                        \
+        if (over_chosen) { if (granule >= 16) ROWS_GO(kWide, true); else if (granule >= 8) ROWS_GO(kWide / 2, true); else ROWS_GO(1, true); } \
+        else { if (granule >= 16) ROWS_GO(kWide, false); else if (granule >= 8) ROWS_GO(kWide / 2, false); else ROWS_GO(1, false); }          \
     } while (0)
     ROWS_WITH_TYPE(dtype, ROWS_TYPE);
+#undef ROWS_TYPE
 #undef ROWS_GO
     return rc;
 }
