@@ -101,8 +101,7 @@ __global__ void __launch_bounds__(kThreads) combine_kernel(unsigned* status, uin
         }
     }
     RowsVec<E, N> out;
-#pragma unroll
-    for (int i = 0; i < N; ++i) out.put(i, sum[i]);
+    out.set(sum);
     rows_store_vec<E, N>(y + t * ld_y + (uint64_t)col * N, out);
 }
 
@@ -148,9 +147,11 @@ __global__ void __launch_bounds__(kThreads) combine_grad_kernel(unsigned* status
 #pragma unroll
                 for (int j = 0; j < KC; ++j) {
                     if (at[j] < 0) continue;
-                    RowsVec<E, N> o;
+                    float part[N];
 #pragma unroll
-                    for (int i = 0; i < N; ++i) o.put(i, __fmul_rn(wt[j], a.get(i)));
+                    for (int i = 0; i < N; ++i) part[i] = __fmul_rn(wt[j], a.get(i));
+                    RowsVec<E, N> o;
+                    o.set(part);
                     rows_store_vec<E, N>(dz + ((uint64_t)(uint32_t)at[j] * cols + col) * N, o);
                 }
             }

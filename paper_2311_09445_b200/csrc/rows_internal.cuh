@@ -120,12 +120,24 @@ template <> struct RowsElem<__half> {
     static __device__ __forceinline__ __half down(float x) { return __float2half_rn(x); }
     static __device__ __forceinline__ uint16_t bits(__half x) { return __half_as_ushort(x); }
     static __device__ __forceinline__ __half from_bits(uint16_t b) { return __ushort_as_half(b); }
+    static __device__ __forceinline__ float2 up2(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+    static __device__ __forceinline__ uint32_t down2(float lo, float hi)
+    {
+        const __half2 h = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
 };
 template <> struct RowsElem<__nv_bfloat16> {
     static __device__ __forceinline__ float up(__nv_bfloat16 x) { return __bfloat162float(x); }
     static __device__ __forceinline__ __nv_bfloat16 down(float x) { return __float2bfloat16_rn(x); }
     static __device__ __forceinline__ uint16_t bits(__nv_bfloat16 x) { return __bfloat16_as_ushort(x); }
     static __device__ __forceinline__ __nv_bfloat16 from_bits(uint16_t b) { return __ushort_as_bfloat16(b); }
+    static __device__ __forceinline__ float2 up2(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)); }
+    static __device__ __forceinline__ uint32_t down2(float lo, float hi)
+    {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
 };
 
 // A raw access of B bytes: what is loaded and stored at once.  sm_100 moves 32 bytes a thread: a copy of 131048 rows of 4 KB to
@@ -205,15 +217,19 @@ union RowsVec {
     {
         if constexpr (sizeof(T) == 4) return __uint_as_float(raw.r[i]);
         else if constexpr (N == 1) return RowsElem<T>::up(RowsElem<T>::from_bits(raw.r[0]));
-        else return RowsElem<T>::up(RowsElem<T>::from_bits((uint16_t)(raw.r[i / 2] >> (i % 2 * 16))));
+        else { const float2 f = RowsElem<T>::up2(raw.r[i / 2]); return i % 2 ? f.y : f.x; }
     }
-    // (the elements in order, from 0)
-    __device__ __forceinline__ void put(int i, float x)
+    __device__ __forceinline__ void set(const float* x)
     {
-        if constexpr (sizeof(T) == 4) raw.r[i] = __float_as_uint(x);
-        else if constexpr (N == 1) raw.r[0] = RowsElem<T>::bits(RowsElem<T>::down(x));
-        else if (i % 2 == 0) raw.r[i / 2] = RowsElem<T>::bits(RowsElem<T>::down(x));
-        else raw.r[i / 2] |= (uint32_t)RowsElem<T>::bits(RowsElem<T>::down(x)) << 16;
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) raw.r[i] = __float_as_uint(x[i]);
+        } else if constexpr (N == 1) {
+            raw.r[0] = RowsElem<T>::bits(RowsElem<T>::down(x[0]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) raw.r[i] = RowsElem<T>::down2(x[2 * i], x[2 * i + 1]);
+        }
     }
 };
 template <typename T, int N>

@@ -125,7 +125,7 @@ __global__ void __launch_bounds__(kThreads) rounds_kernel(unsigned* status, uint
 
 // ---- up to 8 choices -------------------------------------------------------------------------------------------------
 // Keys.  16-bit logits: the logit's bits made rising in the upper half, 0xFFFF - expert in the lower; binary32: the same in 64 bits.
-// Below -infinity's key (NaN with the sign set, and places behind the last expert) there is nothing to choose.
+// Up to -infinity's key (which places behind the last expert have, too) there is nothing to choose.
 template <typename E> struct Key;
 template <> struct Key<float> {
     typedef uint64_t type;
@@ -144,7 +144,6 @@ template <> struct Key<float> {
         const uint32_t b = w[I];
         return ((uint64_t)(b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u)) << 32) | (0xFFFFu - I);
     }
-    static __device__ __forceinline__ type none(int i) { return 0xFFFFu - i; }
     static __device__ __forceinline__ uint32_t rising(type k) { return (uint32_t)(k >> 32); }
     static __device__ __forceinline__ float logit(type k)
     {
@@ -155,14 +154,18 @@ template <> struct Key<float> {
 };
 template <typename E> struct Key16 {
     typedef uint32_t type;
-    // both halves at once: a set sign flips the other bits, too
-    static __device__ __forceinline__ uint32_t rising2(uint32_t w) { return w ^ (((w >> 15) & 0x00010001u) * 0x7FFFu | 0x80008000u); }
+    // both halves at once: a set sign flips the other bits, too (prmt spreads the two signs)
+    static __device__ __forceinline__ uint32_t rising2(uint32_t w)
+    {
+        uint32_t signs;
+        asm("prmt.b32 %0, %1, 0, 0xBB99;" : "=r"(signs) : "r"(w));
+        return w ^ (signs | 0x80008000u);
+    }
     template <int I> static __device__ __forceinline__ type of(const uint32_t* w)
     {
         const uint32_t r = rising2(w[I / 2]);
-        return (I % 2 ? r & 0xFFFF0000u : r << 16) | (0xFFFFu - I);
+        return I % 2 ? (r & 0xFFFF0000u) | (0xFFFFu - I) : r * 0x10000u + (0xFFFFu - I);
     }
-    static __device__ __forceinline__ type none(int i) { return 0xFFFFu - i; }
     static __device__ __forceinline__ uint32_t rising(type k) { return k >> 16; }
     static __device__ __forceinline__ uint16_t bits(type k) { return (uint16_t)((k >> 16) ^ (k & 0x80000000u ? 0x8000u : 0xFFFFu)); }
 };
@@ -240,13 +243,10 @@ template <typename E, int FROM, int P, int I = 0> struct KeysOf {
 // The P best of a lane's logits FROM .. N - 1, merged into `best`.
 template <typename E, int N, int P, int FROM = 0> struct Choose {
     typedef typename Key<E>::type K;
-    static __device__ __forceinline__ void run(const uint32_t* w, uint32_t there, K (&best)[P])
+    static __device__ __forceinline__ void run(const uint32_t* w, K (&best)[P])
     {
         K group[P];
         KeysOf<E, FROM, P>::get(w, group);
-#pragma unroll
-        for (int i = 0; i < P; ++i)
-            if ((uint32_t)(FROM + i) >= there) group[i] = Key<E>::none(FROM + i);
         sort_falling<P>(group);
         if constexpr (FROM == 0) {
 #pragma unroll
@@ -257,7 +257,7 @@ template <typename E, int N, int P, int FROM = 0> struct Choose {
             for (int i = 0; i < P; ++i) reversed[i] = group[P - 1 - i];
             merge_falling<P>(best, reversed);
         }
-        if constexpr (FROM + P < N) Choose<E, N, P, FROM + P>::run(w, there, best);
+        if constexpr (FROM + P < N) Choose<E, N, P, FROM + P>::run(w, best);
     }
 };
 
@@ -311,7 +311,7 @@ __global__ void __launch_bounds__(kThreads) route_kernel(unsigned* status, uint3
     for (int i = 0; i < kWords; ++i) x[i] = Q::canonical(x[i]);           // (-0 becomes 0)
 
     K best[P];
-    Choose<E, N, P>::run(x, there, best);
+    Choose<E, N, P>::run(x, best);
 #pragma unroll
     for (int i = 0; i < P; ++i) best[i] -= first;                         // the expert's number in the row
 #pragma unroll
@@ -322,28 +322,36 @@ __global__ void __launch_bounds__(kThreads) route_kernel(unsigned* status, uint3
         merge_falling<P>(best, reversed);
     }
     const float shift = Q::rising(best[0]) <= Q::kNothing ? 0.0f : Q::logit(best[0]);
-    float e[P], sum = 0.0f;
-#pragma unroll
-    for (int i = 0; i < P; ++i) {
-        e[i] = (uint32_t)i < k && Q::rising(best[i]) > Q::kNothing ? __expf(__fsub_rn(Q::logit(best[i]), shift)) : 0.0f;
-        sum = __fadd_rn(sum, e[i]);
-    }
-    if (!over_chosen) {
-        sum = 0.0f;
-#pragma unroll
-        for (int i = 0; i < N; ++i) sum = __fadd_rn(sum, __expf(__fsub_rn(Q::value(x, i), shift)));
-        sum = over_lanes_sum<L>(sum);
-    }
-    if (t >= T) return;
-    const float scale = sum > 0.0f ? sum : 1.0f;
-    // the lanes share the row's choices
+    // every lane has the row's choices; each hands out its share of them
     constexpr int kEach = P / L > 0 ? P / L : 1;
+    K mine[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) mine[i] = 0;
 #pragma unroll
     for (int i = 0; i < P; ++i)
-        if ((uint32_t)i < k && (int)lane == i / kEach) {
-            ids[t * k + i] = Q::rising(best[i]) > Q::kNothing ? (int32_t)(0xFFFFu - (uint32_t)(best[i] & 0xFFFFu)) : -1;
-            w[t * k + i] = __fdiv_rn(e[i], scale);
+        if ((int)lane == i / kEach) mine[i % kEach] = best[i];
+    float e[kEach], sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        if (lane * kEach + i >= k || Q::rising(mine[i]) <= Q::kNothing) mine[i] = 0;
+        e[i] = mine[i] ? __expf(__fsub_rn(Q::logit(mine[i]), shift)) : 0.0f;
+        if (over_chosen) sum = __fadd_rn(sum, e[i]);
+    }
+    if (!over_chosen) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum = __fadd_rn(sum, __expf(__fsub_rn(Q::value(x, i), shift)));
+    }
+    sum = over_lanes_sum<L>(sum);
+    if (t >= T) return;
+    const float scale = sum > 0.0f ? __fdiv_rn(1.0f, sum) : 0.0f;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const uint32_t j = lane * kEach + i;
+        if (j < k) {
+            ids[t * k + j] = mine[i] ? (int32_t)(0xFFFFu - (uint32_t)(mine[i] & 0xFFFFu)) : -1;
+            w[t * k + j] = __fmul_rn(e[i], scale);
         }
+    }
 }
 
 // ---- the gradient ----------------------------------------------------------------------------------------------------
@@ -372,7 +380,7 @@ __device__ __forceinline__ bool load_block(const E* x, uint32_t c, uint32_t expe
         if (!(v[i] < kInf)) { bad = true; v[i] = -kInf; }
     return bad;
 }
-constexpr uint32_t kRowFloats = 1024;                // of shared memory per warp: R rows of the experts, rounded up to 4
+constexpr uint32_t kRowFloats = 1024;                // of shared memory per warp at most: R rows of the experts, rounded up to 4
 template <typename E, int M, bool kChosen>
 __global__ void __launch_bounds__(kThreads) route_grad_kernel(unsigned* status, uint32_t T, uint32_t experts, uint32_t k, uint32_t log_kl,
                                                               uint32_t log_r, const E* __restrict__ logits, uint64_t ld,
@@ -380,79 +388,108 @@ __global__ void __launch_bounds__(kThreads) route_grad_kernel(unsigned* status, 
                                                               const float* __restrict__ dw, E* __restrict__ dlogits, uint64_t ld_d)
 {
     constexpr int B = 16 / (int)sizeof(E);
-    __shared__ __align__(16) float shared[kThreads / 32][kRowFloats];
-    rows_begin();
+    extern __shared__ __align__(16) float shared[];
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x / 32, pitch = (experts + 3u) & ~3u, rows = 1u << log_r;
-    float* g = shared[warp];
-    const uint64_t t0 = ((uint64_t)blockIdx.x * (kThreads / 32) + warp) << log_r;
+    float* g = shared + warp * rows * pitch;
     for (uint32_t i = lane * 4; i < rows * pitch; i += 128) *reinterpret_cast<float4*>(g + i) = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    rows_begin();
 
+    const uint32_t groups = (T + rows - 1) >> log_r, all_warps = gridDim.x * (kThreads / 32);
     const uint32_t r = lane >> log_kl, j = lane & ((1u << log_kl) - 1u);
-    const bool slot = r < rows && t0 + r < T && j < k;
-    const uint64_t at = (t0 + r) * k + j;
-    int32_t id = slot ? __ldg(ids + at) : -1;
-    const float weight = slot ? __ldg(w + at) : 0.0f, d = slot ? __ldg(dw + at) : 0.0f;
-    if ((uint32_t)id >= experts) {
-        if (id != -1) atomicOr(status, PEARL_ST_BAD_INDEX);
-        id = -1;
-    }
-    float mean = id >= 0 ? __fmul_rn(weight, d) : 0.0f;
-    for (uint32_t q = 1; q < 1u << log_kl; q *= 2) mean = __fadd_rn(mean, __shfl_xor_sync(0xFFFFFFFFu, mean, q));
-    const float add = kChosen ? __fmul_rn(weight, __fsub_rn(d, mean)) : d;
-    const uint32_t to = id >= 0 ? r * pitch + (uint32_t)id : 0x80000000u | lane;
-    const bool alone = __popc(__match_any_sync(0xFFFFFFFFu, to)) == 1;
-    __syncwarp();
-    if (__all_sync(0xFFFFFFFFu, alone)) {
-        if (id >= 0) g[to] = add;
-    } else {
-        for (uint32_t q = 0; q < 1u << log_kl; ++q) {                     // (an expert named twice in a row: its parts in order)
-            if (j == q && id >= 0) g[to] = __fadd_rn(g[to], add);
-            __syncwarp();
-        }
-    }
-    __syncwarp();
-
     // (a lane's experts do not depend on M, the width of an access: neither does the order of the sum)
     const uint32_t log_lr = 5u - log_r, row = lane >> log_lr, step = B << log_lr, from = (lane & ((1u << log_lr) - 1u)) * B;
-    const uint64_t t = t0 + row;
-    mean = __shfl_sync(0xFFFFFFFFu, mean, (int)(row << log_kl));
-    const bool there = t < T;
-    float top = -kInf, sum = 0.0f, shift = 0.0f, p_scale = 0.0f;
-    const E* x = logits + (there ? t : 0) * ld;
-    if (!kChosen) {
-        bool bad = false;
-        for (uint32_t c = from; c < experts && there; c += step) {
-            float v[B];
-            bad |= load_block<E, M, B>(x, c, experts, v);
-#pragma unroll
-            for (int i = 0; i < B; ++i) top = fmaxf(top, v[i]);
+    int32_t next_id = -1;
+    float next_weight = 0.0f, next_d = 0.0f;
+    const auto fetch = [&](uint32_t group) {
+        const uint64_t t = ((uint64_t)group << log_r) + r;
+        const bool slot = group < groups && r < rows && t < T && j < k;
+        const uint64_t at = t * k + j;
+        next_id = slot ? __ldg(ids + at) : -1;
+        next_weight = slot ? __ldg(w + at) : 0.0f;
+        next_d = slot ? __ldg(dw + at) : 0.0f;
+    };
+    uint32_t group = blockIdx.x * (kThreads / 32) + warp;
+    fetch(group);
+    for (; group < groups; group += all_warps) {
+        int32_t id = next_id;
+        const float weight = next_weight, d = next_d;
+        fetch(group + all_warps);                                         // (the next rows' choices are on their way meanwhile)
+        if ((uint32_t)id >= experts) {
+            if (id != -1) atomicOr(status, PEARL_ST_BAD_INDEX);
+            id = -1;
         }
-        if (bad) atomicOr(status, PEARL_ST_BAD_SCORE);
-        for (uint32_t q = 1; q < 1u << log_lr; q *= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, q));
-        shift = top == -kInf ? 0.0f : top;
-        for (uint32_t c = from; c < experts && there; c += step) {
-            float v[B];
-            load_block<E, M, B>(x, c, experts, v);
-#pragma unroll
-            for (int i = 0; i < B; ++i) sum = __fadd_rn(sum, __expf(__fsub_rn(v[i], shift)));
-        }
-        for (uint32_t q = 1; q < 1u << log_lr; q *= 2) sum = __fadd_rn(sum, __shfl_xor_sync(0xFFFFFFFFu, sum, q));
-        p_scale = sum > 0.0f ? __fdiv_rn(1.0f, sum) : 0.0f;
-    }
-    if (!there) return;
-    const float* mine = g + row * pitch;
-    for (uint32_t c = from; c < experts; c += step) {
-        float v[B];
-        if (!kChosen) load_block<E, M, B>(x, c, experts, v);
-        RowsVec<E, M> out;
-#pragma unroll
-        for (int i = 0; i < B; ++i) {
-            if (c + i < experts) {
-                const float p = kChosen ? 0.0f : __fmul_rn(__expf(__fsub_rn(v[i], shift)), p_scale);
-                out.put(i % M, kChosen ? mine[c + i] : __fmul_rn(p, __fsub_rn(mine[c + i], mean)));
-                if (i % M == M - 1) rows_store_vec<E, M>(dlogits + t * ld_d + c + i - (M - 1), out);
+        float mean = id >= 0 ? __fmul_rn(weight, d) : 0.0f;
+        for (uint32_t q = 1; q < 1u << log_kl; q *= 2) mean = __fadd_rn(mean, __shfl_xor_sync(0xFFFFFFFFu, mean, q));
+        const float add = kChosen ? __fmul_rn(weight, __fsub_rn(d, mean)) : d;
+        const uint32_t to = r * pitch + (uint32_t)id;
+        __syncwarp();
+        // each choice leaves its lane's number (as bits) at its expert and looks whether it is still there: a hand-made row may name one twice
+        if (id >= 0) g[to] = __uint_as_float(lane);
+        __syncwarp();
+        const bool alone = id < 0 || __float_as_uint(g[to]) == lane;
+        __syncwarp();
+        if (__all_sync(0xFFFFFFFFu, alone)) {
+            if (id >= 0) g[to] = add;
+        } else {
+            if (id >= 0) g[to] = 0.0f;
+            __syncwarp();
+            for (uint32_t q = 0; q < 1u << log_kl; ++q) {                 // (its parts in order)
+                if (j == q && id >= 0) g[to] = __fadd_rn(g[to], add);
+                __syncwarp();
             }
         }
+        __syncwarp();
+
+        const uint64_t t = ((uint64_t)group << log_r) + row;
+        mean = __shfl_sync(0xFFFFFFFFu, mean, (int)(row << log_kl));
+        const bool there = t < T;
+        float top = -kInf, sum = 0.0f, shift = 0.0f, p_scale = 0.0f;
+        const E* x = logits + (there ? t : 0) * ld;
+        if (!kChosen) {
+            bool bad = false;
+            for (uint32_t c = from; c < experts && there; c += step) {
+                float v[B];
+                bad |= load_block<E, M, B>(x, c, experts, v);
+#pragma unroll
+                for (int i = 0; i < B; ++i) top = fmaxf(top, v[i]);
+            }
+            if (bad) atomicOr(status, PEARL_ST_BAD_SCORE);
+            for (uint32_t q = 1; q < 1u << log_lr; q *= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, q));
+            shift = top == -kInf ? 0.0f : top;
+            for (uint32_t c = from; c < experts && there; c += step) {
+                float v[B];
+                load_block<E, M, B>(x, c, experts, v);
+#pragma unroll
+                for (int i = 0; i < B; ++i) sum = __fadd_rn(sum, __expf(__fsub_rn(v[i], shift)));
+            }
+            for (uint32_t q = 1; q < 1u << log_lr; q *= 2) sum = __fadd_rn(sum, __shfl_xor_sync(0xFFFFFFFFu, sum, q));
+            p_scale = sum > 0.0f ? __fdiv_rn(1.0f, sum) : 0.0f;
+        }
+        const float* mine = g + row * pitch;
+        for (uint32_t c = from; c < experts && there; c += step) {
+            float v[B];
+            if (!kChosen) load_block<E, M, B>(x, c, experts, v);
+            float part[B];
+#pragma unroll
+            for (int i = 0; i < B; i += 4) {
+                float4 four = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (c + i < experts) four = *reinterpret_cast<const float4*>(mine + c + i);
+                part[i] = four.x; part[i + 1] = four.y; part[i + 2] = four.z; part[i + 3] = four.w;
+            }
+            if (!kChosen) {
+#pragma unroll
+                for (int i = 0; i < B; ++i)
+                    part[i] = __fmul_rn(__fmul_rn(__expf(__fsub_rn(v[i], shift)), p_scale), __fsub_rn(part[i], mean));
+            }
+#pragma unroll
+            for (int i = 0; i < B; i += M) {
+                RowsVec<E, M> out;
+                out.set(part + i);
+                if (c + i < experts) rows_store_vec<E, M>(dlogits + t * ld_d + c + i, out);
+            }
+        }
+        __syncwarp();
+        if (id >= 0) g[to] = 0.0f;                                        // (all zeros again)
     }
 }
 
@@ -539,11 +576,14 @@ int rows_launch_route_grad(unsigned* status, uint32_t T, uint32_t E, uint32_t k,
     uint32_t log_r = 5 - log_kl;
     while (log_r > 0 && ((E + 3) / 4 * 4) << log_r > kRowFloats) --log_r;
     const uint32_t bytes = rows_elem_bytes(dtype), rows = (kThreads / 32) << log_r;
+    const size_t smem = (size_t)((E + 3) / 4 * 4) * rows * sizeof(float);                      // 32 KB at most
+    const uint32_t most = rows_sm_count() * 8, blocks = (T + rows - 1) / rows;
+    const dim3 grid(blocks < most ? blocks : most);
     const uint32_t granule = rows_granule((uint64_t)E * bytes, (uintptr_t)dlogits, ld_d * bytes, over_chosen ? 0 : (uintptr_t)logits,
                                           over_chosen ? 0 : ld * bytes);
     int rc = -1;
 #define ROWS_GO(M, CHOSEN)                                                                                                     \
-    rc = rows_launch(route_grad_kernel<ROWS_T, M, CHOSEN>, dim3((T + rows - 1) / rows), dim3(kThreads), 0, s, 0, status, T, E, k, log_kl, log_r, \
+    rc = rows_launch(route_grad_kernel<ROWS_T, M, CHOSEN>, grid, dim3(kThreads), smem, s, 0, status, T, E, k, log_kl, log_r, \
                      (const ROWS_T*)logits, ld, w, ids, dw, (ROWS_T*)dlogits, ld_d)
 #define ROWS_TYPE(X)                                                                                                           \
     do {                                                                                                                       \
