@@ -315,18 +315,20 @@ def _plain(s):
 _routers = {}
 
 
-def _router():
-    """The program's handle for the current stream (made once, kept)."""
-    stream = torch.cuda.current_stream()
-    key = (stream.device_index, stream.cuda_stream)
-    if key not in _routers:
-        from paper_2311_09445_b200 import RowRouter
-        _routers[key] = RowRouter(stream=stream)
-    return _routers[key]
+def _router(s):
+    """The program's handle: made once for a stream, and kept where the program keeps its tensors."""
+    if "router" not in s:
+        stream = torch.cuda.current_stream()
+        key = (stream.device_index, stream.cuda_stream)
+        if key not in _routers:
+            from paper_2311_09445_b200 import RowRouter
+            _routers[key] = RowRouter(stream=stream)
+        s["router"] = _routers[key]
+    return s["router"]
 
 
 def _own(s):
-    c, r = s["case"], _router()
+    c, r = s["case"], _router(s)
     if c["op"] == "route":
         r.route(s["logits"], s["w"], s["ids"], over_chosen=c["chosen"])
         if not c["grad"]:
