@@ -16,15 +16,17 @@ namespace {
 
 constexpr uint64_t kSlabBytes = 256;
 
+// Makes `dev` the current device for a call; the device that was current is so again afterwards.
 struct DeviceGuard {
     int prev;
-    bool ok;
-    explicit DeviceGuard(int dev) : prev(-1), ok(true)
+    bool ok, other;
+    explicit DeviceGuard(int dev) : prev(-1), ok(true), other(false)
     {
         if (cudaGetDevice(&prev) != cudaSuccess) { ok = false; return; }
-        if (prev != dev && cudaSetDevice(dev) != cudaSuccess) ok = false;
+        other = prev != dev;
+        if (other && cudaSetDevice(dev) != cudaSuccess) ok = false;
     }
-    ~DeviceGuard() { if (prev >= 0) cudaSetDevice(prev); }
+    ~DeviceGuard() { if (other) cudaSetDevice(prev); }
 };
 
 bool misaligned(const void* p, uint32_t to) { return ((uintptr_t)p & (to - 1)) != 0; }

@@ -19,16 +19,20 @@ constexpr uint32_t kMostThreads = 1024, kMostCtas = 16;
 constexpr uint32_t kPitch = 33;          // of an expert's counts, one per warp (the odd pitch keeps a warp's accesses apart)
 constexpr int kHeld = 8;                 // groups of 32 slots whose ranks a lane holds
 
-// Shared memory: count[E][kPitch], total[E] (this CTA's slots per expert), start[E], sums[32].
-// The lanes whose expert is this lane's (e < 0: none), by one vote a bit: 7 votes for 64 experts, where one match instruction of the
-// warp took some 60 cycles of a unit that the SM has once (131048 slots: 20 us in all, 9 with votes).
+// Shared memory: count[E][kPitch], total[E] (this CTA's slots per expert), start[E], sums[32], and unless kLong local[E] and staged[slots
+// of a CTA]: a CTA's slots are sorted there first, so that what goes to `order` is runs of an expert's slots and not single words
+// (a warp's store to 32 places takes the SM 32 cycles).
+// The lanes whose expert is this lane's (e < 0: none), by one vote a bit.
 __device__ __forceinline__ uint32_t lanes_alike(int32_t e, uint32_t bits)
 {
     uint32_t alike = __ballot_sync(0xFFFFFFFFu, e >= 0);
     if (e < 0) alike = ~alike;
-    for (uint32_t b = 0; b < bits; ++b) {
-        const uint32_t set = __ballot_sync(0xFFFFFFFFu, (e >> b & 1) != 0);
-        alike &= e >> b & 1 ? set : ~set;
+#pragma unroll
+    for (uint32_t b = 0; b < 10; ++b) {
+        if (b >= bits) break;
+        const bool one = (e & (1 << b)) != 0;
+        const uint32_t set = __ballot_sync(0xFFFFFFFFu, one);
+        alike &= one ? set : ~set;
     }
     return alike;
 }
@@ -64,12 +68,17 @@ __global__ void __launch_bounds__(kMostThreads) sort_kernel(unsigned* status, ui
             const uint32_t s = s0 + q * 32 + lane;
             e[q] = s < end ? __ldg(ids + s) : -1;
         }
+        uint32_t alike[kHeld];
+#pragma unroll
+        for (int q = 0; q < kHeld; ++q) {
+            bad |= (uint32_t)e[q] >= E && e[q] != -1;
+            if ((uint32_t)e[q] >= E) e[q] = -1;
+            alike[q] = s0 + q * 32 < end ? lanes_alike(e[q], bits) : 0u;
+        }
 #pragma unroll
         for (int q = 0; q < kHeld; ++q) {
             if (s0 + q * 32 >= end) break;
-            bad |= (uint32_t)e[q] >= E && e[q] != -1;
-            if ((uint32_t)e[q] >= E) e[q] = -1;
-            const uint32_t peers = lanes_alike(e[q], bits);
+            const uint32_t peers = alike[q];
             uint32_t* mine = count + (e[q] >= 0 ? (uint32_t)e[q] * kPitch + warp : 0u);
             rank[q] = __popc(peers & below);
             uint32_t before = 0;
@@ -109,11 +118,13 @@ __global__ void __launch_bounds__(kMostThreads) sort_kernel(unsigned* status, ui
         const uint32_t x = threadIdx.x * per + i;
         sum[i] = 0;
         if (i >= per || x >= E) continue;
-        uint32_t before = 0;
-        for (uint32_t q = 0; q < ctas; ++q) {
-            const uint32_t c = *cluster.map_shared_rank(total + x, q);
-            if (q < cta) before += c;
-            sum[i] += c;
+        uint32_t before = 0, theirs[kMostCtas];
+#pragma unroll
+        for (uint32_t q = 0; q < kMostCtas; ++q) theirs[q] = q < ctas ? *cluster.map_shared_rank(total + x, q) : 0u;
+#pragma unroll
+        for (uint32_t q = 0; q < kMostCtas; ++q) {
+            if (q < cta) before += theirs[q];
+            sum[i] += theirs[q];
         }
         start[x] = here + before;
         here += sum[i];
@@ -126,8 +137,7 @@ __global__ void __launch_bounds__(kMostThreads) sort_kernel(unsigned* status, ui
     }
     if (lane == 31) sums[warp] = scan;
     cluster.sync();                       // (nobody reads this CTA's memory from here on)
-    uint32_t base = scan - here;
-    for (uint32_t q = 0; q < warp; ++q) base += sums[q];
+    const uint32_t base = __reduce_add_sync(0xFFFFFFFFu, lane < warp ? sums[lane] : 0u) + scan - here;
     uint32_t run = base;
 #pragma unroll
     for (uint32_t i = 0; i < 8; ++i) {
@@ -142,24 +152,81 @@ __global__ void __launch_bounds__(kMostThreads) sort_kernel(unsigned* status, ui
     }
     __syncthreads();
 
-    for (uint32_t s0 = begin; s0 < end; s0 += 32 * kHeld) {
-        if (kLong) {
+    if (!kLong && ctas == 1) {
+        // (few slots: staging them costs more than it saves; 512 slots 4.9 us without, 5.6 with)
 #pragma unroll
-            for (int q = 0; q < kHeld; ++q) {
-                const uint32_t s = s0 + q * 32 + lane;
-                rank[q] = s < end ? (uint32_t)place[s] : 0xFFFFFFFFu;
-                e[q] = s < end ? __ldg(ids + s) : -1;
-                if ((uint32_t)e[q] >= E) e[q] = -1;
+        for (int q = 0; q < kHeld; ++q) {
+            const uint32_t s = begin + q * 32 + lane;
+            if (s >= end) continue;
+            const uint32_t at = e[q] >= 0 ? start[e[q]] + count[(uint32_t)e[q] * kPitch + warp] + rank[q] : 0u;
+            place[s] = e[q] >= 0 ? (int32_t)at : -1;
+            if (e[q] >= 0 && order != nullptr && ROWS_IN_BOUNDS(status, at < slots)) order[at] = (int32_t)s;
+        }
+        return;
+    }
+    if (!kLong) {
+        // where an expert's slots start among this CTA's: the exclusive sum of the CTA's totals
+        uint32_t* local = sums + 32;
+        uint32_t* staged = local + E;
+        uint32_t own = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) {
+            const uint32_t x = threadIdx.x * per + i;
+            if (i < per && x < E) own += total[x];
+        }
+        uint32_t upto = own;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const uint32_t o = __shfl_up_sync(0xFFFFFFFFu, upto, d);
+            if (lane >= (uint32_t)d) upto += o;
+        }
+        __syncthreads();                                                      // (`sums` has been read)
+        if (lane == 31) sums[warp] = upto;
+        __syncthreads();
+        upto += __reduce_add_sync(0xFFFFFFFFu, lane < warp ? sums[lane] : 0u);
+        uint32_t at = upto - own;
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) {
+            const uint32_t x = threadIdx.x * per + i;
+            if (i >= per || x >= E) continue;
+            local[x] = at;
+            at += total[x];
+        }
+        __syncthreads();
+        const uint64_t cta_first = (uint64_t)cta * warps * each * 32u;
+#pragma unroll
+        for (int q = 0; q < kHeld; ++q) {
+            const uint32_t s = begin + q * 32 + lane;
+            if (s >= end) continue;
+            if (e[q] < 0) {
+                place[s] = -1;
+                continue;
             }
+            const uint32_t within = count[(uint32_t)e[q] * kPitch + warp] + rank[q];
+            place[s] = (int32_t)(start[e[q]] + within);
+            staged[local[e[q]] + within] = (uint32_t)(s - cta_first) << 10 | (uint32_t)e[q];      // (at most 8192 slots, 1024 experts)
+        }
+        if (order == nullptr) return;
+        __syncthreads();
+        const uint32_t n = local[E - 1] + total[E - 1];
+        for (uint32_t i = threadIdx.x; i < n; i += blockDim.x) {
+            const uint32_t v = staged[i], x = v & 1023u, to = start[x] + i - local[x];
+            if (ROWS_IN_BOUNDS(status, to < slots)) order[to] = (int32_t)(cta_first + (v >> 10));
+        }
+        return;
+    }
+    for (uint32_t s0 = begin; s0 < end; s0 += 32 * kHeld) {
+#pragma unroll
+        for (int q = 0; q < kHeld; ++q) {
+            const uint32_t s = s0 + q * 32 + lane;
+            rank[q] = s < end ? (uint32_t)place[s] : 0xFFFFFFFFu;
+            e[q] = s < end ? __ldg(ids + s) : -1;
+            if ((uint32_t)e[q] >= E) e[q] = -1;
         }
 #pragma unroll
         for (int q = 0; q < kHeld; ++q) {
             const uint32_t s = s0 + q * 32 + lane;
-            if (s >= end) continue;
-            if (e[q] < 0) {
-                if (!kLong) place[s] = -1;
-                continue;
-            }
+            if (s >= end || e[q] < 0) continue;
             const uint32_t at = start[e[q]] + count[(uint32_t)e[q] * kPitch + warp] + rank[q];
             place[s] = (int32_t)at;
             if (order != nullptr && ROWS_IN_BOUNDS(status, at < slots)) order[at] = (int32_t)s;
@@ -179,9 +246,9 @@ int rows_launch_sort(unsigned* status, uint32_t slots, uint32_t E, const int32_t
     uint32_t ctas = 1;
     while (ctas < kMostCtas && ctas * warps * 2 < groups) ctas *= 2;
     const bool is_long = groups > ctas * warps * kHeld;
-    const size_t smem = ((size_t)E * (kPitch + 2) + 32) * sizeof(uint32_t);
+    const size_t smem = ((size_t)E * (kPitch + 2) + 32 + (is_long ? 0 : E + warps * kHeld * 32)) * sizeof(uint32_t);
     const auto kernel = is_long ? sort_kernel<true> : sort_kernel<false>;
-    const int most = (int)(PEARL_ROWS_MAX_EXPERTS * (kPitch + 2) + 32) * (int)sizeof(uint32_t);
+    const int most = (int)(PEARL_ROWS_MAX_EXPERTS * (kPitch + 3) + 32 + kMostThreads * kHeld) * (int)sizeof(uint32_t);      // 176 KB
     if ((smem > 48 * 1024 || ctas > 8) && !rows_large_cluster(kernel, most)) return -1;
     return rows_launch(kernel, dim3(ctas), dim3(warps * 32), smem, s, ctas, status, slots, E,
                        ids, offsets, order, place);

@@ -7,6 +7,7 @@ states.  Every step runs in the library's CUDA kernels; there is no CPU path.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 from typing import Optional
 
 import torch
@@ -57,6 +58,51 @@ def load_library():
     return _lib
 
 
+def _pieces(shape, stride):
+    """A state's axes (those from the fourth on) as (pieces, elements of a piece, distance of pieces)."""
+    width, i = 1, len(shape)
+    while i > 3 and (shape[i - 1] == 1 or stride[i - 1] == width):
+        i -= 1
+        width *= shape[i]
+    pieces, pitch = 1, width
+    while i > 3:
+        i -= 1
+        if shape[i] == 1:
+            continue
+        if pieces == 1:
+            pitch = stride[i]
+        elif stride[i] != pitch * pieces:
+            raise ValueError("a state must be equally distant pieces of contiguous elements")
+        pieces *= shape[i]
+    return pieces, width, pitch
+
+
+def _distances(shape, stride):
+    """The distance of a block from the next one, and of a state."""
+    blocks, G, W = shape[:3]
+    if G > 1 and W > 1 and stride[1] != W * stride[2]:
+        raise ValueError("states must lie equally far apart")
+    return stride[0] if blocks > 1 else 0, stride[2] if W > 1 else (stride[1] if G > 1 else 0)
+
+
+@functools.lru_cache(maxsize=256)
+def _move(shape, stride, stride_out, size):
+    """pearl_rows_beam_reorder's arguments that follow from shapes and strides alone (a growing cache's for each of its lengths)."""
+    pieces, width, pitch = _pieces(shape, stride)
+    pieces_out, width_out, pitch_out = _pieces(shape, stride_out)
+    if pieces != pieces_out:
+        # one of the two is more contiguous than the other: cut it into the other's pieces
+        if pieces == 1:
+            pieces, width, pitch = pieces_out, width_out, width_out
+        elif pieces_out == 1:
+            pitch_out = width
+        else:
+            raise ValueError("states and out must be cut into the same pieces")
+    src, dst = (_States(block * size, state * size, p * size) for (block, state), p in
+                ((_distances(shape, stride), pitch), (_distances(shape, stride_out), pitch_out)))
+    return pieces, width * size, C.byref(src), C.byref(dst)
+
+
 class RowRouter:
     """The row operators on one GPU: calls enqueue on `stream` (default: the current torch stream at construction).
 
@@ -86,19 +132,27 @@ class RowRouter:
             raise PearlError(rc, "pearl_rows_create")
         self._h = h
         self._lib = lib
+        self._ordinal = self.device.index
 
     # ---- argument checks -------------------------------------------------------------------------
+    # (a device is compared by its number, -1 for a tensor that is not on a GPU: half the time of comparing torch.device objects,
+    # and these checks are a good part of what a small call costs)
     def _dense(self, t: torch.Tensor, what: str, dtype, count: int) -> int:
-        if t.dtype is not dtype or not t.is_contiguous() or t.numel() != count or t.device != self.device:
+        if t.dtype is not dtype or t.numel() != count or t.get_device() != self._ordinal or not t.is_contiguous():
             raise ValueError("%s must be a contiguous %s tensor of %d elements on %s" % (what, dtype, count, self.device))
         return t.data_ptr()
 
     def _matrix(self, t: torch.Tensor, what: str):
         """(address, rows, row length, distance of the rows in elements) of a 2-D tensor."""
-        if t.dim() != 2 or t.device != self.device or (t.shape[1] > 1 and t.stride(1) != 1):
+        if t.dim() != 2 or t.get_device() != self._ordinal:
             raise ValueError("%s must be a 2-D tensor on %s with contiguous rows" % (what, self.device))
         rows, cols = t.shape
-        ld = t.stride(0) if rows > 1 else cols
+        if t.is_contiguous():
+            return t.data_ptr(), rows, cols, cols
+        ld, step = t.stride()
+        if cols > 1 and step != 1:
+            raise ValueError("%s must be a 2-D tensor on %s with contiguous rows" % (what, self.device))
+        ld = ld if rows > 1 else cols
         if ld < cols:
             raise ValueError("the rows of %s overlap" % what)
         return t.data_ptr(), rows, cols, ld
@@ -151,7 +205,8 @@ class RowRouter:
 
     def _sorted(self, t: torch.Tensor, what: str, width: int, like: torch.Tensor, name: str):
         """(address, rows) of a dense matrix of rows in sorted order."""
-        if t.dim() != 2 or t.shape[1] != width or t.dtype is not like.dtype or not t.is_contiguous() or t.device != self.device:
+        if (t.dim() != 2 or t.shape[1] != width or t.dtype is not like.dtype or not t.is_contiguous() or
+                t.get_device() != self._ordinal):
             raise ValueError("%s must be a contiguous [rows, %d] tensor on %s of the type of %s" % (what, width, self.device, name))
         return t.data_ptr(), t.shape[0]
 
@@ -205,7 +260,7 @@ class RowRouter:
     def beam_select(self, logits, scores, best_score, best_beam, best_token, done=None, end_token: int = 0) -> None:
         """logits [G, W, V], scores [G, W] -> the C best offers of each group: best_score, best_beam, best_token [G, C].
         done [G, W] (uint8 or bool): finished beams, which offer end_token at their score."""
-        if logits.dim() != 3 or logits.device != self.device or (logits.shape[2] > 1 and logits.stride(2) != 1):
+        if logits.dim() != 3 or logits.get_device() != self._ordinal or (logits.shape[2] > 1 and logits.stride(2) != 1):
             raise ValueError("logits must be a 3-D tensor on %s with contiguous rows" % self.device)
         G, W, V = logits.shape
         ld = logits.stride(1) if W > 1 else (logits.stride(0) if G > 1 else V)
@@ -225,58 +280,21 @@ class RowRouter:
         if rc != 0:
             raise PearlError(rc, "pearl_rows_beam_select")
 
-    @staticmethod
-    def _pieces(t: torch.Tensor, what: str):
-        """A state's axes (those from the fourth on) as (pieces, elements of a piece, distance of pieces)."""
-        shape, stride = t.shape[3:], t.stride()[3:]
-        width, i = 1, len(shape)
-        while i > 0 and (shape[i - 1] == 1 or stride[i - 1] == width):
-            i -= 1
-            width *= shape[i]
-        pieces, pitch = 1, width
-        while i > 0:
-            i -= 1
-            if shape[i] == 1:
-                continue
-            if pieces == 1:
-                pitch = stride[i]
-            elif stride[i] != pitch * pieces:
-                raise ValueError("a state of %s must be equally distant pieces of contiguous elements" % what)
-            pieces *= shape[i]
-        return pieces, width, pitch
-
     def beam_reorder(self, states, parent, out=None) -> None:
         """out[o, g, i] = states[o, g, parent[g, i]]; states [blocks, G, W, ...], out None (or the same view): in place.
         The axes behind W may be a part of a larger cache, such as [heads, :length, dim]."""
         out = states if out is None else out
-        for t, what in ((states, "states"), (out, "out")):
-            if t.dim() < 3 or t.device != self.device:
-                raise ValueError("%s must be [blocks, G, W, ...] on %s" % (what, self.device))
-        if out.shape != states.shape or out.dtype is not states.dtype:
+        shape = states.shape
+        if len(shape) < 3 or states.get_device() != self._ordinal or out.get_device() != self._ordinal:
+            raise ValueError("states and out must be [blocks, G, W, ...] on %s" % self.device)
+        if out.shape != shape or out.dtype is not states.dtype:
             raise ValueError("out must have the shape and type of states")
-        blocks, G, W = states.shape[:3]
         if states.numel() == 0:
             return
-        size = states.element_size()
-        layouts = []
-        for t, what in ((states, "states"), (out, "out")):
-            pieces, width, pitch = self._pieces(t, what)
-            if G > 1 and W > 1 and t.stride(1) != W * t.stride(2):
-                raise ValueError("the states of %s must lie equally far apart" % what)
-            per_state = t.stride(2) if W > 1 else (t.stride(1) if G > 1 else 0)
-            layouts.append((pieces, width, _States((t.stride(0) if blocks > 1 else 0) * size, per_state * size, pitch * size)))
-        (pieces, width, src), (pieces_out, width_out, dst) = layouts
-        if (pieces, width) != (pieces_out, width_out):
-            # one of the two is more contiguous than the other: cut it into the other's pieces
-            if pieces == 1:
-                pieces, width, src.piece_pitch = pieces_out, width_out, width_out * size
-            elif pieces_out == 1:
-                dst.piece_pitch = width * size
-            else:
-                raise ValueError("states and out must be cut into the same pieces")
-        rc = self._lib.pearl_rows_beam_reorder(self._h, blocks, G, W, pieces, width * size,
-                                               self._dense(parent, "parent", _I32, G * W), states.data_ptr(), C.byref(src),
-                                               out.data_ptr(), C.byref(dst))
+        pieces, piece_bytes, src, dst = _move(shape, states.stride(), out.stride(), states.element_size())
+        rc = self._lib.pearl_rows_beam_reorder(self._h, shape[0], shape[1], shape[2], pieces, piece_bytes,
+                                               self._dense(parent, "parent", _I32, shape[1] * shape[2]), states.data_ptr(), src,
+                                               out.data_ptr(), dst)
         if rc != 0:
             raise PearlError(rc, "pearl_rows_beam_reorder")
 
