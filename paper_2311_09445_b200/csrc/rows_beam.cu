@@ -410,17 +410,15 @@ __device__ __forceinline__ bool arrived(uint32_t barrier)
     return false;
 }
 
-// The entries of a falling list that precede `key`.
-__device__ __forceinline__ uint32_t preceding(const uint64_t* list, uint32_t n, uint64_t key, bool equal_precedes)
+// The entries of a falling list of n that are larger than `bar`; `top` is the largest power of two up to n.
+__device__ __forceinline__ uint32_t larger_than(const uint64_t* list, uint32_t n, uint32_t top, uint64_t bar)
 {
-    const uint64_t bar = key - (equal_precedes ? 1u : 0u);                // (keys are not 0)
-    uint32_t lo = 0, hi = n;
-    while (lo < hi) {
-        const uint32_t mid = (lo + hi) / 2;
-        if (list[mid] > bar) lo = mid + 1;
-        else hi = mid;
+    uint32_t at = 0;
+    for (uint32_t step = top; step > 0; step >>= 1) {
+        const uint32_t next = at + step;
+        if (next <= n && list[next - 1] > bar) at = next;
     }
-    return lo;
+    return at;
 }
 
 struct SelectArgs {
@@ -429,6 +427,7 @@ struct SelectArgs {
     uint32_t parts;             // runs a row is cut into
     uint32_t run;               // logits of a run (a multiple of 8)
     uint32_t units_per_cta;
+    uint32_t by_parts, by_C;    // 2^16 / parts and 2^20 / C, rounded up: (x * by_parts) >> 16 and (x * by_C) >> 20 divide what is divided here
     const void* logits;
     uint64_t ld;
     const float* scores;
@@ -477,7 +476,7 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const SelectArgs a)
     const E* all_end = all + ((uint64_t)a.G * a.W - 1) * a.ld + a.V;
     for (uint32_t q = 0; q < a.units_per_cta; ++q) {
         const uint32_t u = cta * a.units_per_cta + q;
-        const uint32_t b = u < units ? u / a.parts : 0u, part = u < units ? u - b * a.parts : 0u;
+        const uint32_t b = u < units ? (u * a.by_parts) >> 16 : 0u, part = u < units ? u - b * a.parts : 0u;
         const uint64_t first = (uint64_t)part * a.run;
         const bool any = u < units && first < a.V;
         const Run<E> r(all + ((uint64_t)g * a.W + b) * a.ld + (any ? first : 0), any ? (uint32_t)(a.V - first < a.run ? a.V - first : a.run) : 0u, all,
@@ -509,7 +508,10 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const SelectArgs a)
             // the logits do not matter; a finished beam has one offer, whose key only has to be valid
             Stream<false, E>::finish();
             const uint32_t n = done_of[b] && score_of[b] > -kInf && part == 0 ? 1u : 0u;
-            for (uint32_t i = tid; i < C * ctas; i += kThreads) send(mine + i % C * 8u, bar, i / C, i % C < n ? key_of(0.0f, 0u) : 0ull);
+            for (uint32_t i = tid; i < C * ctas; i += kThreads) {
+                const uint32_t c = (i * a.by_C) >> 20, at = i - c * C;
+                send(mine + at * 8u, bar, c, at < n ? key_of(0.0f, 0u) : 0ull);
+            }
             if (tid < ctas) send(sums_at + u * (uint32_t)sizeof(UnitSum), bar, tid, UnitSum{0.0, kLowest, n});
             continue;
         }
@@ -616,7 +618,10 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const SelectArgs a)
                     }
                 }
             __syncthreads();
-            for (uint32_t i = tid; i < C * ctas; i += kThreads) send(mine + i % C * 8u, bar, i / C, work[i % C]);
+            for (uint32_t i = tid; i < C * ctas; i += kThreads) {
+                const uint32_t c = (i * a.by_C) >> 20, at = i - c * C;
+                send(mine + at * 8u, bar, c, work[at]);
+            }
         }
         if (q + 1 < a.units_per_cta) __syncthreads();                      // (the next unit uses the same workspace)
     }
@@ -639,7 +644,7 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const SelectArgs a)
     __syncthreads();
     uint64_t* all_totals = work;
     for (uint32_t i = tid; i < units * C; i += kThreads) {
-        const uint32_t b = i / C / a.parts;
+        const uint32_t b = (((i * a.by_C) >> 20) * a.by_parts) >> 16;
         const uint64_t k = all_keys[i];
         const double score = (double)score_of[b];
         all_totals[i] = k == 0 ? 0ull : rising64(done_of[b] ? score : score + ((double)from_rising((uint32_t)(k >> 32)) - lse[b]));
@@ -649,9 +654,9 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const SelectArgs a)
     // the place of each offer of this CTA's units: 2^shift lanes share the lists that may hold offers before it
     uint32_t shift = 5;
     while (shift > 0 && C << shift > kThreads) --shift;
-    const uint32_t each = 1u << shift, sub = tid & (each - 1);
+    const uint32_t each = 1u << shift, sub = tid & (each - 1), top = 1u << (31 - __clz(C));
     for (uint32_t q = 0; q < a.units_per_cta; ++q) {
-        const uint32_t u = cta * a.units_per_cta + q, b = u / a.parts, rows_from = b * a.parts, rows_to = rows_from + a.parts;
+        const uint32_t u = cta * a.units_per_cta + q, b = (u * a.by_parts) >> 16, rows_from = b * a.parts, rows_to = rows_from + a.parts;
         if (u >= units) break;
         const uint64_t* mine = all_keys + u * C;
         for (uint32_t i0 = 0; i0 < C; i0 += kThreads >> shift) {
@@ -660,9 +665,10 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const SelectArgs a)
             uint32_t place = 0;
             if (key)
                 for (uint32_t o = sub; o < units; o += each) {
-                    if (o == u) place += i;
-                    else if (o >= rows_from && o < rows_to) place += preceding(all_keys + o * C, C, key, false);
-                    else place += preceding(all_totals + o * C, C, total, o < u);
+                    // (runs of the same row by their logits and tokens, which are all different; other rows by the sums, equal ones
+                    // of lower beams first)
+                    const bool same = o >= rows_from && o < rows_to;
+                    place += larger_than((same ? all_keys : all_totals) + o * C, C, top, same ? key : total - (o < u ? 1u : 0u));
                 }
             for (uint32_t d = 1; d < each; d *= 2) place += __shfl_xor_sync(0xFFFFFFFFu, place, d);
             if (key && sub == 0 && place < C) {
@@ -761,6 +767,8 @@ int rows_launch_beam_select(unsigned* status, uint32_t G, uint32_t W, uint32_t V
     if ((uint64_t)G * ctas > 0x7FFFFFFFull) return -1;
     a.status = status; a.G = G; a.W = W; a.V = V; a.C = C; a.logits = logits; a.ld = ld; a.scores = scores; a.done = done; a.end_token = end_token;
     a.best_score = best_score; a.best_beam = best_beam; a.best_token = best_token;
+    a.by_parts = (65536u + a.parts - 1) / a.parts;
+    a.by_C = ((1u << 20) + C - 1) / C;
     const size_t keys = ((size_t)units * C + 1) / 2 * 16, ring = kThreads * kSlots * 16;         // (the ring is the largest use of the workspace)
     int rc = -1;
 #define ROWS_GO(E)                                                                                                                    \
