@@ -3,8 +3,10 @@
 // One thread-block cluster has all the slots, each of its CTAs a run of them, each warp a run of its CTA's.  Counts per expert
 // and warp lie in shared memory; the CTAs read each other's sums through it and meet at the cluster's barrier, so nothing goes
 // through global memory and no CTA waits for one that may not be there.
-//   1. A warp takes its run 32 slots at a time: the slots of one expert among them are ranked by lane, the warp's count of that
-//      expert so far is added.  A slot's rank within its warp's run stays in a register (long runs: in the place array).
+//   1. A warp takes its run 32 slots at a time: every lane sets its bit in its expert's word, which then tells the lanes that share
+//      it; a slot's rank is the lanes before its own and the warp's count of that expert so far.  It stays in a register (long runs: in
+//      the place array).  (One vote a bit of the expert's number, or the warp's match instruction, find the same lanes, and keep the
+//      SM's one unit for either busy: 131048 slots of 64 experts took 18 and 20 us, as opposed to 14 this way.)
 //   2. The counts become sums over the warps before, and over the CTAs before; the experts' totals become offsets.
 //   3. place = offset of the expert + slots of the CTAs before + of the warps before + rank.
 #include <cooperative_groups.h>
@@ -16,27 +18,11 @@ namespace cg = cooperative_groups;
 namespace {
 
 constexpr uint32_t kMostThreads = 1024, kMostCtas = 16;
-constexpr uint32_t kPitch = 33;          // of an expert's counts, one per warp (the odd pitch keeps a warp's accesses apart)
 constexpr int kHeld = 8;                 // groups of 32 slots whose ranks a lane holds
 
-// Shared memory: count[E][kPitch], total[E] (this CTA's slots per expert), start[E], sums[32], and unless kLong local[E] and staged[slots
+// Shared memory: tally[E][warps + 1] (x: the lanes of the running 32 slots, y: the warp's count so far), total[E] (this CTA's slots per expert), start[E], sums[32], and unless kLong local[E] and staged[slots
 // of a CTA]: a CTA's slots are sorted there first, so that what goes to `order` is runs of an expert's slots and not single words
 // (a warp's store to 32 places takes the SM 32 cycles).
-// The lanes whose expert is this lane's (e < 0: none), by one vote a bit.
-__device__ __forceinline__ uint32_t lanes_alike(int32_t e, uint32_t bits)
-{
-    uint32_t alike = __ballot_sync(0xFFFFFFFFu, e >= 0);
-    if (e < 0) alike = ~alike;
-#pragma unroll
-    for (uint32_t b = 0; b < 10; ++b) {
-        if (b >= bits) break;
-        const bool one = (e & (1 << b)) != 0;
-        const uint32_t set = __ballot_sync(0xFFFFFFFFu, one);
-        alike &= one ? set : ~set;
-    }
-    return alike;
-}
-
 template <bool kLong>
 __global__ void __launch_bounds__(kMostThreads) sort_kernel(unsigned* status, uint32_t slots, uint32_t E, const int32_t* __restrict__ ids,
                                                             int32_t* __restrict__ offsets, int32_t* __restrict__ order, int32_t* place)
@@ -45,11 +31,12 @@ __global__ void __launch_bounds__(kMostThreads) sort_kernel(unsigned* status, ui
     cg::cluster_group cluster = cg::this_cluster();
     const uint32_t ctas = cluster.num_blocks(), cta = cluster.block_rank();
     const uint32_t warps = blockDim.x / 32, warp = threadIdx.x / 32, lane = threadIdx.x & 31u, below = (1u << lane) - 1u;
-    uint32_t* count = shared;
-    uint32_t* total = count + E * kPitch;
+    const uint32_t pitch = warps + 1;                                          // (odd: a warp's accesses to its counts of several experts are apart)
+    uint2* tally = reinterpret_cast<uint2*>(shared);
+    uint32_t* total = shared + 2 * E * pitch;
     uint32_t* start = total + E;
     uint32_t* sums = start + E;
-    for (uint32_t i = threadIdx.x; i < E * kPitch; i += blockDim.x) count[i] = 0;
+    for (uint32_t i = threadIdx.x; i < E * pitch; i += blockDim.x) tally[i] = make_uint2(0u, 0u);
     rows_begin();
     __syncthreads();
 
@@ -58,7 +45,6 @@ __global__ void __launch_bounds__(kMostThreads) sort_kernel(unsigned* status, ui
     const uint64_t first = (uint64_t)(cta * warps + warp) * each * 32u;
     const uint32_t begin = (uint32_t)(first < slots ? first : slots);
     const uint32_t end = (uint32_t)(first + (uint64_t)each * 32u < slots ? first + (uint64_t)each * 32u : slots);
-    const uint32_t bits = 32u - __clz(E - 1u);                                // of an expert's number (0 for one expert)
     int32_t e[kHeld];
     uint32_t rank[kHeld];
     bool bad = false;
@@ -68,24 +54,21 @@ __global__ void __launch_bounds__(kMostThreads) sort_kernel(unsigned* status, ui
             const uint32_t s = s0 + q * 32 + lane;
             e[q] = s < end ? __ldg(ids + s) : -1;
         }
-        uint32_t alike[kHeld];
-#pragma unroll
-        for (int q = 0; q < kHeld; ++q) {
-            bad |= (uint32_t)e[q] >= E && e[q] != -1;
-            if ((uint32_t)e[q] >= E) e[q] = -1;
-            alike[q] = s0 + q * 32 < end ? lanes_alike(e[q], bits) : 0u;
-        }
 #pragma unroll
         for (int q = 0; q < kHeld; ++q) {
             if (s0 + q * 32 >= end) break;
-            const uint32_t peers = alike[q];
-            uint32_t* mine = count + (e[q] >= 0 ? (uint32_t)e[q] * kPitch + warp : 0u);
-            rank[q] = __popc(peers & below);
-            uint32_t before = 0;
-            if (e[q] >= 0) before = *mine;
+            bad |= (uint32_t)e[q] >= E && e[q] != -1;
+            if ((uint32_t)e[q] >= E) e[q] = -1;
+            uint2* mine = tally + (e[q] >= 0 ? (uint32_t)e[q] * pitch + warp : 0u);
+            if (e[q] >= 0) atomicOr(&mine->x, 1u << lane);
             __syncwarp();
-            if (e[q] >= 0 && rank[q] == 0) *mine = before + __popc(peers);
+            uint2 t = make_uint2(0u, 0u);
+            if (e[q] >= 0) t = *mine;
+            rank[q] = __popc(t.x & below);
             __syncwarp();
+            if (e[q] >= 0 && rank[q] == 0) *mine = make_uint2(0u, t.y + __popc(t.x));
+            __syncwarp();
+            const uint32_t before = t.y;
             rank[q] += before;
             if (kLong) {
                 const uint32_t s = s0 + q * 32 + lane;
@@ -98,14 +81,14 @@ __global__ void __launch_bounds__(kMostThreads) sort_kernel(unsigned* status, ui
 
     // per expert: the warps' counts to sums of the warps before, the CTA's total
     for (uint32_t x = warp; x < E; x += warps) {
-        const uint32_t own = lane < warps ? count[x * kPitch + lane] : 0u;
+        const uint32_t own = lane < warps ? tally[x * pitch + lane].y : 0u;
         uint32_t run = own;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
             const uint32_t o = __shfl_up_sync(0xFFFFFFFFu, run, d);
             if (lane >= (uint32_t)d) run += o;
         }
-        if (lane < warps) count[x * kPitch + lane] = run - own;
+        if (lane < warps) tally[x * pitch + lane].y = run - own;
         if (lane == 31) total[x] = run;
     }
     cluster.sync();
@@ -158,7 +141,7 @@ __global__ void __launch_bounds__(kMostThreads) sort_kernel(unsigned* status, ui
         for (int q = 0; q < kHeld; ++q) {
             const uint32_t s = begin + q * 32 + lane;
             if (s >= end) continue;
-            const uint32_t at = e[q] >= 0 ? start[e[q]] + count[(uint32_t)e[q] * kPitch + warp] + rank[q] : 0u;
+            const uint32_t at = e[q] >= 0 ? start[e[q]] + tally[(uint32_t)e[q] * pitch + warp].y + rank[q] : 0u;
             place[s] = e[q] >= 0 ? (int32_t)at : -1;
             if (e[q] >= 0 && order != nullptr && ROWS_IN_BOUNDS(status, at < slots)) order[at] = (int32_t)s;
         }
@@ -202,7 +185,7 @@ __global__ void __launch_bounds__(kMostThreads) sort_kernel(unsigned* status, ui
                 place[s] = -1;
                 continue;
             }
-            const uint32_t within = count[(uint32_t)e[q] * kPitch + warp] + rank[q];
+            const uint32_t within = tally[(uint32_t)e[q] * pitch + warp].y + rank[q];
             place[s] = (int32_t)(start[e[q]] + within);
             staged[local[e[q]] + within] = (uint32_t)(s - cta_first) << 10 | (uint32_t)e[q];      // (at most 8192 slots, 1024 experts)
         }
@@ -227,7 +210,7 @@ __global__ void __launch_bounds__(kMostThreads) sort_kernel(unsigned* status, ui
         for (int q = 0; q < kHeld; ++q) {
             const uint32_t s = s0 + q * 32 + lane;
             if (s >= end || e[q] < 0) continue;
-            const uint32_t at = start[e[q]] + count[(uint32_t)e[q] * kPitch + warp] + rank[q];
+            const uint32_t at = start[e[q]] + tally[(uint32_t)e[q] * pitch + warp].y + rank[q];
             place[s] = (int32_t)at;
             if (order != nullptr && ROWS_IN_BOUNDS(status, at < slots)) order[at] = (int32_t)s;
         }
@@ -240,16 +223,15 @@ int rows_launch_sort(unsigned* status, uint32_t slots, uint32_t E, const int32_t
                      int32_t* place, cudaStream_t s)
 {
     // A warp has one group of 32 slots before another warp is added, a CTA's 32 warps two each before another CTA is.
-    const uint32_t groups = (slots + 31) / 32;
+    const uint32_t groups = (slots + 31) / 32, most_warps = E > 512 ? 16 : 32;              // (the tallies of 1024 experts and 16 warps are 139 KB)
     uint32_t warps = 4;
-    while (warps < 32 && warps < groups) warps *= 2;
+    while (warps < most_warps && warps < groups) warps *= 2;
     uint32_t ctas = 1;
     while (ctas < kMostCtas && ctas * warps * 2 < groups) ctas *= 2;
     const bool is_long = groups > ctas * warps * kHeld;
-    const size_t smem = ((size_t)E * (kPitch + 2) + 32 + (is_long ? 0 : E + warps * kHeld * 32)) * sizeof(uint32_t);
+    const size_t smem = ((size_t)E * (2 * (warps + 1) + 2) + 32 + (is_long ? 0 : E + warps * kHeld * 32)) * sizeof(uint32_t);
     const auto kernel = is_long ? sort_kernel<true> : sort_kernel<false>;
-    const int most = (int)(PEARL_ROWS_MAX_EXPERTS * (kPitch + 3) + 32 + kMostThreads * kHeld) * (int)sizeof(uint32_t);      // 176 KB
-    if ((smem > 48 * 1024 || ctas > 8) && !rows_large_cluster(kernel, most)) return -1;
+    if ((smem > 48 * 1024 || ctas > 8) && !rows_large_cluster(kernel, 208 * 1024)) return -1;
     return rows_launch(kernel, dim3(ctas), dim3(warps * 32), smem, s, ctas, status, slots, E,
                        ids, offsets, order, place);
 }
