@@ -38,6 +38,12 @@ __device__ __forceinline__ uint32_t rising(float x)
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float from_rising(uint32_t r) { return __uint_as_float(r & 0x80000000u ? r ^ 0x80000000u : ~r); }
+// The logit of a bound; -infinity for one below every finite logit's key.
+__device__ __forceinline__ float logit_of_bound(uint64_t key)
+{
+    const uint32_t r = (uint32_t)(key >> 32);
+    return r < 0x00800000u ? -kInf : from_rising(r);
+}
 __device__ __forceinline__ uint64_t key_of(float x, uint32_t token) { return ((uint64_t)rising(x) << 32) | (0xFFFFFFFFu - token); }
 __device__ __forceinline__ uint64_t rising64(double x)
 {
@@ -340,20 +346,19 @@ __device__ __noinline__ void collect(const Run<E> r, uint32_t access, uint64_t a
         rows_load_if<false>(r.readable(access + m * kThreads), w[m], r.words(access + m * kThreads));
         if (r.off) rows_load_if<false>(r.readable(access + m * kThreads), hi[m], r.words(access + m * kThreads) + 16);
     }
-    const bool every = at_least == 1u;
-    const float low = every ? 0.0f : from_rising((uint32_t)(at_least >> 32));
+    const float low = logit_of_bound(at_least);
     const uint32_t last = 0xFFFFFFFFu - (uint32_t)at_least;               // of equal logits those up to this token
     uint32_t reach = 0;                                                   // bit m * N + j: logit j of access m reaches the bound
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
         if (r.off) r.shift(w[m], hi[m]);
         if (!r.whole(access + m * kThreads)) r.mend(access + m * kThreads, w[m]);
-        if (!every && largest_of<E>(w[m]) < low) continue;
+        if (largest_of<E>(w[m]) < low) continue;
         const uint32_t token = first + (access + m * kThreads) * N, equals = token <= last ? last - token + 1u : 0u;
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             const float x = Word<E>::get(w[m].r, j);
-            if (x < kInf && x > -kInf && (every || x > low || (x == low && (uint32_t)j < equals))) reach |= 1u << (m * N + j);
+            if (x < kInf && (x > low || (x == low && low > -kInf && (uint32_t)j < equals))) reach |= 1u << (m * N + j);
         }
     }
     uint32_t to = reach ? atomicAdd(n_offers, (uint32_t)__popc(reach)) : 0u;
@@ -554,12 +559,12 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const SelectArgs a)
         // The logits that reach the bound.  Should they be more than there is room for, the bound is searched by halving (`low`: too
         // many reach it, `high`: fewer than C do; the keys are all different, so some key has a number between).
         uint64_t low = lowest, high = ~0ull, at_least = lowest;
-        for (;;) {
-            const float low_logit = from_rising((uint32_t)(at_least >> 32));              // (NaN for the lowest key)
-            if (s.best > -kInf && !(s.best < low_logit)) {          // (low_logit is NaN for the lowest key)
+        for (uint32_t tries = 0;; ++tries) {
+            const float low_logit = logit_of_bound(at_least);
+            if (s.best > -kInf && s.best >= low_logit) {
                 collect<E>(r, s.best_at, at_least, (uint32_t)first, work, &n_offers);
-                if (s.second > -kInf && !(s.second < low_logit)) collect<E>(r, s.second_at, at_least, (uint32_t)first, work, &n_offers);
-                if (s.third > -kInf && !(s.third < low_logit)) deep[atomicAdd(&n_deep, 1u)] = make_uint2(s.best_at, s.second_at);
+                if (s.second > -kInf && s.second >= low_logit) collect<E>(r, s.second_at, at_least, (uint32_t)first, work, &n_offers);
+                if (s.third > -kInf && s.third >= low_logit) deep[atomicAdd(&n_deep, 1u)] = make_uint2(s.best_at, s.second_at);
             }
             __syncthreads();
             const uint32_t a_thread = Stream<false, E>::pairs(r), all_deep = n_deep * a_thread;
@@ -572,6 +577,10 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const SelectArgs a)
             __syncthreads();
             const uint32_t n = n_offers;
             if (n <= kRoom && (n >= C || at_least == lowest)) break;
+            if (tries == 80) {                                             // (64 halvings are enough)
+                if (tid == 0) atomicOr(a.status, PEARL_ST_INTERNAL);
+                break;
+            }
             if (n > kRoom) low = at_least;
             else high = at_least;
             at_least = low + (high - low) / 2;
@@ -579,7 +588,7 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const SelectArgs a)
             if (tid == 0) { n_deep = 0; n_offers = 0; }
             __syncthreads();
         }
-        const uint32_t n = n_offers;
+        const uint32_t n = n_offers < kRoom ? n_offers : kRoom;
         if (warp == kWarps - 1) {
             // the unit's sum, relative to the largest reference, added in a fixed order
             const float mine_ref = lane < kWarps ? warp_ref[lane] : kLowest;

@@ -398,6 +398,27 @@ def test_beam_select_crowded(rows, kind):
             check_select(rows, logits, torch.zeros(1, 1), C)
 
 
+@pytest.mark.parametrize("kind", ["fp32", "bf16"])
+def test_beam_select_mostly_masked(rows, kind):
+    """Most of a vocabulary barred or masked with the type's lowest value, in blocks that leave some warps without a logit, and more
+    logits at the lowest value than are sorted at once."""
+    t, V = TYPES[kind], 60000
+    lowest = torch.finfo(t).min
+    for barred, some in ((30000, 3), (256, 5), (59000, 2), (8 * 32 * 2, 0), (1000, 7)):
+        logits = torch.full((1, 2, V), lowest, dtype=t)
+        logits[0, :, :barred] = -math.inf
+        for i in range(some):
+            logits[0, :, barred + 97 * i] = 0.25 * i - 1
+        logits[0, 1, 0::2] = -math.inf
+        for C in (1, 8, 64):
+            check_select(rows, logits, torch.tensor([[0.0, -0.5]]), C)
+    # a grammar that allows a run of tokens
+    logits = torch.full((1, 3, V), -math.inf, dtype=t)
+    logits[0, :, 20000:27000] = torch.randn(3, 7000, generator=gen(57)).to(t)
+    check_select(rows, logits, torch.tensor([[0.0, -0.5, -3.0]]), 12)
+    assert rows.sync() == 0
+
+
 @pytest.mark.parametrize("kind", ["fp32", "fp16", "bf16"])
 def test_beam_select_barred_beams_and_tokens(rows, kind):
     t = TYPES[kind]
@@ -509,10 +530,7 @@ def test_binding_refuses(rows):
     from paper_2311_09445_b200 import PearlError
     for call, code in ((lambda: rows.route(f, torch.zeros(4, 9, device="cuda"), torch.zeros(4, 9, dtype=torch.int32, device="cuda")), -7),
                        (lambda: rows.sort(i, 0, torch.zeros(1, dtype=torch.int32, device="cuda"), i, i), -7),
-                       (lambda: rows.beam_reorder(f.view(1, 2, 2, 8), i[:2].contiguous(), f.view(1, 2, 2, 8).flip(0).view(1, 2, 2, 8)[:, :, :, :]), None)):
-        if code is None:
-            call()
-            continue
+                       (lambda: rows.beam_reorder(p.view(1, 4, 2, 8)[:, 1:3], i[:2].contiguous(), p.view(1, 4, 2, 8)[:, 2:]), -7)):
         with pytest.raises(PearlError) as e:
             call()
         assert e.value.code == code
