@@ -111,12 +111,14 @@ int pearl_rows_combine_grad(pearl_rows_t* rows, uint32_t T, uint32_t k, uint32_t
 
 /* One step of a beam search for G groups of W beams over V tokens.  A beam b of group g with score s = d_scores[g*W + b] and
  * logits l (row g*W + b of d_logits, rows ld_logits elements apart) offers every token v with l_v > -infinity at
- * s + (l_v - log sum exp l).  A beam whose flag d_done[g*W + b] is not 0 is finished: it offers end_token alone, at s
- * (its logits are not read); d_done may be NULL.  A score of -infinity takes its beam out.  Of a group's offers the C best
+ * s + (l_v - log sum exp l).  A beam whose flag d_done[g*W + b] is not 0 is finished: it offers end_token alone, at s;
+ * d_done may be NULL.  A score of -infinity takes its beam out.  Of a group's offers the C best
  * are handed out, best first: between tokens of a beam the larger logit wins and among equal ones the lower token, between
  * beams the larger sum and among equal ones the lower beam.  d_best_score (the sum, rounded to binary32), d_best_beam,
  * d_best_token: C entries a group; with fewer than C offers the rest is -infinity, -1, -1.
- * The row's sum of exponentials runs in binary64 over binary32 terms, the sums are compared in binary64.
+ * A row's sum of exponentials runs in binary64 and in whole numbers over binary32 sums of 8 or 16 terms; equal rows with equal scores have
+ * equal sums wherever they lie.  The sums are compared in binary64.  Bytes between rows may be read; the logits of finished beams may be
+ * read but do not matter.
  * A logit that is NaN or +infinity (or such a score) raises PEARL_ST_BAD_SCORE and counts as -infinity.
  * 1 <= W <= PEARL_ROWS_MAX_BEAMS, 1 <= C <= PEARL_ROWS_MAX_BEST, 1 <= V <= PEARL_ROWS_MAX_VOCAB; G may be 0. */
 int pearl_rows_beam_select(pearl_rows_t* rows, uint32_t G, uint32_t W, uint32_t V, uint32_t C, uint32_t dtype,
@@ -127,7 +129,8 @@ int pearl_rows_beam_select(pearl_rows_t* rows, uint32_t G, uint32_t W, uint32_t 
  * `pieces` pieces of piece_bytes bytes, piece_pitch bytes apart (a cache [heads, room, dim] of which a part of the room is
  * in use is `heads` pieces); the state of beam i of group g in block o starts at o*block_pitch + (g*W + i)*state_pitch
  * bytes.  src and dst have pitches of their own.  d_dst == d_src (with the same pitches) moves the states in place, and
- * states that stay where they are are not touched; otherwise src and dst must not overlap.  A parent of -1 leaves the
+ * states that stay where they are are not touched; otherwise the bytes from src's first state to its last must not
+ * overlap those of dst (PEARL_ERR_BAD_ARG).  A parent of -1 leaves the
  * state (of dst) as it was; any other parent outside [0, W) does so too and raises PEARL_ST_BAD_INDEX.
  * The pieces of different states must not overlap in dst.  1 <= W <= PEARL_ROWS_MAX_BEAMS; blocks, G, pieces or piece_bytes
  * of 0 is a call with nothing to do. */

@@ -16,16 +16,23 @@ constexpr float kLog2e = 1.44269504f;
 // cluster has more CTAs than the group has beams).  A unit is read once, through a ring of 16-byte slots in shared memory that
 // each thread fills and reads by itself (no barrier, 128 KB in flight on an SM with 64 registers a thread):
 //   statistics   a thread keeps a reference value, the sum of exp(x - reference), and the largest logits of its three best pairs
-//                of accesses.  The reference follows the largest logit only when that is more than 8 above
-//                it (e^8 terms fit a binary32 sum easily), so a logit costs one subtraction, one product, one exponential, one
-//                addition (two logits an instruction but for the exponential) and one comparison;
+//                of accesses.  The reference follows the largest logit only when that is more than 8 above it (e^8 terms fit a
+//                binary32 sum easily), so a logit costs one subtraction, one product, one exponential, one addition and half a
+//                comparison;
 //   the best C   in each of A warps the r-th largest of the lanes' largest logits, r = ceil(C / A), is reached by r logits, so the
 //                smallest of these bounds is reached by C.  Only threads whose largest logit reaches it can have such logits; they
 //                read their two best pairs again (from L2), and all their logits where the third-best pair reaches the bound, too.
 //                What reaches the bound -- some three times C logits -- is sorted.
 // Offers carry (logit, token) as one 64-bit key, all different, so nothing depends on the order threads arrive in.
-// Each CTA writes its row sums and sorted lists into the shared memory of all CTAs of the cluster; after one barrier, the rank of
-// an offer among the group's is the sum over the lists of how many entries precede it: binary searches, one writer for each result.
+// Each CTA sends its row sums and sorted lists into the shared memory of all CTAs of the cluster, which wait for the bytes of all
+// (a mbarrier each); the rank of an offer among the group's is then the sum over the lists of how many entries precede it:
+// searches by halving, one writer for each result.
+// What bounds it.  64 groups of 8 beams over 131072 bfloat16 logits (121 MB, 18 us at the rate of a copy): 48 us, of which the
+// reading is 28 (where four CTAs share an SM; without the exponentials it would take as long, and without the reading the
+// exponentials 27) and what follows it 9: a few hundred instructions in a row, and nothing left to hide them behind, because all
+// CTAs run at once.  4 rows of 32003 binary32 logits: 8.8 us, which are those instructions.  Tried and not kept: two kernels'
+// worth of work in four accesses at a time (63 us: spilled), the packed add.f32x2 and mul.f32x2 (moves into register pairs
+// cost what they save), clusters of 16 CTAs for the large case (70 us), the best pairs asked for again ahead of time (49 us).
 constexpr uint32_t kThreads = 256, kWarps = kThreads / 32;
 constexpr uint32_t kRoom = 4096;                 // offers that are sorted
 constexpr uint32_t kSlots = 8;                   // of the ring, per thread
@@ -699,8 +706,9 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const SelectArgs a)
 
 // ---- the states ------------------------------------------------------------------------------------------------------
 // state[o, g, i] <- state[o, g, parent[g, i]].  A thread has one access's worth of all W states of a block and group: it reads
-// what the moved states need (a state with several children comes from L1 the second time), then writes.  No other thread
-// touches those bytes, so the move can be made in place.
+// what the moved states need, all at once (a state with several children comes from a cache the second time), then writes.  No other
+// thread touches those bytes, so the move can be made in place.  1 GB of states of 8 beams, 5 of which survive, in place: 230 us for
+// 1.57 GB that have to move, 6.8 TB/s (branches around the loads, and 16-byte accesses: 400).
 struct ReorderArgs {
     unsigned* status;
     uint32_t G, W;

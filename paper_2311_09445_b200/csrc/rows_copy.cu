@@ -41,7 +41,8 @@ __device__ __forceinline__ void load_places(unsigned* status, const int32_t* __r
 
 // ---- dispatch --------------------------------------------------------------------------------------------------------
 // xs[place[t, j]] = x[t].  A thread reads its access of row t once and writes it k times: (1 + k) rows of traffic for k
-// copies, bound by the stores.
+// copies, bound by HBM's writes: 131048 rows of 4 KB from 16381 in 96 us, 6.3 TB/s.  (Two or four rows a thread: 99 us; 16-byte accesses:
+// 101.)
 template <int B, int KC>
 __global__ void __launch_bounds__(kThreads) dispatch_kernel(unsigned* status, uint32_t T, uint32_t k, uint32_t cols, uint32_t across,
                                                             uint32_t down, const unsigned char* __restrict__ x, uint64_t ld_x,
@@ -66,7 +67,8 @@ __global__ void __launch_bounds__(kThreads) dispatch_kernel(unsigned* status, ui
 
 // ---- combine ---------------------------------------------------------------------------------------------------------
 // y[t] = sum_j w[t, j] z[place[t, j]], j ascending, in binary32.  A thread holds the sums of N elements; the k reads do not
-// depend on one another and are issued together.
+// depend on one another and are issued together (predicated loads: branches around them made it 124 us).  32768 rows of 2048
+// binary16 elements from 117965 answers: 100 us, 6.2 TB/s, bound by HBM.
 template <typename E, int N, int KC, bool kWeights>
 __global__ void __launch_bounds__(kThreads) combine_kernel(unsigned* status, uint32_t T, uint32_t k, uint32_t cols, uint32_t across,
                                                            uint32_t down, const E* __restrict__ z, uint32_t sorted_rows,
@@ -108,7 +110,8 @@ __global__ void __launch_bounds__(kThreads) combine_kernel(unsigned* status, uin
 // ---- the gradient of combine -----------------------------------------------------------------------------------------
 // dz[place[t, j]] = w[t, j] dy[t], dw[t, j] = <dy[t], z[place[t, j]]>.  A team of `team` threads (a power of two, 32 .. 256) has one
 // row t: each thread reads its accesses of dy once for KC slots at a time and keeps one partial sum a slot; the partial sums are
-// added in a fixed order (a tree over the lanes, then the warps in turn).
+// added in a fixed order (a tree over the lanes, then the warps in turn).  8192 rows of 4096 bfloat16 elements, k = 8: with the
+// gradient of dispatch 269 us for 1.75 GB, 6.5 TB/s, the rate of a copy.
 template <typename E, int N, int KC>
 __global__ void __launch_bounds__(kThreads) combine_grad_kernel(unsigned* status, uint32_t T, uint32_t k, uint32_t cols, uint32_t team,
                                                                 const E* __restrict__ dy, uint64_t ld_dy, const E* __restrict__ z,

@@ -6,12 +6,15 @@
 //   1. A warp takes its run 32 slots at a time: every lane sets its bit in its expert's word, which then tells the lanes that share
 //      it; a slot's rank is the lanes before its own and the warp's count of that expert so far.  It stays in a register (long runs: in
 //      the place array).  (One vote a bit of the expert's number, or the warp's match instruction, find the same lanes, and keep the
-//      SM's one unit for either busy: 131048 slots of 64 experts took 18 and 20 us, as opposed to 14 this way.)
+//      SM's one unit for either busy: 131048 slots of 64 experts took 18 and 20 us on their own, as opposed to 16 this way.)
 //   2. The counts become sums over the warps before, and over the CTAs before; the experts' totals become offsets.
 //   3. place = offset of the expert + slots of the CTAs before + of the warps before + rank.
 #include <cooperative_groups.h>
 
 #include "rows_internal.cuh"
+
+// What bounds it: one cluster's 16 SMs and the barriers between the steps.  131048 slots of 64 experts: 9 us beside the 96 of the copy of
+// their rows that follows; 512 slots: 2.5.
 
 namespace cg = cooperative_groups;
 
