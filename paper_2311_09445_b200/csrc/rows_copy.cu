@@ -108,7 +108,7 @@ __global__ void __launch_bounds__(kThreads) combine_kernel(unsigned* status, uin
 }
 
 // ---- the gradient of combine -----------------------------------------------------------------------------------------
-// dz[place[t, j]] = w[t, j] dy[t], dw[t, j] = <dy[t], z[place[t, j]]>.  A team of `team` threads (a power of two, 32 .. 256) has one
+// dz[place[t, j]] = w[t, j] dy[t], dw[t, j] = <dy[t], z[place[t, j]]>.  A team of `team` threads (a power of two, 4 .. 256) has one
 // row t: each thread reads its accesses of dy once for KC slots at a time and keeps one partial sum a slot; the partial sums are
 // added in a fixed order (a tree over the lanes, then the warps in turn).  8192 rows of 4096 bfloat16 elements, k = 8: with the
 // gradient of dispatch 269 us for 1.75 GB, 6.5 TB/s, the rate of a copy.
@@ -160,10 +160,9 @@ __global__ void __launch_bounds__(kThreads) combine_grad_kernel(unsigned* status
             }
         }
         if (dw == nullptr) continue;
+        for (uint32_t d = (team < 32 ? team : 32u) / 2; d > 0; d >>= 1)
 #pragma unroll
-        for (int j = 0; j < KC; ++j)
-#pragma unroll
-            for (int d = 16; d > 0; d >>= 1) dot[j] = __fadd_rn(dot[j], __shfl_xor_sync(0xFFFFFFFFu, dot[j], d));
+            for (int j = 0; j < KC; ++j) dot[j] = __fadd_rn(dot[j], __shfl_xor_sync(0xFFFFFFFFu, dot[j], d));
         if (team > 32) {
             const uint32_t warp = threadIdx.x / 32;
             __syncthreads();                          // the sums of the slots before these have been read
@@ -275,8 +274,9 @@ int rows_launch_combine_grad(unsigned* status, uint32_t T, uint32_t k, uint32_t 
 #define ROWS_GO(E, N, KC)                                                                                                  \
     do {                                                                                                                   \
         const uint32_t cols = D / (N);                                                                                     \
-        uint32_t team = 32;                                                                                                \
-        while (team < kThreads && team * 4 < cols) team *= 2;                                                              \
+        uint32_t team = 4;            /* a lane an access up to a warp, then up to four accesses a thread */               \
+        while (team < 32 && team < cols) team *= 2;                                                                        \
+        while (team >= 32 && team < kThreads && team * 4 < cols) team *= 2;                                                \
         const uint32_t each = kThreads / team;                                                                             \
         rc = rows_launch(combine_grad_kernel<E, N, KC>, dim3((T + each - 1) / each), dim3(kThreads), 0, s, 0, status, T, k, cols, team, \
                          (const E*)dy, ld_dy, (const E*)z, sorted_rows, place, w, (E*)dz, dw);                             \
