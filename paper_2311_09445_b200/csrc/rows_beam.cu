@@ -353,19 +353,22 @@ __device__ __noinline__ void collect(const Run<E> r, uint32_t access, uint64_t a
         rows_load_if<false>(r.readable(access + m * kThreads), w[m], r.words(access + m * kThreads));
         if (r.off) rows_load_if<false>(r.readable(access + m * kThreads), hi[m], r.words(access + m * kThreads) + 16);
     }
+    // (no branch a logit: a few cycles each instead of some hundred)
     const float low = logit_of_bound(at_least);
+    const bool finite = low > -kInf;
     const uint32_t last = 0xFFFFFFFFu - (uint32_t)at_least;               // of equal logits those up to this token
     uint32_t reach = 0;                                                   // bit m * N + j: logit j of access m reaches the bound
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
         if (r.off) r.shift(w[m], hi[m]);
         if (!r.whole(access + m * kThreads)) r.mend(access + m * kThreads, w[m]);
-        if (largest_of<E>(w[m]) < low) continue;
-        const uint32_t token = first + (access + m * kThreads) * N, equals = token <= last ? last - token + 1u : 0u;
+        const uint32_t token = first + (access + m * kThreads) * N;
+        const int equals = finite && token <= last ? (int)(last - token < (uint32_t)N ? last - token + 1u : (uint32_t)N) : 0;
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             const float x = Word<E>::get(w[m].r, j);
-            if (x < kInf && (x > low || (x == low && low > -kInf && (uint32_t)j < equals))) reach |= 1u << (m * N + j);
+            const bool over = x > low, even = (x == low) & (j < equals);
+            reach |= (over | even) & (x < kInf) ? 1u << (m * N + j) : 0u;
         }
     }
     uint32_t to = reach ? atomicAdd(n_offers, (uint32_t)__popc(reach)) : 0u;
