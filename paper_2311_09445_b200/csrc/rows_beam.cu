@@ -760,6 +760,58 @@ __global__ void __launch_bounds__(kMoveThreads) reorder_kernel(const ReorderArgs
     if (bad && col == 0) atomicOr(a.status, PEARL_ST_BAD_INDEX);
 }
 
+// The same where states start at odd bytes or odd 2-byte places (67 MB of states of 4 beams in pieces of 251 x 33 binary16 elements, in
+// place: 31 us, by 2 bytes 75).  A block has kAnyTile bytes of a piece of all W states of a block and group: its threads read
+// what the moved states need, each thread the 16-byte words of each destination that it will store, meet, and store.  No other
+// block stores to those bytes, so this move can be made in place, too.  (The first and last words of a tile hold bytes of the tiles
+// beside it, which may be stored to meanwhile: those bytes are shifted out or not stored.)
+constexpr uint32_t kAnyTile = (kMoveThreads - 1) * 16;
+template <int S, int M>
+__global__ void __launch_bounds__(kMoveThreads) reorder_any_kernel(const ReorderArgs a, uint64_t src_bytes)
+{
+    rows_begin();
+    // (cols, piece_cols: bytes; col_blocks: tiles of all pieces of a state)
+    const uint64_t og = blockIdx.x / a.col_blocks;
+    const uint32_t g = (uint32_t)(og % a.G), tiles = (uint32_t)((a.piece_cols + kAnyTile - 1) / kAnyTile);
+    const uint64_t o = og / a.G, of = blockIdx.x - og * a.col_blocks, piece = of / tiles;
+    const uint64_t begin = (of - piece * tiles) * kAnyTile;
+    const int bytes = (int)(a.piece_cols - begin < kAnyTile ? a.piece_cols - begin : kAnyTile);
+    const unsigned char* src = a.src + o * a.sp.block_pitch + (uint64_t)g * a.W * a.sp.state_pitch + piece * a.sp.piece_pitch + begin;
+    unsigned char* dst = a.dst + o * a.dp.block_pitch + (uint64_t)g * a.W * a.dp.state_pitch + piece * a.dp.piece_pitch + begin;
+    RowsAny<S, true> v[M];
+    int32_t from[M];
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < M; ++i) from[i] = (uint32_t)i < a.W ? __ldg(a.parent + (uint64_t)g * a.W + i) : -1;
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+        bad |= from[i] < -1 || from[i] >= (int32_t)a.W;
+        if ((uint32_t)from[i] >= a.W || (a.in_place && from[i] == i)) from[i] = -1;
+        const int first = (int)(threadIdx.x * 16) - (int)((uint32_t)(uintptr_t)(dst + (uint64_t)i * a.dp.state_pitch) & 15u);
+        v[i].fetch(from[i] >= 0 && first < bytes, src + (uint64_t)(uint32_t)from[i] * a.sp.state_pitch + first, a.src, a.src + src_bytes);
+    }
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+        const int first = (int)(threadIdx.x * 16) - (int)((uint32_t)(uintptr_t)(dst + (uint64_t)i * a.dp.state_pitch) & 15u);
+        if (from[i] >= 0 && first < bytes)
+            v[i].get(src + (uint64_t)(uint32_t)from[i] * a.sp.state_pitch + first, a.src, a.src + src_bytes);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+        unsigned char* to = dst + (uint64_t)i * a.dp.state_pitch;
+        const int first = (int)(threadIdx.x * 16) - (int)((uint32_t)(uintptr_t)to & 15u);
+        if (from[i] >= 0 && first < bytes) rows_store_part<S>(to + first, v[i].v, -first, bytes - first);
+    }
+    if (bad && of == 0 && threadIdx.x == 0) atomicOr(a.status, PEARL_ST_BAD_INDEX);
+}
+template <int S>
+int launch_reorder_any(const ReorderArgs& a, uint64_t src_bytes, dim3 grid, cudaStream_t s)
+{
+    if (a.W <= 4) return rows_launch(reorder_any_kernel<S, 4>, grid, dim3(kMoveThreads), 0, s, 0, a, src_bytes);
+    return rows_launch(reorder_any_kernel<S, 8>, grid, dim3(kMoveThreads), 0, s, 0, a, src_bytes);
+}
+
 template <int B>
 int launch_reorder(const ReorderArgs& a, dim3 grid, cudaStream_t s)
 {
@@ -814,6 +866,16 @@ int rows_launch_beam_reorder(unsigned* status, uint32_t blocks, uint32_t G, uint
     if (blocks > 1) all |= sp.block_pitch | dp.block_pitch;
     uint32_t g = rows_granule(all);
     if (g == 32 && W > 16) g = 16;          // (32 states of 32 bytes are more than a thread's registers)
+    if (g <= 2 && piece_bytes >= kRowsAnyBytes && W <= 8) {            // (more beams' words are more than a thread's registers)
+        const uint64_t src_bytes = (uint64_t)(blocks - 1) * sp.block_pitch + ((uint64_t)G * W - 1) * sp.state_pitch + (uint64_t)(pieces - 1) * sp.piece_pitch + piece_bytes;
+        a.piece_cols = piece_bytes;
+        a.cols = piece_bytes * pieces;
+        a.col_blocks = (piece_bytes + kAnyTile - 1) / kAnyTile * pieces;
+        const uint64_t groups = (uint64_t)blocks * G;
+        if (a.col_blocks > 0x7FFFFFFFull / groups) return -1;
+        const dim3 tiles((uint32_t)(a.col_blocks * groups));
+        return g == 2 ? launch_reorder_any<2>(a, src_bytes, tiles, s) : launch_reorder_any<1>(a, src_bytes, tiles, s);
+    }
     a.piece_cols = piece_bytes / g;
     a.cols = a.piece_cols * pieces;
     a.col_blocks = (a.cols + kMoveThreads - 1) / kMoveThreads;

@@ -65,6 +65,39 @@ __global__ void __launch_bounds__(kThreads) dispatch_kernel(unsigned* status, ui
     }
 }
 
+// The same where rows start at odd bytes or odd 2-byte places: a thread has a 16-byte word of each of the k destinations.
+template <int S, int KC>
+__global__ void __launch_bounds__(kThreads) dispatch_any_kernel(unsigned* status, uint32_t T, uint32_t k, uint32_t row_bytes, uint32_t cols, uint32_t across,
+                                                                uint32_t down, const unsigned char* __restrict__ x, uint64_t ld_x,
+                                                                const int32_t* __restrict__ place, uint32_t sorted_rows, unsigned char* xs)
+{
+    rows_begin();
+    const uint32_t in = threadIdx.x / across;
+    const uint32_t col = threadIdx.x - in * across + blockIdx.y * across;
+    const uint64_t t = (uint64_t)blockIdx.x * down + in;
+    if (in >= down || t >= T || col >= cols) return;
+    const unsigned char *row = x + t * ld_x, *end = x + (T - 1) * ld_x + row_bytes;
+    for (uint32_t j0 = 0; j0 < k; j0 += KC) {
+        int32_t at[KC];
+        load_places<KC>(status, place + t * k + j0, k - j0, sorted_rows, col == 0, at);
+        RowsAny<S> v[KC];
+        int shift[KC];
+#pragma unroll
+        for (int j = 0; j < KC; ++j) {
+            // the word's first byte is byte 16 col - shift of the row
+            shift[j] = at[j] < 0 ? 0 : (int)((uint32_t)(uintptr_t)(xs + (uint64_t)(uint32_t)at[j] * row_bytes) & 15u);
+            if (at[j] >= 0 && (int)(col * 16) - shift[j] >= (int)row_bytes) at[j] = -1;
+            v[j].fetch(at[j] >= 0, row + (int)(col * 16) - shift[j], x, end);
+        }
+#pragma unroll
+        for (int j = 0; j < KC; ++j) {
+            if (at[j] < 0) continue;
+            const int first = (int)(col * 16) - shift[j];
+            rows_store_part<S>(xs + (uint64_t)(uint32_t)at[j] * row_bytes + first, v[j].get(row + first, x, end), -first, (int)row_bytes - first);
+        }
+    }
+}
+
 // ---- combine ---------------------------------------------------------------------------------------------------------
 // y[t] = sum_j w[t, j] z[place[t, j]], j ascending, in binary32.  A thread holds the sums of N elements; the k reads do not
 // depend on one another and are issued together (predicated loads: branches around them made it 124 us).  32768 rows of 2048
@@ -105,6 +138,50 @@ __global__ void __launch_bounds__(kThreads) combine_kernel(unsigned* status, uin
     RowsVec<E, N> out;
     out.set(sum);
     rows_store_vec<E, N>(y + t * ld_y + (uint64_t)col * N, out);
+}
+
+// The same for 16-bit elements where rows start at odd places: a thread has a 16-byte word of y.
+template <typename E, int KC, bool kWeights>
+__global__ void __launch_bounds__(kThreads) combine_any_kernel(unsigned* status, uint32_t T, uint32_t k, uint32_t D, uint32_t cols, uint32_t across,
+                                                               uint32_t down, const E* __restrict__ z, uint32_t sorted_rows,
+                                                               const int32_t* __restrict__ place, const float* __restrict__ w,
+                                                               E* __restrict__ y, uint64_t ld_y)
+{
+    constexpr int S = (int)sizeof(E), N = 16 / S;
+    rows_begin();
+    const uint32_t in = threadIdx.x / across;
+    const uint32_t col = threadIdx.x - in * across + blockIdx.y * across;
+    const uint64_t t = (uint64_t)blockIdx.x * down + in;
+    if (in >= down || t >= T || col >= cols) return;
+    unsigned char* out = reinterpret_cast<unsigned char*>(y + t * ld_y);
+    const int first = (int)(col * 16) - (int)((uint32_t)(uintptr_t)out & 15u), row_bytes = (int)(D * S);
+    if (first >= row_bytes) return;
+    const unsigned char *from = reinterpret_cast<const unsigned char*>(z), *end = from + (uint64_t)sorted_rows * row_bytes;
+    float sum[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum[i] = 0.0f;
+    for (uint32_t j0 = 0; j0 < k; j0 += KC) {
+        int32_t at[KC];
+        float wt[KC];
+        RowsAny<S> any[KC];
+        load_places<KC>(status, place + t * k + j0, k - j0, sorted_rows, col == 0, at);
+#pragma unroll
+        for (int j = 0; j < KC; ++j) {
+            wt[j] = kWeights && j0 + j < k ? __ldg(w + t * k + j0 + j) : 1.0f;
+            any[j].fetch(at[j] >= 0, from + (uint64_t)(uint32_t)at[j] * row_bytes + first, from, end);
+        }
+#pragma unroll
+        for (int j = 0; j < KC; ++j) {
+            if (at[j] < 0) continue;
+            RowsVec<E, N> v;
+            v.raw = any[j].get(from + (uint64_t)(uint32_t)at[j] * row_bytes + first, from, end);
+#pragma unroll
+            for (int i = 0; i < N; ++i) sum[i] = kWeights ? __fmaf_rn(wt[j], v.get(i), sum[i]) : __fadd_rn(sum[i], v.get(i));
+        }
+    }
+    RowsVec<E, N> o;
+    o.set(sum);
+    rows_store_part<S>(out + first, o.raw, -first, row_bytes - first);
 }
 
 // ---- the gradient of combine -----------------------------------------------------------------------------------------
@@ -184,6 +261,15 @@ __global__ void __launch_bounds__(kThreads) combine_grad_kernel(unsigned* status
     }
 }
 
+// Threads that share a row of `cols` accesses: a lane an access up to a warp, then up to four accesses a thread.
+uint32_t team_of(uint32_t cols)
+{
+    uint32_t team = 4;
+    while (team < 32 && team < cols) team *= 2;
+    while (team >= 32 && team < kThreads && team * 4 < cols) team *= 2;
+    return team;
+}
+
 // Runs CALL(N) with the elements per access that `granule` allows for elements of S bytes.
 #define ROWS_WITH_VEC(S, granule, CALL)                                         \
     do {                                                                        \
@@ -207,10 +293,23 @@ int rows_launch_dispatch(unsigned* status, uint32_t T, uint32_t k, uint32_t row_
 {
     if (T == 0) return 0;
     const uint32_t g = rows_granule(row_bytes, ld_x, (uintptr_t)x, (uintptr_t)xs);
+    int rc = -1;
+    if (g <= 2 && row_bytes >= kRowsAnyBytes) {
+        const uint32_t words = (row_bytes + 30) / 16;                     // of a destination, wherever it starts
+        const Tiling t = tile(T, words);
+#define ROWS_ANY(S, KC)                                                                                                     \
+    rc = rows_launch(dispatch_any_kernel<S, KC>, t.grid, t.block, 0, s, 0, status, T, k, row_bytes, words, t.across, t.down,     \
+                     (const unsigned char*)x, ld_x, place, sorted_rows, (unsigned char*)xs)
+#define ROWS_K(KC)                                                                                                          \
+    do { if (g == 2) ROWS_ANY(2, KC); else ROWS_ANY(1, KC); } while (0)
+        if (k <= 2) ROWS_K(2); else ROWS_K(4);
+#undef ROWS_K
+#undef ROWS_ANY
+        return rc;
+    }
     const uint32_t cols = row_bytes / g;
     const Tiling t = tile(T, cols);
     if (t.grid.y > 65535u) return -1;
-    int rc = -1;
 #define ROWS_GO(B, KC)                                                                                                      \
     rc = rows_launch(dispatch_kernel<B, KC>, t.grid, t.block, 0, s, 0, status, T, k, cols, t.across, t.down, (const unsigned char*)x, ld_x, \
                      place, sorted_rows, (unsigned char*)xs)
@@ -236,6 +335,21 @@ int rows_launch_combine(unsigned* status, uint32_t T, uint32_t k, uint32_t D, ui
     const uint32_t S = rows_elem_bytes(dtype);
     const uint32_t g = rows_granule((uint64_t)D * S, ld_y * S, (uintptr_t)z, (uintptr_t)y);
     int rc = -1;
+    if (g == 2 && dtype != PEARL_F32 && D * S >= kRowsAnyBytes) {
+        const uint32_t words = (D * S + 30) / 16;
+        const Tiling t = tile(T, words);
+#define ROWS_ANY(E, KC)                                                                                                     \
+    do {                                                                                                                    \
+        if (w) rc = rows_launch(combine_any_kernel<E, KC, true>, t.grid, t.block, 0, s, 0, status, T, k, D, words, t.across, t.down, \
+                                (const E*)z, sorted_rows, place, w, (E*)y, ld_y);                                           \
+        else rc = rows_launch(combine_any_kernel<E, KC, false>, t.grid, t.block, 0, s, 0, status, T, k, D, words, t.across, t.down,  \
+                              (const E*)z, sorted_rows, place, w, (E*)y, ld_y);                                             \
+    } while (0)
+        if (dtype == PEARL_F16) { if (k <= 2) ROWS_ANY(__half, 2); else ROWS_ANY(__half, 4); }
+        else { if (k <= 2) ROWS_ANY(__nv_bfloat16, 2); else ROWS_ANY(__nv_bfloat16, 4); }
+#undef ROWS_ANY
+        return rc;
+    }
 #define ROWS_GO(E, N, KC)                                                                                                           \
     do {                                                                                                                            \
         const uint32_t cols = D / (N);                                                                                              \
@@ -274,10 +388,7 @@ int rows_launch_combine_grad(unsigned* status, uint32_t T, uint32_t k, uint32_t 
 #define ROWS_GO(E, N, KC)                                                                                                  \
     do {                                                                                                                   \
         const uint32_t cols = D / (N);                                                                                     \
-        uint32_t team = 4;            /* a lane an access up to a warp, then up to four accesses a thread */               \
-        while (team < 32 && team < cols) team *= 2;                                                                        \
-        while (team >= 32 && team < kThreads && team * 4 < cols) team *= 2;                                                \
-        const uint32_t each = kThreads / team;                                                                             \
+        const uint32_t team = team_of(cols), each = kThreads / team;                                                                             \
         rc = rows_launch(combine_grad_kernel<E, N, KC>, dim3((T + each - 1) / each), dim3(kThreads), 0, s, 0, status, T, k, cols, team, \
                          (const E*)dy, ld_dy, (const E*)z, sorted_rows, place, w, (E*)dz, dw);                             \
     } while (0)

@@ -202,6 +202,71 @@ __device__ __forceinline__ void rows_store(void* p, const RowsRaw<B>& v)
         *reinterpret_cast<uint8_t*>(p) = v.r[0];
 }
 
+// ---- rows that do not start on 16-byte boundaries ---------------------------------------------------------------------
+// Such rows are moved by whole 16-byte words of the destination: a word's bytes come from the two words of the source that hold
+// them, shifted together, and only the words at a row's ends are stored in parts.  S: 1 or 2, what every address is a multiple of (rows
+// on 4-byte boundaries move faster by accesses of that size: 8192 sums of 4 rows of 2047 binary16 elements 92 us by 2 bytes, 57 so;
+// of 2046 elements 51 by 4 bytes, 57 so).
+
+// The 16 bytes at p, in two steps, so that several such reads are in flight together.  Words that lie in part outside [lo, hi), the
+// array that p points into, are not read as such; bytes outside it are 0.  kKept: as for rows_load_if.
+template <int S, bool kKept = false>
+struct RowsAny {
+    RowsRaw<16> v, w;
+    __device__ __forceinline__ static bool whole(const unsigned char* p, const unsigned char* lo, const unsigned char* hi)
+    {
+        const uint32_t off = (uint32_t)(uintptr_t)p & 15u;
+        return (p - off >= lo) & (p - off + (off ? 32 : 16) <= hi);
+    }
+    __device__ __forceinline__ void fetch(bool there, const unsigned char* p, const unsigned char* lo, const unsigned char* hi)
+    {
+        const uint32_t off = (uint32_t)(uintptr_t)p & 15u;
+        const bool words = there & whole(p, lo, hi);
+        rows_load_if<kKept>(words, v, p - off);
+        rows_load_if<kKept>(words & (off != 0), w, p - off + 16);
+    }
+    __device__ __forceinline__ const RowsRaw<16>& get(const unsigned char* p, const unsigned char* lo, const unsigned char* hi)
+    {
+        const uint32_t off = (uint32_t)(uintptr_t)p & 15u;
+        if (off & 8u) { v.r[0] = v.r[2]; v.r[1] = v.r[3]; v.r[2] = w.r[0]; v.r[3] = w.r[1]; w.r[0] = w.r[2]; w.r[1] = w.r[3]; }
+        if (off & 4u) { v.r[0] = v.r[1]; v.r[1] = v.r[2]; v.r[2] = v.r[3]; v.r[3] = w.r[0]; w.r[0] = w.r[1]; }
+        const uint32_t bits = (off & 3u) * 8u;
+        v.r[0] = __funnelshift_r(v.r[0], v.r[1], bits);
+        v.r[1] = __funnelshift_r(v.r[1], v.r[2], bits);
+        v.r[2] = __funnelshift_r(v.r[2], v.r[3], bits);
+        v.r[3] = __funnelshift_r(v.r[3], w.r[0], bits);
+        if (!whole(p, lo, hi)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v.r[i] = 0u;
+#pragma unroll
+            for (int i = 0; i < 16; i += S) {
+                const unsigned char* at = p + i;
+                if (at < lo || at + S > hi) continue;
+                if constexpr (S == 2) v.r[i / 4] |= (uint32_t)*reinterpret_cast<const uint16_t*>(at) << (i % 4 * 8);
+                else v.r[i / 4] |= (uint32_t)*at << (i % 4 * 8);
+            }
+        }
+        return v;
+    }
+};
+// Bytes [from, to) of a word, to the 16-byte boundary p.
+template <int S>
+__device__ __forceinline__ void rows_store_part(unsigned char* p, const RowsRaw<16>& v, int from, int to)
+{
+    if (from <= 0 && to >= 16) {
+        rows_store(p, v);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; i += S) {
+        if (i < from || i >= to) continue;
+        if constexpr (S == 2) *reinterpret_cast<uint16_t*>(p + i) = (uint16_t)(v.r[i / 4] >> (i % 4 * 8));
+        else p[i] = (unsigned char)(v.r[i / 4] >> (i % 4 * 8));
+    }
+}
+// Rows of at least this many bytes are moved so: below, the words at the ends are most of a row.
+constexpr uint32_t kRowsAnyBytes = 128;
+
 // N consecutive elements, moved as one access.
 template <typename T, int N>
 union RowsVec {

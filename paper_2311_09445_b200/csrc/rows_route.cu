@@ -493,11 +493,10 @@ __global__ void __launch_bounds__(kThreads) route_grad_kernel(unsigned* status, 
     }
 }
 
-// Runs CALL(L, N): the lanes of a row and the logits of a lane for E experts (L * N >= E).
+// Runs CALL(L, N): the lanes of a row and the logits of a lane for E experts, 9 at least (L * N >= E).
 #define ROWS_WITH_SPREAD(E, CALL)                                               \
     do {                                                                        \
-        if ((E) <= 8) { CALL(4, 2); }                                           \
-        else if ((E) <= 16) { CALL(4, 4); }                                     \
+        if ((E) <= 16) { CALL(4, 4); }                                          \
         else if ((E) <= 32) { CALL(8, 4); }                                     \
         else if ((E) <= 64) { CALL(8, 8); }                                     \
         else if ((E) <= 128) { CALL(16, 8); }                                   \

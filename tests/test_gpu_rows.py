@@ -227,7 +227,7 @@ def places(T, k, dropped, seed):
 
 
 ROWS = [(1, 1, 1), (1, 8, 4096), (3, 2, 17), (64, 2, 17), (5, 3, 8), (10, 4, 1000), (33, 8, 264), (7, 9, 100), (40, 1, 513), (2, 17, 2056),
-        (257, 5, 33), (6, 2, 8200)]
+        (257, 5, 33), (6, 2, 8200), (5, 4, 2047), (3, 7, 4098), (130, 2, 65), (2, 1, 12289)]
 
 
 @pytest.mark.parametrize("T,k,D", ROWS)
@@ -459,7 +459,8 @@ def test_beam_select_reports_nan_and_infinity(rows):
 
 @pytest.mark.parametrize("W", [1, 2, 4, 5, 8, 16, 31, 32])
 @pytest.mark.parametrize("dtype,heads,length,room,dim", [(torch.float32, 2, 5, 7, 8), (torch.bfloat16, 3, 9, 9, 33), (torch.uint8, 1, 1, 3, 1),
-                                                         (torch.float16, 4, 16, 40, 64), (torch.uint8, 2, 3, 4, 5)])
+                                                         (torch.float16, 4, 16, 40, 64), (torch.uint8, 2, 3, 4, 5), (torch.float16, 2, 251, 311, 33),
+                                                         (torch.uint8, 3, 1700, 1701, 7), (torch.float32, 1, 100, 101, 3), (torch.int64, 1, 17, 19, 1)])
 def test_beam_reorder(rows, W, dtype, heads, length, room, dim):
     blocks, G = 3, 2
     g = gen(60, W, dim)
@@ -479,6 +480,28 @@ def test_beam_reorder(rows, W, dtype, heads, length, room, dim):
     rows.beam_reorder(there[:, :, :, :, :length], parent.cuda())
     assert torch.equal(second.cpu().view(torch.uint8), want_other.view(torch.uint8))
     assert torch.equal(there.cpu().view(torch.uint8), want.view(torch.uint8))
+    assert rows.sync() == 0
+
+
+def test_beam_reorder_at_odd_addresses(rows):
+    """States that start at every offset from a 16-byte boundary, longer than a block's tile, in place and across."""
+    for shift in range(16):
+        length = 9001 + shift
+        store = torch.randint(0, 256, (2 * 3 * length + shift,), generator=gen(63, shift), dtype=torch.uint8)
+        there = store.cuda()
+        states = there[shift:].view(1, 2, 3, length)
+        parent = torch.tensor([[1, 2, 0], [2, 2, -1]], dtype=torch.int32)
+        was = states.clone()
+        other = torch.full((2 * 3 * length + 5,), 9, dtype=torch.uint8, device="cuda")
+        out = other[5:].view(1, 2, 3, length)
+        rows.beam_reorder(states, parent.cuda(), out)
+        rows.beam_reorder(states, parent.cuda())
+        for g in range(2):
+            for i in range(3):
+                want = was[0, g, parent[g, i]] if parent[g, i] >= 0 else None
+                assert torch.equal(states[0, g, i], want if want is not None else was[0, g, i])
+                assert torch.equal(out[0, g, i], want) if want is not None else (out[0, g, i] == 9).all()
+        assert torch.equal(there[:shift].cpu(), store[:shift]) and (other[:5] == 9).all()
     assert rows.sync() == 0
 
 
