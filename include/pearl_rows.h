@@ -20,8 +20,9 @@
  *   - `dtype` names the element type of logits and rows; sums, softmax statistics, weights and scores are binary32 or
  *     wider, each result is rounded once.
  *   - Rows of a matrix may lie apart (the ld_* arguments, in elements, at least the row's length); the elements of
- *     a row are consecutive.  Pointers must be aligned to their element size, else PEARL_ERR_ALIGN.  Rows whose start and
- *     length are multiples of 16 bytes move fastest.
+ *     a row are consecutive.  The bytes between rows are never written; up to 16 of them beside a row may be read.
+ *     Pointers must be aligned to their element size, else PEARL_ERR_ALIGN.  Rows whose start and length are multiples of
+ *     16 bytes move fastest.
  *   - Results do not depend on timing: the same inputs give the same bits.
  *   - Conditions found on the device never trap; they set PEARL_ST_* bits that pearl_rows_sync() returns and clears.
  *   - One handle is used from one host thread at a time.

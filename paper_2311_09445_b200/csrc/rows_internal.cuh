@@ -5,6 +5,9 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+#include <mutex>
+
 #include "../../include/pearl_rows.h"
 
 // The checked build (-DPEARL_CHECKED): an index into an array that the kernel computed is compared with its extent before it
@@ -56,7 +59,7 @@ inline int rows_device()
 }
 inline uint32_t rows_sm_count()
 {
-    static uint32_t known[kRowsMaxDevices];
+    static std::atomic<uint32_t> known[kRowsMaxDevices];
     const int dev = rows_device();
     if (dev < 0) return 148;
     if (known[dev] == 0) {
@@ -71,6 +74,8 @@ template <typename... Params> inline bool rows_large_cluster(void (*kernel)(Para
 {
     struct Known { const void* kernel; bool done[kRowsMaxDevices]; };
     static Known known[8];
+    static std::mutex lock;                  // (handles of several host threads share the table)
+    const std::lock_guard<std::mutex> held(lock);
     const int dev = rows_device();
     for (Known& k : known) {
         if (k.kernel != nullptr && k.kernel != (const void*)kernel) continue;
@@ -153,8 +158,8 @@ template <> struct RowsRaw<1> {
 };
 
 // Loads *p if `there`, else leaves v as it is: a predicated load, so that several of them are in flight together.  kKept: the bytes
-// may be written by this kernel (a move in place), so they do not go through the read-only path; `volatile` keeps such loads in
-// front of the stores that follow them.
+// may be written by this kernel (a move in place), so they do not go through the read-only path.  `volatile` keeps the loads behind
+// rows_begin, and kKept ones in front of the stores that follow them.
 template <bool kKept, int B>
 __device__ __forceinline__ void rows_load_if(bool there, RowsRaw<B>& v, const void* p)
 {
@@ -164,16 +169,16 @@ __device__ __forceinline__ void rows_load_if(bool there, RowsRaw<B>& v, const vo
                          : "+r"(v.r[0]), "+r"(v.r[1]), "+r"(v.r[2]), "+r"(v.r[3]), "+r"(v.r[4]), "+r"(v.r[5]), "+r"(v.r[6]), "+r"(v.r[7])
                          : "l"(p), "r"((uint32_t)there) : "memory");
         else
-            asm("{ .reg .pred q; setp.ne.u32 q, %9, 0; @q ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8]; }"
-                : "+r"(v.r[0]), "+r"(v.r[1]), "+r"(v.r[2]), "+r"(v.r[3]), "+r"(v.r[4]), "+r"(v.r[5]), "+r"(v.r[6]), "+r"(v.r[7])
-                : "l"(p), "r"((uint32_t)there));
+            asm volatile("{ .reg .pred q; setp.ne.u32 q, %9, 0; @q ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8]; }"
+                         : "+r"(v.r[0]), "+r"(v.r[1]), "+r"(v.r[2]), "+r"(v.r[3]), "+r"(v.r[4]), "+r"(v.r[5]), "+r"(v.r[6]), "+r"(v.r[7])
+                         : "l"(p), "r"((uint32_t)there));
     } else if constexpr (B == 16) {
         if constexpr (kKept)
             asm volatile("{ .reg .pred q; setp.ne.u32 q, %5, 0; @q ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4]; }"
                          : "+r"(v.r[0]), "+r"(v.r[1]), "+r"(v.r[2]), "+r"(v.r[3]) : "l"(p), "r"((uint32_t)there) : "memory");
         else
-            asm("{ .reg .pred q; setp.ne.u32 q, %5, 0; @q ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4]; }"
-                : "+r"(v.r[0]), "+r"(v.r[1]), "+r"(v.r[2]), "+r"(v.r[3]) : "l"(p), "r"((uint32_t)there));
+            asm volatile("{ .reg .pred q; setp.ne.u32 q, %5, 0; @q ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4]; }"
+                         : "+r"(v.r[0]), "+r"(v.r[1]), "+r"(v.r[2]), "+r"(v.r[3]) : "l"(p), "r"((uint32_t)there));
     } else if constexpr (B == 8) {
         if (there) { const uint2 a = *reinterpret_cast<const uint2*>(p); v.r[0] = a.x; v.r[1] = a.y; }
     } else if constexpr (B == 4) {
