@@ -9,15 +9,15 @@ namespace {
 
 constexpr float kInf = __builtin_huge_valf();
 constexpr float kLowest = -3.402823466e+38f;
-constexpr float kLog2e = 1.44269504f;
+constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
 
 // ---- selection -------------------------------------------------------------------------------------------------------
 // One thread-block cluster has a group.  A unit of work is a run of one beam's logits (the whole row, or a part of it where the
 // cluster has more CTAs than the group has beams).  A unit is read once, through a ring of 16-byte slots in shared memory that
 // each thread fills and reads by itself (no barrier, 128 KB in flight on an SM with 64 registers a thread):
 //   statistics   a thread keeps a reference value, the sum of exp(x - reference), and the largest logits of its three best pairs
-//                of accesses.  The reference follows the largest logit only when that is more than 8 above it (e^8 terms fit a
-//                binary32 sum easily), so a logit costs one subtraction, one product, one exponential, one addition and half a
+//                of accesses.  The reference moves only when a pair's sum becomes large (a binary32 sum has room), so a logit costs
+//                one fused operation, one exponential, one addition -- the first and the last two logits at a time -- and half a
 //                comparison;
 //   the best C   in each of A warps the r-th largest of the lanes' largest logits, r = ceil(C / A), is reached by r logits, so the
 //                smallest of these bounds is reached by C.  Only threads whose largest logit reaches it can have such logits; they
@@ -27,12 +27,12 @@ constexpr float kLog2e = 1.44269504f;
 // Each CTA sends its row sums and sorted lists into the shared memory of all CTAs of the cluster, which wait for the bytes of all
 // (a mbarrier each); the rank of an offer among the group's is then the sum over the lists of how many entries precede it:
 // searches by halving, one writer for each result.
-// What bounds it.  64 groups of 8 beams over 131072 bfloat16 logits (121 MB, 18 us at the rate of a copy): 48 us, of which the
-// reading is 28 (where four CTAs share an SM; without the exponentials it would take as long, and without the reading the
-// exponentials 27) and what follows it 9: a few hundred instructions in a row, and nothing left to hide them behind, because all
-// CTAs run at once.  4 rows of 32003 binary32 logits: 8.8 us, which are those instructions.  Tried and not kept: two kernels'
-// worth of work in four accesses at a time (63 us: spilled), the packed add.f32x2 and mul.f32x2 (moves into register pairs
-// cost what they save), clusters of 16 CTAs for the large case (70 us), the best pairs asked for again ahead of time (49 us).
+// What bounds it.  64 groups of 8 beams over 131072 bfloat16 logits (121 MB, 18 us at the rate of a copy): 40 us.  Reading takes
+// some 26 where four CTAs share an SM, 0.84 for 16 logits of each of its threads: 114 instructions a warp, half of what the SM can issue
+// in that time, and 17 for the unit of the exponentials, two thirds of what that can.  The rest are some 1700 instructions a warp in a
+// row, and nothing left to hide them behind, because all CTAs run at once.  4 rows of 32003 binary32 logits: 8.7 us, which are those
+// instructions.  Tried and not kept: four accesses at a time (63 us: spilled), clusters of 16 CTAs for the large case (70 us against
+// 48 then), the best pairs asked for again ahead of time (49 us against 48).
 constexpr uint32_t kThreads = 256, kWarps = kThreads / 32;
 constexpr uint32_t kRoom = 4096;                 // offers that are sorted
 constexpr uint32_t kSlots = 8;                   // of the ring, per thread
@@ -171,7 +171,7 @@ struct Run {
         return reinterpret_cast<const unsigned char*>(run) + (uint64_t)v * 16u - off;
     }
     // The access's logits in order, in lo, from the two words that hold it.
-    __device__ __forceinline__ void shift(RowsRaw<16>& lo, RowsRaw<16>& hi) const
+    static __device__ __forceinline__ void shift(uint32_t off, RowsRaw<16>& lo, RowsRaw<16>& hi)
     {
         if (off & 8u) { lo.r[0] = lo.r[2]; lo.r[1] = lo.r[3]; lo.r[2] = hi.r[0]; lo.r[3] = hi.r[1]; hi.r[0] = hi.r[2]; hi.r[1] = hi.r[3]; }
         if (off & 4u) { lo.r[0] = lo.r[1]; lo.r[1] = lo.r[2]; lo.r[2] = lo.r[3]; lo.r[3] = hi.r[0]; hi.r[0] = hi.r[1]; }
@@ -214,60 +214,130 @@ template <typename E> __device__ __forceinline__ float largest_of(const RowsRaw<
 {
     return Word<E>::largest(Word<E>::larger(Word<E>::larger(w.r[0], w.r[1]), Word<E>::larger(w.r[2], w.r[3])));
 }
-// The sum of exp(x - ref) over an access.  (x log2e - ref log2e as one fused operation would be off by the rounding of the second
-// product, and overflows where x - ref does not.)
-template <typename E> __device__ __forceinline__ float exp_sum(const RowsRaw<16>& w, float ref)
+// Two binary32 values in a register pair: one instruction works on both.
+__device__ __forceinline__ uint64_t pair_of(float lo, float hi)
 {
-    constexpr int N = 16 / (int)sizeof(E);
-    float e[N];
+    uint64_t p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(lo), "f"(hi));
+    return p;
+}
+__device__ __forceinline__ float2 both_of(uint64_t p)
+{
+    float2 f;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(p));
+    return f;
+}
+__device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b)
+{
+    uint64_t c;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(c) : "l"(a), "l"(b));
+    return c;
+}
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+// The sum of 2^(x log2e - c) over two accesses.  kPairs: two terms an instruction, with the same results (a third fewer instructions,
+// and more registers).
+template <bool kPairs, typename E> __device__ __forceinline__ float exp_sum(const RowsRaw<16>& a, const RowsRaw<16>& b, float c)
+{
+    constexpr int P = 8 / (int)sizeof(E);                  // pairs of an access
+    if constexpr (kPairs) {
+        const uint64_t scale = pair_of(kLog2e, kLog2e), minus_c = pair_of(-c, -c);
+        uint64_t e[2 * P];
 #pragma unroll
-    for (int i = 0; i < N; ++i) e[i] = exp2_of(__fmul_rn(__fsub_rn(Word<E>::get(w.r, i), ref), kLog2e));
+        for (int i = 0; i < 2 * P; ++i) {
+            const RowsRaw<16>& w = i % 2 ? b : a;
+            const float2 x = both_of(fma_pair(pair_of(Word<E>::get(w.r, i / 2 * 2), Word<E>::get(w.r, i / 2 * 2 + 1)), scale, minus_c));
+            e[i] = pair_of(exp2_of(x.x), exp2_of(x.y));
+        }
 #pragma unroll
-    for (int d = N / 2; d > 0; d >>= 1)
+        for (int d = 1; d < 2 * P; d *= 2)
 #pragma unroll
-        for (int i = 0; i < d; ++i) e[i] = __fadd_rn(e[i], e[i + d]);
-    return e[0];
+            for (int i = 0; i < 2 * P; i += 2 * d) e[i] = add_pair(e[i], e[i + d]);
+        const float2 f = both_of(e[0]);
+        return __fadd_rn(f.x, f.y);
+    } else {
+        float half[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float e[2 * P];
+#pragma unroll
+            for (int i = 0; i < 2 * P; ++i) e[i] = exp2_of(__fmaf_rn(Word<E>::get((i % 2 ? b : a).r, i / 2 * 2 + h), kLog2e, -c));
+#pragma unroll
+            for (int d = 1; d < 2 * P; d *= 2)
+#pragma unroll
+                for (int i = 0; i < 2 * P; i += 2 * d) e[i] = __fadd_rn(e[i], e[i + d]);
+            half[h] = e[0];
+        }
+        return __fadd_rn(half[0], half[1]);
+    }
+}
+// The sum of exp(x - ref) over an access, for any ref.
+template <typename E> __device__ __forceinline__ float exp_sum_of(const RowsRaw<16>& w, float ref)
+{
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16 / (int)sizeof(E); ++i) sum = __fadd_rn(sum, exp2_of(__fmul_rn(__fsub_rn(Word<E>::get(w.r, i), ref), kLog2e)));
+    return sum;
 }
 
 // What a thread knows of its part of a run.  Its accesses are taken in pairs.  (Four at a time need a quarter fewer instructions, and
 // more than the 64 registers that let four CTAs share an SM.)
 struct Stats {
     double sum;                     // of exp(x - ref)
-    float ref;
+    float ref;                      // (while the run is read: c, see below)
     float best, second, third;      // the largest logits of the three pairs that have the largest
-    uint32_t best_at, second_at;    // best_at: the access that has the largest logit first; second_at: any of the second pair's
+    uint32_t best_at, second_at;    // the first accesses of the two best pairs
     bool bad;
 };
-template <typename E> __device__ __forceinline__ void take(Stats& s, RowsRaw<16>& a, RowsRaw<16>& b, uint32_t v)
+// While a run is read the sum is of 2^(x log2e - c), c = ref log2e rounded: one fused operation a logit, and every term off by the same
+// factor, which is put right at the end.  (A difference first and then a product: 48 us instead of 40 at the size named above, the packed
+// operations and the loop without branches included.)  That is good for |ref| <= kFar, where the factor is near 1.  A thread's c starts at
+// that of -kFar; a logit above kFar makes it infinity, and no term counts from there on.  Where that leaves no sum -- no logit of the run is
+// far above -kFar, or a thread has one above kFar -- far_sum() takes it from the logits once more.
+constexpr float kFar = 1048576.0f;
+constexpr float kMost = 3000.0f;    // a pair whose sum is larger moves the reference to its largest logit
+template <typename E> __device__ __forceinline__ float largest_of(const RowsRaw<16>& a, const RowsRaw<16>& b)
 {
-    float top = 0.0f, sum = 0.0f;
-    uint32_t m = 0;
-#pragma unroll 1
-    for (uint32_t tries = 0; tries < 2; ++tries) {
-        m = Word<E>::larger(Word<E>::larger(a.r[0], a.r[1]), Word<E>::larger(a.r[2], a.r[3]));
-        top = Word<E>::largest(Word<E>::larger(m, Word<E>::larger(Word<E>::larger(b.r[0], b.r[1]), Word<E>::larger(b.r[2], b.r[3]))));
-        sum = kInf;
-        if (top < kInf) {
-            if (top > __fadd_rn(s.ref, 8.0f)) {
-                s.sum *= (double)exp2_of(__fmul_rn(__fsub_rn(s.ref, top), kLog2e));
-                s.ref = top;
-            }
-            sum = __fadd_rn(exp_sum<E>(a, s.ref), exp_sum<E>(b, s.ref));
-        }
-        if (sum < kInf) break;                       // (a NaN among the logits makes the sum one)
-        s.bad |= clean<E>(a);
-        s.bad |= clean<E>(b);
-    }
+    return Word<E>::largest(Word<E>::larger(Word<E>::larger(Word<E>::larger(a.r[0], a.r[1]), Word<E>::larger(a.r[2], a.r[3])),
+                                            Word<E>::larger(Word<E>::larger(b.r[0], b.r[1]), Word<E>::larger(b.r[2], b.r[3]))));
+}
+// Pair p, whose largest logit is `top`, with its sum.
+__device__ __forceinline__ void add(Stats& s, float top, float sum, uint32_t p)
+{
     s.sum += (double)sum;
     s.third = fmaxf(s.third, fminf(s.second, top));
     if (top > s.best) {
         s.second_at = s.best_at;
-        s.best_at = Word<E>::largest(m) == top ? v : v + kThreads;
+        s.best_at = p;
     } else if (top > s.second) {
-        s.second_at = v;
+        s.second_at = p;
     }
     s.second = fmaxf(s.second, fminf(s.best, top));
     s.best = fmaxf(s.best, top);
+}
+// Any pair p.
+template <typename E> __device__ __forceinline__ void take(Stats& s, RowsRaw<16>& a, RowsRaw<16>& b, uint32_t p)
+{
+    float top = 0.0f, sum = 0.0f;
+#pragma unroll 1
+    for (uint32_t tries = 0; tries < 4; ++tries) {           // (moved, cleaned of NaN and infinity, moved)
+        top = largest_of<E>(a, b);
+        sum = exp_sum<false, E>(a, b, s.ref);
+        if (sum <= kMost) break;                             // (a NaN among the logits makes the sum one)
+        const float to = top <= kFar ? __fmul_rn(top, kLog2e) : kInf;
+        if (top < kInf && to > s.ref) {
+            s.sum *= (double)exp2_of(__fsub_rn(s.ref, to));
+            s.ref = to;
+        } else {
+            s.bad |= clean<E>(a);
+            s.bad |= clean<E>(b);
+        }
+    }
+    add(s, top, sum, p);
 }
 
 __device__ __forceinline__ void copy_16(uint32_t to, const unsigned char* from)
@@ -279,6 +349,27 @@ __device__ __forceinline__ RowsRaw<16> ring_word(uint32_t at)
     RowsRaw<16> w;
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w.r[0]), "=r"(w.r[1]), "=r"(w.r[2]), "=r"(w.r[3]) : "r"(at) : "memory");
     return w;
+}
+
+// The sum of exp(x - best) over a thread's accesses of a run, read once more.
+template <typename E>
+__device__ __noinline__ double far_sum(const Run<E> r, float best)
+{
+    double sum = 0.0;
+    if (best == -kInf) return sum;
+#pragma unroll 1
+    for (uint32_t v = threadIdx.x; v < r.accesses; v += kThreads) {
+        RowsRaw<16> w, hi;
+        rows_load_if<false>(r.readable(v), w, r.words(v));
+        if (r.off) {
+            rows_load_if<false>(r.readable(v), hi, r.words(v) + 16);
+            Run<E>::shift(r.off, w, hi);
+        }
+        if (!r.whole(v)) r.mend(v, w);
+        clean<E>(w);
+        sum += (double)exp_sum_of<E>(w, best);
+    }
+    return sum;
 }
 
 // A thread's way through a run: pair p is accesses tid + 2p * kThreads and the next one.  kDepth pairs are in the ring at a time;
@@ -310,35 +401,118 @@ struct Stream {
         for (uint32_t p = 0; p < kDepth; ++p) issue(r, ring + p * 2 * kStep, p, at + p * kPairBytes, p >= r.from && p < plain(r));
     }
     static __device__ __forceinline__ void finish() { asm volatile("cp.async.wait_group 0;" ::: "memory"); }
-    // (a function of its own: inlined, the registers of what follows it in the kernel are spilled inside this loop)
-    static __device__ __noinline__ Stats run(const Run<E> r, uint32_t ring)
+    // The oldest pair in the ring.
+    static __device__ __forceinline__ void read(uint32_t slot, uint32_t off, RowsRaw<16>& a, RowsRaw<16>& b)
     {
-        Stats s{0.0, kLowest, -kInf, -kInf, -kInf, 0u, 0u, false};
-        const uint32_t all = pairs(r), plain_pairs = plain(r), last = ring + (kDepth - 1) * 2 * kStep;
-        const unsigned char* at = r.words(threadIdx.x) + kDepth * kPairBytes;
-        uint32_t slot = ring;
+        asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
+        a = ring_word(slot);
+        b = ring_word(slot + kStep);
+        if (kShifted) {
+            RowsRaw<16> a_hi = ring_word(slot + kThreads * 16u), b_hi = ring_word(slot + kStep + kThreads * 16u);
+            Run<E>::shift(off, a, a_hi);
+            Run<E>::shift(off, b, b_hi);
+        }
+    }
+    // The reference that take() gives a thread by its first pair; -kFar if that pair is out of the ordinary.
+    static __device__ __forceinline__ float first_reference(uint32_t ring, uint32_t off)
+    {
+        RowsRaw<16> a, b;
+        read(ring, off, a, b);
+        const float top = largest_of<E>(a, b);
+        return __fmul_rn(top > 16.0f - kFar && top <= kFar ? top : -kFar, kLog2e);
+    }
+    // Pairs from p on, all whole, up to `end` or to one that take() has to look at for a lane of the warp; p becomes the next pair.
+    // (Accesses first .. first + span - 1 may be read as 16-byte words.)
+    static __device__ __forceinline__ Stats whole_pairs(const unsigned char* at, uint32_t off, uint32_t first, uint32_t span, uint32_t ring, uint32_t& p,
+                                                        uint32_t end, Stats s)
+    {
+        const uint32_t last = ring + (kDepth - 1) * 2 * kStep;
+        uint32_t slot = ring + p % kDepth * 2 * kStep, v = threadIdx.x + 2 * (p + kDepth) * kThreads - first, q = p;
+        at += (uint64_t)(p + kDepth) * kPairBytes;
 #pragma unroll 1
-        for (uint32_t p = 0; p < all; ++p) {
-            asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
-            RowsRaw<16> a = ring_word(slot), b = ring_word(slot + kStep);
-            if (kShifted) {
-                RowsRaw<16> a_hi = ring_word(slot + kThreads * 16u), b_hi = ring_word(slot + kStep + kThreads * 16u);
-                r.shift(a, a_hi);
-                r.shift(b, b_hi);
-            }
-            const uint32_t v = threadIdx.x + 2 * p * kThreads;
-            if (p >= plain_pairs || p < r.from) {
-                if (!r.whole(v)) r.mend(v, a);
-                if (!r.whole(v + kThreads)) r.mend(v + kThreads, b);
-            }
-            take<E>(s, a, b, v);
-            issue(r, slot, p + kDepth, at, p + kDepth < plain_pairs);          // (into the slots that have just been read)
+        for (; q < end; ++q) {
+            RowsRaw<16> a, b;
+            read(slot, off, a, b);
+            const float sum = exp_sum<true, E>(a, b, s.ref);
+            if (__any_sync(0xFFFFFFFFu, !(sum <= kMost))) break;
+            add(s, largest_of<E>(a, b), sum, q);
+#pragma unroll
+            for (uint32_t i = 0; i < 2; ++i)                               // (into the slots that have just been read)
+                if (v + i * kThreads < span) {
+                    copy_16(slot + i * kStep, at + i * kThreads * 16u);
+                    if (kShifted) copy_16(slot + i * kStep + kThreads * 16u, at + i * kThreads * 16u + 16);
+                }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            v += 2 * kThreads;
             at += kPairBytes;
             slot = slot == last ? ring : slot + 2 * kStep;
         }
-        finish();
+        p = q;
         return s;
     }
+    // Pairs p .. end - 1, of any kind.
+    static __device__ __forceinline__ Stats any_pairs(const Run<E>& r, uint32_t ring, uint32_t p, uint32_t end, Stats s)
+    {
+        const unsigned char* at = r.words(threadIdx.x) + (uint64_t)(p + kDepth) * kPairBytes;
+#pragma unroll 1
+        for (; p < end; ++p) {
+            const uint32_t slot = ring + p % kDepth * 2 * kStep, v = threadIdx.x + 2 * p * kThreads;
+            RowsRaw<16> a, b;
+            read(slot, r.off, a, b);
+            if (!r.whole(v)) r.mend(v, a);
+            if (!r.whole(v + kThreads)) r.mend(v + kThreads, b);
+            take<E>(s, a, b, p);
+            issue(r, slot, p + kDepth, at, false);
+            at += kPairBytes;
+        }
+        return s;
+    }
+    static __device__ __noinline__ Stats whole_call(const unsigned char* at, uint32_t off, uint32_t first, uint32_t span, uint32_t ring, uint32_t& p,
+                                                    uint32_t end, Stats s)
+    {
+        return whole_pairs(at, off, first, span, ring, p, end, s);
+    }
+    static __device__ __noinline__ Stats any_call(const Run<E> r, uint32_t ring, uint32_t p, uint32_t end, Stats s) { return any_pairs(r, ring, p, end, s); }
+
+    template <bool kCalls> static __device__ __forceinline__ Stats walk(const Run<E>& r, uint32_t ring)
+    {
+        Stats s{0.0, -kFar * kLog2e, -kInf, -kInf, -kInf, 0u, 0u, false};
+        const uint32_t all = pairs(r), whole = plain(r), first = kShifted ? r.from : 0u;
+        constexpr uint32_t kLeast = kCalls ? kLong : 1u;                   // whole pairs that are worth a call
+        if (whole && !first) s.ref = first_reference(ring, r.off);
+        uint32_t p = 0;
+#pragma unroll 1
+        while (p < all) {
+            if (p >= first && p + kLeast <= whole) {
+                if constexpr (kCalls) s = whole_call(r.words(threadIdx.x), r.off, first, r.upto - first, ring, p, whole, s);
+                else s = whole_pairs(r.words(threadIdx.x), r.off, first, r.upto - first, ring, p, whole, s);
+            }
+            if (p >= all) break;
+            const uint32_t to = p + kLeast <= whole ? p + 1 : all;
+            if constexpr (kCalls) s = any_call(r, ring, p, to, s);
+            else s = any_pairs(r, ring, p, to, s);
+            p = to;
+        }
+        finish();
+        s.best_at = threadIdx.x + 2 * kThreads * s.best_at;
+        s.second_at = threadIdx.x + 2 * kThreads * s.second_at;
+        const float c = s.ref;
+        if (!__syncthreads_or(c > (4.0f - kFar) * kLog2e) || c == kInf) {
+            s.ref = kInf;                                                  // (for far_sum)
+        } else {
+            // c = ref log2e + off: the sum is 2^off too small
+            s.ref = __fmul_rn(c, kLn2);
+            const float off = __fmul_rn(__fmaf_rn(-s.ref, kLog2e, c), kLn2);
+            const float more = __fmaf_rn(__fmul_rn(off, off), __fmaf_rn(off, 0.166666667f, 0.5f), off);       // e^off - 1, |off| < 0.1
+            s.sum = fma(s.sum, (double)more, s.sum);
+        }
+        return s;
+    }
+    // Long runs call a function for the loop, because inlined the registers of what follows in the kernel are spilled inside it (42 us
+    // instead of 40); short ones are a function as a whole, whose way is shorter (8.7 us for 4 rows of 32003 instead of 9.1).
+    static constexpr uint32_t kLong = 9;
+    static __device__ __noinline__ Stats short_run(const Run<E> r, uint32_t ring) { return walk<false>(r, ring); }
+    static __device__ __forceinline__ Stats run(const Run<E>& r, uint32_t ring) { return plain(r) < kLong ? short_run(r, ring) : walk<true>(r, ring); }
 };
 
 // The logits of the pair of accesses that `access` is one of that reach the bound, appended to `offers`.
@@ -354,21 +528,18 @@ __device__ __noinline__ void collect(const Run<E> r, uint32_t access, uint64_t a
         if (r.off) rows_load_if<false>(r.readable(access + m * kThreads), hi[m], r.words(access + m * kThreads) + 16);
     }
     // (no branch a logit: a few cycles each instead of some hundred)
-    const float low = logit_of_bound(at_least);
-    const bool finite = low > -kInf;
-    const uint32_t last = 0xFFFFFFFFu - (uint32_t)at_least;               // of equal logits those up to this token
+    const float low = logit_of_bound(at_least), above = low > -kInf ? from_rising((uint32_t)(at_least >> 32) + 1u) : kLowest;
+    const uint32_t last = 0xFFFFFFFFu - (uint32_t)at_least;               // of equal logits those up to this token, and some after it
     uint32_t reach = 0;                                                   // bit m * N + j: logit j of access m reaches the bound
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
-        if (r.off) r.shift(w[m], hi[m]);
+        if (r.off) Run<E>::shift(r.off, w[m], hi[m]);
         if (!r.whole(access + m * kThreads)) r.mend(access + m * kThreads, w[m]);
-        const uint32_t token = first + (access + m * kThreads) * N;
-        const int equals = finite && token <= last ? (int)(last - token < (uint32_t)N ? last - token + 1u : (uint32_t)N) : 0;
+        const float least = low > -kInf && first + (access + m * kThreads) * N <= last ? low : above;
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             const float x = Word<E>::get(w[m].r, j);
-            const bool over = x > low, even = (x == low) & (j < equals);
-            reach |= (over | even) & (x < kInf) ? 1u << (m * N + j) : 0u;
+            if ((x >= least) & (x < kInf)) reach |= 1u << (m * N + j);
         }
     }
     uint32_t to = reach ? atomicAdd(n_offers, (uint32_t)__popc(reach)) : 0u;
@@ -530,11 +701,15 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const SelectArgs a)
             if (tid < ctas) send(sums_at + u * (uint32_t)sizeof(UnitSum), bar, tid, UnitSum{0.0, kLowest, n});
             continue;
         }
-        const Stats s = r.off ? Stream<true, E>::run(r, ring) : Stream<false, E>::run(r, ring);
+        Stats s = r.off ? Stream<true, E>::run(r, ring) : Stream<false, E>::run(r, ring);
+        if (s.ref == kInf) {
+            s.sum = far_sum<E>(r, s.best);
+            s.ref = fmaxf(s.best, kLowest);
+        }
         if (s.bad) atomicOr(a.status, PEARL_ST_BAD_SCORE);
 
-        // a bound that C logits reach: the smallest key that the logit of its access can have stands for it
-        const uint64_t key = s.best == -kInf ? 0ull : key_of(s.best, (uint32_t)first + s.best_at * N + N - 1);
+        // a bound that C logits reach: the smallest key that the logit of its pair can have stands for it
+        const uint64_t key = s.best == -kInf ? 0ull : key_of(s.best, (uint32_t)first + (s.best_at + kThreads) * N + N - 1);
         const uint32_t full_warps = r.accesses / 32u;
         const uint32_t active = full_warps < 1u ? 1u : full_warps < kWarps ? full_warps : kWarps;
         const uint32_t need = (C + active - 1) / active;
@@ -549,8 +724,8 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const SelectArgs a)
             const uint32_t low = __reduce_min_sync(0xFFFFFFFFu, (uint32_t)(key >> 32) == top ? (uint32_t)key : 0xFFFFFFFFu);
             mark = top ? ((uint64_t)top << 32) | low : 1ull;                 // (too few lanes have a logit: every logit is an offer)
         }
-        // the warp's sum relative to its largest reference, in fixed point (30 bits behind the point: the sum is 1 at least if there
-        // is a logit, and 2^60 of these at most): whole numbers add up in any order, three limbs of 22 bits at a time
+        // the warp's sum relative to its largest reference, in fixed point (30 bits behind the point: the sum is near 1 at least if
+        // there is a logit, and 2^60 of these at most): whole numbers add up in any order, three limbs of 22 bits at a time
         {
             const float ref = from_rising(__reduce_max_sync(0xFFFFFFFFu, rising(s.ref)));
             const double scaled = s.sum * (double)exp2_of(__fmul_rn(__fsub_rn(s.ref, ref), kLog2e));

@@ -398,6 +398,49 @@ def test_beam_select_crowded(rows, kind):
             check_select(rows, logits, torch.zeros(1, 1), C)
 
 
+@pytest.mark.parametrize("kind", ["fp32", "fp16", "bf16"])
+@pytest.mark.parametrize("V", [1500, 60011])
+def test_beam_select_magnitudes(rows, kind, V):
+    """Logits around values of every size, on both sides of 2^20 (where the sums change their way) among others."""
+    t = TYPES[kind]
+    bases = [-40.0, -300.0, 300.0, 6e4, -6e4]
+    if kind != "fp16":
+        bases += [1048576.0 - 20, 1048576.0 + 20, -1048576.0 - 20, -1048576.0 + 20, 1e6, 3e6, -3e6, 1e30, -1e30, 2.5e38, -3e38]
+    noise = torch.randn(1, 2, V, generator=gen(59, V))
+    for base in bases:
+        for spread in (2.0, 1000.0):
+            logits = (noise * spread + base).to(t)
+            check_select(rows, logits, torch.tensor([[0.0, -0.5]]), 9)
+    assert rows.sync() == 0
+    # ordinary rows with a few logits that are far above or far below, or not numbers
+    for value in (3e4,) if kind == "fp16" else (2e6, 3e38, -3e38):
+        for at in ([0], [V - 1], [5, 6, V // 2, V // 2 + 1], list(range(0, V, 700))):
+            logits = (noise * 3).to(t)
+            logits[0, :, at] = value
+            check_select(rows, logits, torch.tensor([[0.0, -0.5]]), 9)
+            logits[0, 0, 3::311] = math.nan
+            logits[0, 1, 1::411] = math.inf
+            assert rows.sync() == 0
+            check_select(rows, logits, torch.tensor([[0.0, -0.5]]), 9)
+            assert rows.sync() == BAD_SCORE
+
+
+@pytest.mark.parametrize("kind", ["fp32", "bf16"])
+def test_beam_select_equal_long_rows(rows, kind):
+    """Equal rows of many accesses have equal sums at every offset from a 16-byte boundary."""
+    V, W, C = 60013, 9, 18
+    row = (torch.randn(1, V, generator=gen(60)) * 4).to(TYPES[kind])
+    row[0, 30000:30100] += 14.0
+    logits = row.expand(W, V).contiguous().view(1, W, V)
+    scores = torch.full((1, W), -1.5)
+    dense = check_select(rows, logits, scores, C)
+    for extra, shift in ((1, 0), (3, 5), (0, 3), (8, 7)):
+        got = check_select(rows, logits, scores, C, view=strided(logits[0], extra, shift).unsqueeze(0))
+        assert all((a == b).all() for a, b in zip(got, dense))
+    first = np.sort(f64(row)[0])[::-1]
+    assert first[0] == first[1] or dense[1][0].tolist()[:W] == list(range(W))
+
+
 @pytest.mark.parametrize("kind", ["fp32", "bf16"])
 def test_beam_select_mostly_masked(rows, kind):
     """Most of a vocabulary barred or masked with the type's lowest value, in blocks that leave some warps without a logit, and more
