@@ -4,8 +4,9 @@
 // orders like (larger logit, lower expert): for 16-bit logits 32 bits, so that a comparison and exchange is one minimum and one
 // maximum.  A lane sorts its logits KP at a time by a network (KP: k rounded up to a power of two), keeps the KP best of them by
 // bitonic merges, and merges with the other lanes' lists by exchanges.  No branch depends on the data.  65521 rows of 128 bfloat16
-// logits, k = 8, choice and gradient: 15.4 us (by rounds, below: 49); the choice is bound by its minima and maxima, which run at half
-// the rate of other instructions (59 a row), the gradient, 9.5 us on its own, by the 16.8 MB it writes and the instructions for it.
+// logits, k = 8, over the chosen ones: 9.5 us, bound by minima and maxima, which run at half the rate of other instructions (59 a row);
+// its gradient 5.5 us, of which the 23 MB it reads and writes are 3.5 (both: 15.2; by rounds, below: 49).  binary32 logits cost more, because a
+// 64-bit minimum and maximum are six instructions: 65521 rows of 64, k = 6: 14.5 us.
 // More choices (rounds_kernel): k rounds of "largest that is left" over the row's lanes.
 #include "rows_internal.cuh"
 
@@ -380,8 +381,10 @@ __device__ __forceinline__ bool load_block(const E* x, uint32_t c, uint32_t expe
         if (!(v[i] < kInf)) { bad = true; v[i] = -kInf; }
     return bad;
 }
-constexpr uint32_t kRowFloats = 1024;                // of shared memory per warp at most: R rows of the experts, rounded up to 4
-template <typename E, int M, bool kChosen>
+// Where the softmax runs over all experts a lane holds its logits, H = 16 or 32 of them, and then their exponentials (read again for the
+// maximum, the sum and the gradient: 16.1 us instead of 12.6 for 65521 rows of 128 bfloat16 logits).
+constexpr uint32_t kRowFloats = 1024;                // of shared memory per warp at most: R rows of the experts, rounded up to 4; so 32 a lane
+template <typename E, int M, bool kChosen, int H>
 __global__ void __launch_bounds__(kThreads) route_grad_kernel(unsigned* status, uint32_t T, uint32_t experts, uint32_t k, uint32_t log_kl,
                                                               uint32_t log_r, const E* __restrict__ logits, uint64_t ld,
                                                               const float* __restrict__ w, const int32_t* __restrict__ ids,
@@ -443,32 +446,44 @@ __global__ void __launch_bounds__(kThreads) route_grad_kernel(unsigned* status, 
         const uint64_t t = ((uint64_t)group << log_r) + row;
         mean = __shfl_sync(0xFFFFFFFFu, mean, (int)(row << log_kl));
         const bool there = t < T;
-        float top = -kInf, sum = 0.0f, shift = 0.0f, p_scale = 0.0f;
-        const E* x = logits + (there ? t : 0) * ld;
-        if (!kChosen) {
+        float held[kChosen ? 1 : H / B][B];
+        if constexpr (!kChosen) {
+            float top = -kInf, sum = 0.0f;
+            const E* x = logits + (there ? t : 0) * ld;
             bool bad = false;
-            for (uint32_t c = from; c < experts && there; c += step) {
-                float v[B];
-                bad |= load_block<E, M, B>(x, c, experts, v);
 #pragma unroll
-                for (int i = 0; i < B; ++i) top = fmaxf(top, v[i]);
+            for (int n = 0; n < H / B; ++n) {
+                const uint32_t c = from + n * step;
+                if (c < experts && there) {
+                    bad |= load_block<E, M, B>(x, c, experts, held[n]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < B; ++i) held[n][i] = -kInf;
+                }
             }
             if (bad) atomicOr(status, PEARL_ST_BAD_SCORE);
-            for (uint32_t q = 1; q < 1u << log_lr; q *= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, q));
-            shift = top == -kInf ? 0.0f : top;
-            for (uint32_t c = from; c < experts && there; c += step) {
-                float v[B];
-                load_block<E, M, B>(x, c, experts, v);
 #pragma unroll
-                for (int i = 0; i < B; ++i) sum = __fadd_rn(sum, __expf(__fsub_rn(v[i], shift)));
-            }
+            for (int n = 0; n < H / B; ++n)
+#pragma unroll
+                for (int i = 0; i < B; ++i) top = fmaxf(top, held[n][i]);
+            for (uint32_t q = 1; q < 1u << log_lr; q *= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, q));
+            const float shift = top == -kInf ? 0.0f : top;
+#pragma unroll
+            for (int n = 0; n < H / B; ++n)
+#pragma unroll
+                for (int i = 0; i < B; ++i) {
+                    held[n][i] = __expf(__fsub_rn(held[n][i], shift));
+                    sum = __fadd_rn(sum, held[n][i]);
+                }
             for (uint32_t q = 1; q < 1u << log_lr; q *= 2) sum = __fadd_rn(sum, __shfl_xor_sync(0xFFFFFFFFu, sum, q));
-            p_scale = sum > 0.0f ? __fdiv_rn(1.0f, sum) : 0.0f;
+            const float p_scale = sum > 0.0f ? __fdiv_rn(1.0f, sum) : 0.0f;
+#pragma unroll
+            for (int n = 0; n < H / B; ++n)
+#pragma unroll
+                for (int i = 0; i < B; ++i) held[n][i] = __fmul_rn(held[n][i], p_scale);
         }
         const float* mine = g + row * pitch;
-        for (uint32_t c = from; c < experts && there; c += step) {
-            float v[B];
-            if (!kChosen) load_block<E, M, B>(x, c, experts, v);
+        const auto write = [&](uint32_t c, const float* p) {
             float part[B];
 #pragma unroll
             for (int i = 0; i < B; i += 4) {
@@ -478,8 +493,7 @@ __global__ void __launch_bounds__(kThreads) route_grad_kernel(unsigned* status, 
             }
             if (!kChosen) {
 #pragma unroll
-                for (int i = 0; i < B; ++i)
-                    part[i] = __fmul_rn(__fmul_rn(__expf(__fsub_rn(v[i], shift)), p_scale), __fsub_rn(part[i], mean));
+                for (int i = 0; i < B; ++i) part[i] = __fmul_rn(p[i], __fsub_rn(part[i], mean));
             }
 #pragma unroll
             for (int i = 0; i < B; i += M) {
@@ -487,6 +501,13 @@ __global__ void __launch_bounds__(kThreads) route_grad_kernel(unsigned* status, 
                 out.set(part + i);
                 if (c + i < experts) rows_store_vec<E, M>(dlogits + t * ld_d + c + i, out);
             }
+        };
+        if constexpr (kChosen) {
+            for (uint32_t c = from; c < experts && there; c += step) write(c, nullptr);
+        } else {
+#pragma unroll
+            for (int n = 0; n < H / B; ++n)
+                if (from + n * step < experts && there) write(from + n * step, held[n]);
         }
         __syncwarp();
         if (id >= 0) g[to] = 0.0f;                                        // (all zeros again)
@@ -581,18 +602,22 @@ int rows_launch_route_grad(unsigned* status, uint32_t T, uint32_t E, uint32_t k,
     const uint32_t granule = rows_granule((uint64_t)E * bytes, (uintptr_t)dlogits, ld_d * bytes, over_chosen ? 0 : (uintptr_t)logits,
                                           over_chosen ? 0 : ld * bytes);
     int rc = -1;
-#define ROWS_GO(M, CHOSEN)                                                                                                     \
-    rc = rows_launch(route_grad_kernel<ROWS_T, M, CHOSEN>, grid, dim3(kThreads), smem, s, 0, status, T, E, k, log_kl, log_r, \
+#define ROWS_GO(M, CHOSEN, H)                                                                                                  \
+    rc = rows_launch(route_grad_kernel<ROWS_T, M, CHOSEN, H>, grid, dim3(kThreads), smem, s, 0, status, T, E, k, log_kl, log_r, \
                      (const ROWS_T*)logits, ld, w, ids, dw, (ROWS_T*)dlogits, ld_d)
+#define ROWS_WIDTH(CHOSEN, H)                                                                                                  \
+    do { if (granule >= 16) ROWS_GO(kWide, CHOSEN, H); else if (granule >= 8) ROWS_GO(kWide / 2, CHOSEN, H); else ROWS_GO(1, CHOSEN, H); } while (0)
 #define ROWS_TYPE(X)                                                                                                           \
     do {                                                                                                                       \
         typedef X ROWS_T;                                                                                                      \
         constexpr int kWide = 16 / (int)sizeof(ROWS_T);                                                                        \
-        if (over_chosen) { if (granule >= 16) ROWS_GO(kWide, true); else if (granule >= 8) ROWS_GO(kWide / 2, true); else ROWS_GO(1, true); } \
-        else { if (granule >= 16) ROWS_GO(kWide, false); else if (granule >= 8) ROWS_GO(kWide / 2, false); else ROWS_GO(1, false); }          \
+        if (over_chosen) ROWS_WIDTH(true, 16);                                                                                 \
+        else if (E <= 16u << (5 - log_r)) ROWS_WIDTH(false, 16);                                                               \
+        else ROWS_WIDTH(false, 32);                                                                                            \
     } while (0)
     ROWS_WITH_TYPE(dtype, ROWS_TYPE);
 #undef ROWS_TYPE
+#undef ROWS_WIDTH
 #undef ROWS_GO
     return rc;
 }
