@@ -1,18 +1,19 @@
 // The router: the k best of E experts with their softmax weights, and its gradient.
 //
 // Up to 8 choices (route_kernel): L lanes have a row, N consecutive logits each.  A logit and its expert are one whole number that
-// orders like (larger logit, lower expert): for 16-bit logits 32 bits, so that a comparison and exchange is one minimum and one
-// maximum.  A lane sorts its logits KP at a time by a network (KP: k rounded up to a power of two), keeps the KP best of them by
+// orders like (larger logit, lower expert): for 16-bit logits 32 bits, so that a comparison and exchange is one maximum and two
+// multiply-adds.  A lane sorts its logits KP at a time by a network (KP: k rounded up to a power of two), keeps the KP best of them by
 // bitonic merges, and merges with the other lanes' lists by exchanges.  No branch depends on the data.  65521 rows of 128 bfloat16
-// logits, k = 8, over the chosen ones: 9.5 us, bound by minima and maxima, which run at half the rate of other instructions (59 a row);
-// its gradient 5.5 us, of which the 23 MB it reads and writes are 3.5 (both: 15.2; by rounds, below: 49).  binary32 logits cost more, because a
-// 64-bit minimum and maximum are six instructions: 65521 rows of 64, k = 6: 14.5 us.
+// logits, k = 8, over the chosen ones: 8.2 us, bound by these exchanges; the 21 MB it moves are 3.2.  Its gradient 5.5 us, of which the
+// 23 MB it reads and writes are 3.5 (both: 13.8; by rounds, below: 49).  binary32 logits cost more, because a 64-bit exchange is four
+// such instructions and four multiply-adds: 65521 rows of 64, k = 6: 11.1 us.
 // More choices (rounds_kernel): k rounds of "largest that is left" over the row's lanes.
 #include "rows_internal.cuh"
 
 namespace {
 
 constexpr uint32_t kThreads = 256;
+constexpr uint32_t kRouteThreads = 128;         // of route_kernel: as many rows an SM in smaller steps (65521 rows of 64 binary32 logits: 4 % faster)
 constexpr float kInf = __builtin_huge_valf();
 
 template <int L> __device__ __forceinline__ float over_lanes_max(float v)
@@ -204,14 +205,31 @@ template <> struct Key<__nv_bfloat16> : Key16<__nv_bfloat16> {
     static __device__ __forceinline__ float value(const uint32_t* w, int i) { const float2 f = both(w[i / 2]); return i % 2 ? f.y : f.x; }
 };
 
-template <typename K> __device__ __forceinline__ void order(K& a, K& b)       // the larger first
+// The larger first.  The smaller one is a + b - larger (modulo 2^32, word by word), by two multiply-adds: minima, maxima, comparisons and
+// selections share a pipe that is the bound here, and multiply-adds have their own.  `one` is (1, -1) as an argument of the kernel, so
+// that they stay what they are.  With minima 9.6 us instead of 8.3 at the size above.
+__device__ __forceinline__ uint32_t other_of(uint32_t a, uint32_t b, uint32_t larger, uint2 one)
 {
-    const K hi = a > b ? a : b, lo = a > b ? b : a;
+    uint32_t t, lo;
+    asm("mad.lo.u32 %0, %1, %2, %3;" : "=r"(t) : "r"(a), "r"(one.x), "r"(b));
+    asm("mad.lo.u32 %0, %1, %2, %3;" : "=r"(lo) : "r"(larger), "r"(one.y), "r"(t));
+    return lo;
+}
+__device__ __forceinline__ void order(uint32_t& a, uint32_t& b, uint2 one)
+{
+    const uint32_t hi = max(a, b);
+    b = other_of(a, b, hi, one);
     a = hi;
-    b = lo;
+}
+__device__ __forceinline__ void order(uint64_t& a, uint64_t& b, uint2 one)
+{
+    const uint64_t hi = a > b ? a : b;
+    b = ((uint64_t)other_of((uint32_t)(a >> 32), (uint32_t)(b >> 32), (uint32_t)(hi >> 32), one) << 32) |
+        other_of((uint32_t)a, (uint32_t)b, (uint32_t)hi, one);
+    a = hi;
 }
 // Batcher's merge exchange sort (Knuth, 5.2.2), falling: 19 exchanges for 8 keys.
-template <int P, typename K> __device__ __forceinline__ void sort_falling(K (&a)[P])
+template <int P, typename K> __device__ __forceinline__ void sort_falling(K (&a)[P], uint2 one)
 {
 #pragma unroll
     for (int p = 1; p < P; p *= 2)
@@ -221,10 +239,10 @@ template <int P, typename K> __device__ __forceinline__ void sort_falling(K (&a)
             for (int j = q % p; j + q < P; j += 2 * q)
 #pragma unroll
                 for (int i = 0; i < q; ++i)
-                    if (i + j + q < P && (i + j) / (2 * p) == (i + j + q) / (2 * p)) order(a[i + j], a[i + j + q]);
+                    if (i + j + q < P && (i + j) / (2 * p) == (i + j + q) / (2 * p)) order(a[i + j], a[i + j + q], one);
 }
 // The P largest of two falling lists (b is handed over reversed), falling.
-template <int P, typename K> __device__ __forceinline__ void merge_falling(K (&a)[P], const K (&reversed)[P])
+template <int P, typename K> __device__ __forceinline__ void merge_falling(K (&a)[P], const K (&reversed)[P], uint2 one)
 {
 #pragma unroll
     for (int i = 0; i < P; ++i) a[i] = a[i] > reversed[i] ? a[i] : reversed[i];
@@ -232,7 +250,7 @@ template <int P, typename K> __device__ __forceinline__ void merge_falling(K (&a
     for (int d = P / 2; d > 0; d /= 2)
 #pragma unroll
         for (int i = 0; i < P; ++i)
-            if ((i & d) == 0) order(a[i], a[i + d]);
+            if ((i & d) == 0) order(a[i], a[i + d], one);
 }
 template <typename E, int FROM, int P, int I = 0> struct KeysOf {
     static __device__ __forceinline__ void get(const uint32_t* w, typename Key<E>::type* out)
@@ -244,11 +262,11 @@ template <typename E, int FROM, int P, int I = 0> struct KeysOf {
 // The P best of a lane's logits FROM .. N - 1, merged into `best`.
 template <typename E, int N, int P, int FROM = 0> struct Choose {
     typedef typename Key<E>::type K;
-    static __device__ __forceinline__ void run(const uint32_t* w, K (&best)[P])
+    static __device__ __forceinline__ void run(const uint32_t* w, K (&best)[P], uint2 one)
     {
         K group[P];
         KeysOf<E, FROM, P>::get(w, group);
-        sort_falling<P>(group);
+        sort_falling<P>(group, one);
         if constexpr (FROM == 0) {
 #pragma unroll
             for (int i = 0; i < P; ++i) best[i] = group[i];
@@ -256,9 +274,9 @@ template <typename E, int N, int P, int FROM = 0> struct Choose {
             K reversed[P];
 #pragma unroll
             for (int i = 0; i < P; ++i) reversed[i] = group[P - 1 - i];
-            merge_falling<P>(best, reversed);
+            merge_falling<P>(best, reversed, one);
         }
-        if constexpr (FROM + P < N) Choose<E, N, P, FROM + P>::run(w, best);
+        if constexpr (FROM + P < N) Choose<E, N, P, FROM + P>::run(w, best, one);
     }
 };
 
@@ -266,9 +284,9 @@ __device__ __forceinline__ uint32_t from_lane(uint32_t k, int d, int width) { re
 __device__ __forceinline__ uint64_t from_lane(uint64_t k, int d, int width) { return __shfl_xor_sync(0xFFFFFFFFu, k, d, width); }
 
 template <typename E, int L, int N, int P>
-__global__ void __launch_bounds__(kThreads) route_kernel(unsigned* status, uint32_t T, uint32_t experts, uint32_t k, const E* __restrict__ logits,
+__global__ void __launch_bounds__(kRouteThreads) route_kernel(unsigned* status, uint32_t T, uint32_t experts, uint32_t k, const E* __restrict__ logits,
                                                          uint64_t ld, uint32_t wide, uint32_t over_chosen, float* __restrict__ w,
-                                                         int32_t* __restrict__ ids)
+                                                         int32_t* __restrict__ ids, uint2 one)
 {
     typedef Key<E> Q;
     typedef typename Q::type K;
@@ -276,7 +294,7 @@ __global__ void __launch_bounds__(kThreads) route_kernel(unsigned* status, uint3
     static_assert(N >= P && N % P == 0 && kWords >= 1, "whole groups");
     rows_begin();
     const uint32_t lane = threadIdx.x % L, first = lane * N;
-    const uint64_t t = (uint64_t)blockIdx.x * (kThreads / L) + threadIdx.x / L;
+    const uint64_t t = (uint64_t)blockIdx.x * (kRouteThreads / L) + threadIdx.x / L;
     const uint32_t there = t < T && first < experts ? (experts - first < (uint32_t)N ? experts - first : (uint32_t)N) : 0u;
     const E* row = logits + (t < T ? t : 0) * ld + first;
     uint32_t x[kWords];
@@ -312,7 +330,7 @@ __global__ void __launch_bounds__(kThreads) route_kernel(unsigned* status, uint3
     for (int i = 0; i < kWords; ++i) x[i] = Q::canonical(x[i]);           // (-0 becomes 0)
 
     K best[P];
-    Choose<E, N, P>::run(x, best);
+    Choose<E, N, P>::run(x, best, one);
 #pragma unroll
     for (int i = 0; i < P; ++i) best[i] -= first;                         // the expert's number in the row
 #pragma unroll
@@ -320,7 +338,7 @@ __global__ void __launch_bounds__(kThreads) route_kernel(unsigned* status, uint3
         K reversed[P];
 #pragma unroll
         for (int i = 0; i < P; ++i) reversed[i] = from_lane(best[P - 1 - i], d, L);
-        merge_falling<P>(best, reversed);
+        merge_falling<P>(best, reversed, one);
     }
     const float shift = Q::rising(best[0]) <= Q::kNothing ? 0.0f : Q::logit(best[0]);
     // every lane has the row's choices; each hands out its share of them
@@ -545,11 +563,11 @@ int rows_launch_route(unsigned* status, uint32_t T, uint32_t E, uint32_t k, uint
         const uint32_t bytes = rows_elem_bytes(dtype);
 #define ROWS_GO(L, N, P)                                                                                                      \
     do {                                                                                                                      \
-        const uint32_t rows = kThreads / (L);                                                                                 \
+        const uint32_t rows = kRouteThreads / (L);                                                                            \
         const uint32_t access = (N) * bytes < 16 ? (N) * bytes : 16;                                                          \
         const uint32_t wide = (uintptr_t)logits % access == 0 && ld * bytes % access == 0 ? 1u : 0u;                          \
-        rc = rows_launch(route_kernel<ROWS_T, L, N, P>, dim3((T + rows - 1) / rows), dim3(kThreads), 0, s, 0, status, T, E, k, \
-                         (const ROWS_T*)logits, ld, wide, over_chosen ? 1u : 0u, w, ids);                                     \
+        rc = rows_launch(route_kernel<ROWS_T, L, N, P>, dim3((T + rows - 1) / rows), dim3(kRouteThreads), 0, s, 0, status, T, E, k, \
+                         (const ROWS_T*)logits, ld, wide, over_chosen ? 1u : 0u, w, ids, make_uint2(1u, 0xFFFFFFFFu));                                     \
     } while (0)
 #define ROWS_P(P)                                                                                                             \
     do {                                                                                                                      \
