@@ -316,14 +316,14 @@ _routers = {}
 
 
 def _router(s):
-    """The program's handle: made once for a stream, and kept where the program keeps its tensors."""
-    if "router" not in s:
-        stream = torch.cuda.current_stream()
-        key = (stream.device_index, stream.cuda_stream)
+    """The program's handle of the current stream: made once for it, and kept where the program keeps its tensors."""
+    stream = torch.cuda.current_stream()
+    key = (stream.device_index, stream.cuda_stream)
+    if s.get("stream") != key:
         if key not in _routers:
             from paper_2311_09445_b200 import RowRouter
             _routers[key] = RowRouter(stream=stream)
-        s["router"] = _routers[key]
+        s["stream"], s["router"] = key, _routers[key]
     return s["router"]
 
 
