@@ -922,7 +922,7 @@ __global__ void __launch_bounds__(kMoveThreads) reorder_kernel(const ReorderArgs
     int32_t from[M];
     bool bad = false;
 #pragma unroll
-    for (int i = 0; i < M; ++i) from[i] = (uint32_t)i < a.W ? __ldg(a.parent + (uint64_t)g * a.W + i) : -1;
+    for (int i = 0; i < M; ++i) from[i] = rows_read_if((uint32_t)i < a.W, a.parent + (uint64_t)g * a.W + i, -1);
 #pragma unroll
     for (int i = 0; i < M; ++i) {
         bad |= from[i] < -1 || from[i] >= (int32_t)a.W;
@@ -957,7 +957,7 @@ __global__ void __launch_bounds__(kMoveThreads) reorder_any_kernel(const Reorder
     int32_t from[M];
     bool bad = false;
 #pragma unroll
-    for (int i = 0; i < M; ++i) from[i] = (uint32_t)i < a.W ? __ldg(a.parent + (uint64_t)g * a.W + i) : -1;
+    for (int i = 0; i < M; ++i) from[i] = rows_read_if((uint32_t)i < a.W, a.parent + (uint64_t)g * a.W + i, -1);
 #pragma unroll
     for (int i = 0; i < M; ++i) {
         bad |= from[i] < -1 || from[i] >= (int32_t)a.W;

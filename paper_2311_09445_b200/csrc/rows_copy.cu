@@ -24,12 +24,12 @@ Tiling tile(uint32_t rows, uint32_t cols)
 
 // The places of KC slots from `first` on, -1 where there is none or it is out of range (which is reported once a slot).
 template <int KC>
-__device__ __forceinline__ void load_places(unsigned* status, const int32_t* __restrict__ place, uint32_t n, uint32_t sorted_rows, bool report,
+__device__ __forceinline__ void load_places(unsigned* status, const int32_t* place, uint32_t n, uint32_t sorted_rows, bool report,
                                             int32_t (&at)[KC])
 {
     bool bad = false;
 #pragma unroll
-    for (int j = 0; j < KC; ++j) at[j] = (uint32_t)j < n ? __ldg(place + j) : -1;
+    for (int j = 0; j < KC; ++j) at[j] = rows_read_if((uint32_t)j < n, place + j, -1);
 #pragma unroll
     for (int j = 0; j < KC; ++j)
         if ((uint32_t)at[j] >= sorted_rows) {
@@ -45,9 +45,9 @@ __device__ __forceinline__ void load_places(unsigned* status, const int32_t* __r
 // 101.)
 template <int B, int KC>
 __global__ void __launch_bounds__(kThreads) dispatch_kernel(unsigned* status, uint32_t T, uint32_t k, uint32_t cols, uint32_t across,
-                                                            uint32_t down, const unsigned char* __restrict__ x, uint64_t ld_x,
-                                                            const int32_t* __restrict__ place, uint32_t sorted_rows,
-                                                            unsigned char* __restrict__ xs)
+                                                            uint32_t down, const unsigned char* x, uint64_t ld_x,
+                                                            const int32_t* place, uint32_t sorted_rows,
+                                                            unsigned char* xs)
 {
     rows_begin();
     const uint32_t in = threadIdx.x / across;
@@ -68,8 +68,8 @@ __global__ void __launch_bounds__(kThreads) dispatch_kernel(unsigned* status, ui
 // The same where rows start at odd bytes or odd 2-byte places: a thread has a 16-byte word of each of the k destinations.
 template <int S, int KC>
 __global__ void __launch_bounds__(kThreads) dispatch_any_kernel(unsigned* status, uint32_t T, uint32_t k, uint32_t row_bytes, uint32_t cols, uint32_t across,
-                                                                uint32_t down, const unsigned char* __restrict__ x, uint64_t ld_x,
-                                                                const int32_t* __restrict__ place, uint32_t sorted_rows, unsigned char* xs)
+                                                                uint32_t down, const unsigned char* x, uint64_t ld_x,
+                                                                const int32_t* place, uint32_t sorted_rows, unsigned char* xs)
 {
     rows_begin();
     const uint32_t in = threadIdx.x / across;
@@ -104,9 +104,9 @@ __global__ void __launch_bounds__(kThreads) dispatch_any_kernel(unsigned* status
 // binary16 elements from 117965 answers: 100 us, 6.2 TB/s, bound by HBM.
 template <typename E, int N, int KC, bool kWeights>
 __global__ void __launch_bounds__(kThreads) combine_kernel(unsigned* status, uint32_t T, uint32_t k, uint32_t cols, uint32_t across,
-                                                           uint32_t down, const E* __restrict__ z, uint32_t sorted_rows,
-                                                           const int32_t* __restrict__ place, const float* __restrict__ w,
-                                                           E* __restrict__ y, uint64_t ld_y)
+                                                           uint32_t down, const E* z, uint32_t sorted_rows,
+                                                           const int32_t* place, const float* w,
+                                                           E* y, uint64_t ld_y)
 {
     rows_begin();
     const uint32_t in = threadIdx.x / across;
@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(kThreads) combine_kernel(unsigned* status, uin
         RowsVec<E, N> v[KC];
         load_places<KC>(status, place + t * k + j0, k - j0, sorted_rows, col == 0, at);
 #pragma unroll
-        for (int j = 0; j < KC; ++j) wt[j] = kWeights && j0 + j < k ? __ldg(w + t * k + j0 + j) : 1.0f;
+        for (int j = 0; j < KC; ++j) wt[j] = kWeights ? rows_read_if(j0 + j < k, w + t * k + j0 + j, 1.0f) : 1.0f;
 #pragma unroll
         for (int j = 0; j < KC; ++j) {
             v[j].clear();
@@ -143,9 +143,9 @@ __global__ void __launch_bounds__(kThreads) combine_kernel(unsigned* status, uin
 // The same for 16-bit elements where rows start at odd places: a thread has a 16-byte word of y.
 template <typename E, int KC, bool kWeights>
 __global__ void __launch_bounds__(kThreads) combine_any_kernel(unsigned* status, uint32_t T, uint32_t k, uint32_t D, uint32_t cols, uint32_t across,
-                                                               uint32_t down, const E* __restrict__ z, uint32_t sorted_rows,
-                                                               const int32_t* __restrict__ place, const float* __restrict__ w,
-                                                               E* __restrict__ y, uint64_t ld_y)
+                                                               uint32_t down, const E* z, uint32_t sorted_rows,
+                                                               const int32_t* place, const float* w,
+                                                               E* y, uint64_t ld_y)
 {
     constexpr int S = (int)sizeof(E), N = 16 / S;
     rows_begin();
@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(kThreads) combine_any_kernel(unsigned* status,
         load_places<KC>(status, place + t * k + j0, k - j0, sorted_rows, col == 0, at);
 #pragma unroll
         for (int j = 0; j < KC; ++j) {
-            wt[j] = kWeights && j0 + j < k ? __ldg(w + t * k + j0 + j) : 1.0f;
+            wt[j] = kWeights ? rows_read_if(j0 + j < k, w + t * k + j0 + j, 1.0f) : 1.0f;
             any[j].fetch(at[j] >= 0, from + (uint64_t)(uint32_t)at[j] * row_bytes + first, from, end);
         }
 #pragma unroll
@@ -191,9 +191,9 @@ __global__ void __launch_bounds__(kThreads) combine_any_kernel(unsigned* status,
 // gradient of dispatch 269 us for 1.75 GB, 6.5 TB/s, the rate of a copy.
 template <typename E, int N, int KC>
 __global__ void __launch_bounds__(kThreads) combine_grad_kernel(unsigned* status, uint32_t T, uint32_t k, uint32_t cols, uint32_t team,
-                                                                const E* __restrict__ dy, uint64_t ld_dy, const E* __restrict__ z,
-                                                                uint32_t sorted_rows, const int32_t* __restrict__ place,
-                                                                const float* __restrict__ w, E* __restrict__ dz, float* __restrict__ dw)
+                                                                const E* dy, uint64_t ld_dy, const E* z,
+                                                                uint32_t sorted_rows, const int32_t* place,
+                                                                const float* w, E* dz, float* dw)
 {
     __shared__ float part[kThreads / 32][KC];
     rows_begin();
@@ -207,7 +207,7 @@ __global__ void __launch_bounds__(kThreads) combine_grad_kernel(unsigned* status
         load_places<KC>(status, place + (row ? t : 0) * k + j0, row ? k - j0 : 0u, sorted_rows, me == 0, at);
 #pragma unroll
         for (int j = 0; j < KC; ++j) {
-            wt[j] = row && j0 + j < k && w != nullptr ? __ldg(w + t * k + j0 + j) : 1.0f;
+            wt[j] = rows_read_if(row && j0 + j < k && w != nullptr, w + t * k + j0 + j, 1.0f);
             dot[j] = 0.0f;
         }
         for (uint32_t col = me; col < cols && row; col += team) {

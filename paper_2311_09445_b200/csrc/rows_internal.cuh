@@ -112,7 +112,21 @@ inline int rows_launch(void (*kernel)(Params...), dim3 grid, dim3 block, size_t 
 
 #ifdef __CUDACC__
 
+// Waits for the kernel before.  What a kernel reads may still be written until then, so nothing here promises that it stays as it is
+// while the kernel runs: no pointer is __restrict__ and no load goes through the read-only path, which would let it move ahead of this.
+// Operands are read by plain loads, which stay behind the "memory" here, and by `volatile` ones, which stay behind this one.
 __device__ __forceinline__ void rows_begin() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+// *p if `there`, else `otherwise`: one predicated load.
+__device__ __forceinline__ int32_t rows_read_if(bool there, const int32_t* p, int32_t otherwise)
+{
+    asm volatile("{ .reg .pred q; setp.ne.u32 q, %2, 0; @q ld.global.b32 %0, [%1]; }" : "+r"(otherwise) : "l"(p), "r"((uint32_t)there));
+    return otherwise;
+}
+__device__ __forceinline__ float rows_read_if(bool there, const float* p, float otherwise)
+{
+    return __int_as_float(rows_read_if(there, reinterpret_cast<const int32_t*>(p), __float_as_int(otherwise)));
+}
 
 // ---- elements --------------------------------------------------------------------------------------------------------
 template <typename T> struct RowsElem;
@@ -158,36 +172,30 @@ template <> struct RowsRaw<1> {
 };
 
 // Loads *p if `there`, else leaves v as it is: a predicated load, so that several of them are in flight together.  kKept: the bytes
-// may be written by this kernel (a move in place), so they do not go through the read-only path.  `volatile` keeps the loads behind
-// rows_begin, and kKept ones in front of the stores that follow them.
+// may be written by this kernel (a move in place), so the loads stay in front of the stores that follow them.
 template <bool kKept, int B>
 __device__ __forceinline__ void rows_load_if(bool there, RowsRaw<B>& v, const void* p)
 {
     if constexpr (B == 32) {
-        if constexpr (kKept)
-            asm volatile("{ .reg .pred q; setp.ne.u32 q, %9, 0; @q ld.global.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8]; }"
-                         : "+r"(v.r[0]), "+r"(v.r[1]), "+r"(v.r[2]), "+r"(v.r[3]), "+r"(v.r[4]), "+r"(v.r[5]), "+r"(v.r[6]), "+r"(v.r[7])
-                         : "l"(p), "r"((uint32_t)there) : "memory");
-        else
-            asm volatile("{ .reg .pred q; setp.ne.u32 q, %9, 0; @q ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8]; }"
-                         : "+r"(v.r[0]), "+r"(v.r[1]), "+r"(v.r[2]), "+r"(v.r[3]), "+r"(v.r[4]), "+r"(v.r[5]), "+r"(v.r[6]), "+r"(v.r[7])
-                         : "l"(p), "r"((uint32_t)there));
+        asm volatile("{ .reg .pred q; setp.ne.u32 q, %9, 0; @q ld.global.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8]; }"
+                     : "+r"(v.r[0]), "+r"(v.r[1]), "+r"(v.r[2]), "+r"(v.r[3]), "+r"(v.r[4]), "+r"(v.r[5]), "+r"(v.r[6]), "+r"(v.r[7])
+                     : "l"(p), "r"((uint32_t)there));
     } else if constexpr (B == 16) {
-        if constexpr (kKept)
-            asm volatile("{ .reg .pred q; setp.ne.u32 q, %5, 0; @q ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4]; }"
-                         : "+r"(v.r[0]), "+r"(v.r[1]), "+r"(v.r[2]), "+r"(v.r[3]) : "l"(p), "r"((uint32_t)there) : "memory");
-        else
-            asm volatile("{ .reg .pred q; setp.ne.u32 q, %5, 0; @q ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4]; }"
-                         : "+r"(v.r[0]), "+r"(v.r[1]), "+r"(v.r[2]), "+r"(v.r[3]) : "l"(p), "r"((uint32_t)there));
+        asm volatile("{ .reg .pred q; setp.ne.u32 q, %5, 0; @q ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4]; }"
+                     : "+r"(v.r[0]), "+r"(v.r[1]), "+r"(v.r[2]), "+r"(v.r[3]) : "l"(p), "r"((uint32_t)there));
     } else if constexpr (B == 8) {
-        if (there) { const uint2 a = *reinterpret_cast<const uint2*>(p); v.r[0] = a.x; v.r[1] = a.y; }
+        asm volatile("{ .reg .pred q; setp.ne.u32 q, %3, 0; @q ld.global.v2.b32 {%0, %1}, [%2]; }"
+                     : "+r"(v.r[0]), "+r"(v.r[1]) : "l"(p), "r"((uint32_t)there));
     } else if constexpr (B == 4) {
-        if (there) v.r[0] = *reinterpret_cast<const uint32_t*>(p);
+        asm volatile("{ .reg .pred q; setp.ne.u32 q, %2, 0; @q ld.global.b32 %0, [%1]; }" : "+r"(v.r[0]) : "l"(p), "r"((uint32_t)there));
     } else if constexpr (B == 2) {
-        if (there) v.r[0] = *reinterpret_cast<const uint16_t*>(p);
+        asm volatile("{ .reg .pred q; setp.ne.u32 q, %2, 0; @q ld.global.b16 %0, [%1]; }" : "+h"(v.r[0]) : "l"(p), "r"((uint32_t)there));
     } else {
-        if (there) v.r[0] = *reinterpret_cast<const uint8_t*>(p);
+        uint32_t byte = v.r[0];
+        asm volatile("{ .reg .pred q; setp.ne.u32 q, %2, 0; @q ld.global.u8 %0, [%1]; }" : "+r"(byte) : "l"(p), "r"((uint32_t)there));
+        v.r[0] = (uint8_t)byte;
     }
+    if constexpr (kKept) asm volatile("" ::: "memory");
 }
 template <int B>
 __device__ __forceinline__ void rows_store(void* p, const RowsRaw<B>& v)

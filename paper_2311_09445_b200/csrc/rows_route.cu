@@ -58,9 +58,9 @@ __device__ __forceinline__ bool load_logits(const E* row, uint32_t first, uint32
 }
 
 template <typename E, int L, int N>
-__global__ void __launch_bounds__(kThreads) rounds_kernel(unsigned* status, uint32_t T, uint32_t experts, uint32_t k, const E* __restrict__ logits,
-                                                         uint64_t ld, uint32_t wide, uint32_t over_chosen, float* __restrict__ w,
-                                                         int32_t* __restrict__ ids)
+__global__ void __launch_bounds__(kThreads) rounds_kernel(unsigned* status, uint32_t T, uint32_t experts, uint32_t k, const E* logits,
+                                                         uint64_t ld, uint32_t wide, uint32_t over_chosen, float* w,
+                                                         int32_t* ids)
 {
     rows_begin();
     const uint32_t lane = threadIdx.x % L;
@@ -284,9 +284,9 @@ __device__ __forceinline__ uint32_t from_lane(uint32_t k, int d, int width) { re
 __device__ __forceinline__ uint64_t from_lane(uint64_t k, int d, int width) { return __shfl_xor_sync(0xFFFFFFFFu, k, d, width); }
 
 template <typename E, int L, int N, int P>
-__global__ void __launch_bounds__(kRouteThreads) route_kernel(unsigned* status, uint32_t T, uint32_t experts, uint32_t k, const E* __restrict__ logits,
-                                                         uint64_t ld, uint32_t wide, uint32_t over_chosen, float* __restrict__ w,
-                                                         int32_t* __restrict__ ids, uint2 one)
+__global__ void __launch_bounds__(kRouteThreads) route_kernel(unsigned* status, uint32_t T, uint32_t experts, uint32_t k, const E* logits,
+                                                         uint64_t ld, uint32_t wide, uint32_t over_chosen, float* w,
+                                                         int32_t* ids, uint2 one)
 {
     typedef Key<E> Q;
     typedef typename Q::type K;
@@ -404,9 +404,9 @@ __device__ __forceinline__ bool load_block(const E* x, uint32_t c, uint32_t expe
 constexpr uint32_t kRowFloats = 1024;                // of shared memory per warp at most: R rows of the experts, rounded up to 4; so 32 a lane
 template <typename E, int M, bool kChosen, int H>
 __global__ void __launch_bounds__(kThreads) route_grad_kernel(unsigned* status, uint32_t T, uint32_t experts, uint32_t k, uint32_t log_kl,
-                                                              uint32_t log_r, const E* __restrict__ logits, uint64_t ld,
-                                                              const float* __restrict__ w, const int32_t* __restrict__ ids,
-                                                              const float* __restrict__ dw, E* __restrict__ dlogits, uint64_t ld_d)
+                                                              uint32_t log_r, const E* logits, uint64_t ld,
+                                                              const float* w, const int32_t* ids,
+                                                              const float* dw, E* dlogits, uint64_t ld_d)
 {
     constexpr int B = 16 / (int)sizeof(E);
     extern __shared__ __align__(16) float shared[];
@@ -425,9 +425,9 @@ __global__ void __launch_bounds__(kThreads) route_grad_kernel(unsigned* status, 
         const uint64_t t = ((uint64_t)group << log_r) + r;
         const bool slot = group < groups && r < rows && t < T && j < k;
         const uint64_t at = t * k + j;
-        next_id = slot ? __ldg(ids + at) : -1;
-        next_weight = slot ? __ldg(w + at) : 0.0f;
-        next_d = slot ? __ldg(dw + at) : 0.0f;
+        next_id = rows_read_if(slot, ids + at, -1);
+        next_weight = rows_read_if(slot, w + at, 0.0f);
+        next_d = rows_read_if(slot, dw + at, 0.0f);
     };
     uint32_t group = blockIdx.x * (kThreads / 32) + warp;
     fetch(group);

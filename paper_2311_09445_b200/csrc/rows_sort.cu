@@ -27,8 +27,8 @@ constexpr int kHeld = 8;                 // groups of 32 slots whose ranks a lan
 // expert), start[E], sums[32], and unless kLong local[E] and staged[slots of a CTA]: a CTA's slots are sorted there first, so that what
 // goes to `order` is runs of an expert's slots and not single words (a warp's store to 32 places takes the SM 32 cycles).
 template <bool kLong>
-__global__ void __launch_bounds__(kMostThreads) sort_kernel(unsigned* status, uint32_t slots, uint32_t E, const int32_t* __restrict__ ids,
-                                                            int32_t* __restrict__ offsets, int32_t* __restrict__ order, int32_t* place)
+__global__ void __launch_bounds__(kMostThreads) sort_kernel(unsigned* status, uint32_t slots, uint32_t E, const int32_t* ids,
+                                                            int32_t* offsets, int32_t* order, int32_t* place)
 {
     extern __shared__ uint32_t shared[];
     cg::cluster_group cluster = cg::this_cluster();
@@ -55,7 +55,7 @@ __global__ void __launch_bounds__(kMostThreads) sort_kernel(unsigned* status, ui
 #pragma unroll
         for (int q = 0; q < kHeld; ++q) {
             const uint32_t s = s0 + q * 32 + lane;
-            e[q] = s < end ? __ldg(ids + s) : -1;
+            e[q] = rows_read_if(s < end, ids + s, -1);
         }
 #pragma unroll
         for (int q = 0; q < kHeld; ++q) {
@@ -206,7 +206,7 @@ __global__ void __launch_bounds__(kMostThreads) sort_kernel(unsigned* status, ui
         for (int q = 0; q < kHeld; ++q) {
             const uint32_t s = s0 + q * 32 + lane;
             rank[q] = s < end ? (uint32_t)place[s] : 0xFFFFFFFFu;
-            e[q] = s < end ? __ldg(ids + s) : -1;
+            e[q] = rows_read_if(s < end, ids + s, -1);
             if ((uint32_t)e[q] >= E) e[q] = -1;
         }
 #pragma unroll

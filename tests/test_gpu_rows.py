@@ -831,3 +831,39 @@ def test_other_device_than_the_current_one():
     assert r.sync() == 0 and torch.cuda.current_device() == 0
     assert all((a.cpu().numpy() == b).all() for a, b in zip(o, ref.sort(ids.numpy(), 5)))
     r.close()
+
+
+@pytest.mark.parametrize("B", [64, 1000])
+def test_rows_right_behind_a_sample(rows, B):
+    """The buffer's kernels let the next kernel of the stream start early; what they gather, and the indices and weights that they draw, are
+    operands here with nothing in between.  Every pass draws others, so a row, a place or a weight read too early is one of the pass before."""
+    from paper_2311_09445_b200 import PrioritizedReplay
+    N, D, E = 2048, 17, 5
+    g = gen(76)
+    prb = PrioritizedReplay(N, 16, 4 * D, 4, 1024)
+    obs = torch.randn(N, D, generator=g).cuda()
+    for part in obs.split(512):
+        prb.insert(part.view(torch.uint8), torch.zeros(512, 4, dtype=torch.uint8, device="cuda"), torch.zeros(512, device="cuda"),
+                   part.view(torch.uint8), torch.zeros(512, dtype=torch.uint8, device="cuda"), torch.rand(512, generator=g).cuda() + 0.1)
+    idx, isw, x = torch.zeros(B, 1, dtype=torch.int32, device="cuda"), torch.zeros(B, 1, device="cuda"), torch.zeros(B, D, device="cuda")
+    place = torch.randperm(B, generator=g).to(torch.int32).view(B, 1).cuda()
+    xs, y, w, ids = torch.zeros(B, D, device="cuda"), torch.zeros(B, D, device="cuda"), torch.zeros(B, E, device="cuda"), torch.zeros(B, E, dtype=torch.int32, device="cuda")
+    seed = 0
+
+    def draw():
+        nonlocal seed
+        seed += 1
+        prb.sample(B, 0.4, seed, idx.view(-1), isw.view(-1), x.view(torch.uint8))
+
+    for _ in range(25):
+        draw()
+        rows.dispatch(x, place, xs)
+        assert torch.equal(x, obs[idx.view(-1).long()]) and torch.equal(xs[place.view(-1).long()], x)
+        draw()
+        rows.combine(obs, idx, isw, y)
+        assert torch.equal(y, isw * obs[idx.view(-1).long()])
+        draw()
+        rows.route(x, w, ids, over_chosen=True)
+        assert torch.equal(ids.long(), x.topk(E, dim=1).indices)
+    assert rows.sync() == 0 and prb.sync() == 0
+    prb.close()
