@@ -582,12 +582,20 @@ __device__ __forceinline__ void send(uint32_t to, uint32_t barrier, uint32_t ran
     asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.b64 [%0], {%1, %2}, [%3];"
                  ::"r"(in_cta(to, rank)), "l"((uint64_t)__double_as_longlong(s.sum)), "l"(ref_offers), "r"(in_cta(barrier, rank)) : "memory");
 }
-// Waits until all of them are here; the barrier's one phase.  Every CTA of the cluster sends a fixed number of bytes, so this
-// ends; should it not, the limit ends it (PEARL_ST_INTERNAL, the group's results are missing).
+// Waits until all of them are here, for `polls` looks at most; the barrier's one phase.  Every CTA of the cluster sends a fixed number of
+// bytes, so this ends; but a CTA whose rows have to be searched again and again may be far behind, and a CTA that left before its
+// lists are here would leave them without a place to go.  So after kPolls looks the cluster's barrier is waited for, at which a CTA
+// arrives once it has sent everything.  (Checked build: at once, so that this way is taken.)  Should they not be here then, PEARL_ST_INTERNAL
+// tells of it, and the group's results are missing.
+#ifdef PEARL_CHECKED
+constexpr uint32_t kPolls = 0;
+#else
 constexpr uint32_t kPolls = 1u << 22;
-__device__ __forceinline__ bool arrived(uint32_t barrier)
+#endif
+constexpr uint32_t kLastPolls = 1u << 22;
+__device__ __forceinline__ bool arrived(uint32_t barrier, uint32_t polls)
 {
-    for (uint32_t i = 0; i < kPolls; ++i) {
+    for (uint32_t i = 0; i < polls; ++i) {
         uint32_t ok;
         asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], 0; selp.u32 %0, 1, 0, p; }"
                      : "=r"(ok) : "r"(barrier) : "memory");
@@ -595,6 +603,10 @@ __device__ __forceinline__ bool arrived(uint32_t barrier)
     }
     return false;
 }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+// (without an order on memory: what has been sent is counted by the receiver's barrier)
+__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 // The entries of a falling list of n that are larger than `bar`; `top` is the largest power of two up to n.
 __device__ __forceinline__ uint32_t larger_than(const uint64_t* list, uint32_t n, uint32_t top, uint64_t bar)
@@ -655,7 +667,7 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const SelectArgs a)
         n_all = 0;
     }
     __syncwarp();
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    cluster_arrive();
     rows_begin();
 
     const E* all = reinterpret_cast<const E*>(a.logits);
@@ -682,7 +694,7 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const SelectArgs a)
                 score_of[tid] = score;
             }
             __syncwarp();
-            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");      // the others' barriers may be used from here on
+            cluster_wait();                                                           // the others' barriers may be used from here on
             __syncthreads();
         }
         if (u >= units) {
@@ -819,8 +831,14 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const SelectArgs a)
         }
         if (q + 1 < a.units_per_cta) __syncthreads();                      // (the next unit uses the same workspace)
     }
-    if (!arrived(bar)) atomicOr(a.status, PEARL_ST_INTERNAL);
-    __syncthreads();
+    __syncwarp();
+    cluster_arrive_relaxed();                                              // (this CTA has sent everything)
+    const bool late = __syncthreads_or(!arrived(bar, kPolls)) != 0;
+    if (late) {
+        cluster_wait();
+        if (!arrived(bar, kLastPolls)) atomicOr(a.status, PEARL_ST_INTERNAL);
+        __syncthreads();
+    }
 
     if (tid < a.W) {
         float ref = kLowest;
@@ -880,6 +898,8 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const SelectArgs a)
             a.best_beam[to] = -1;
             a.best_token[to] = -1;
         }
+    __syncwarp();
+    if (!late) cluster_wait();                                             // (long past, where all lists are here)
 }
 
 // ---- the states ------------------------------------------------------------------------------------------------------

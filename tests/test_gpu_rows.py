@@ -867,3 +867,21 @@ def test_rows_right_behind_a_sample(rows, B):
         assert torch.equal(ids.long(), x.topk(E, dim=1).indices)
     assert rows.sync() == 0 and prb.sync() == 0
     prb.close()
+
+
+def test_beam_select_waits_for_rows_that_are_searched_long(rows):
+    """Rows of one value, but for a thread's share, whose bound has to be searched over nearly all logits, in one CTA of a group
+    whose other CTAs have finished beams alone and nothing to do but wait."""
+    W, V, C = 32, 1 << 22, 64
+    logits = torch.zeros(1, W, V, dtype=torch.bfloat16, device="cuda")
+    share = logits.view(W, V // 2048, 256, 8)[:4, :-1, 255]                 # the 16-byte accesses of the last of 256 threads, but for its last one
+    share.fill_(-1.0)
+    scores, done = torch.zeros(1, W), torch.ones(1, W, dtype=torch.uint8)
+    scores[0, 4:] = -math.inf
+    done[0, :4] = 0
+    score, beam, token = run_select(rows, logits, scores, C, done=done)
+    lower = int((logits[0, 0] < 0).sum())
+    lse = math.log(V - lower + lower * math.exp(-1.0))
+    assert (beam[0] == 0).all() and token[0].tolist() == list(range(C))       # four equal beams: the lowest one's lowest tokens
+    assert np.abs(score[0] + lse).max() <= 25 * U + 2.0 ** -26 + lse * U
+    assert rows.sync() == 0

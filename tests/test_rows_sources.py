@@ -28,3 +28,14 @@ def test_no_load_may_move_ahead_of_the_wait_for_the_kernel_before(path):
 def test_every_kernel_waits_for_the_one_before(path):
     bodies = re.split(r"__global__", code(path))[1:]
     assert bodies and all("rows_begin();" in body for body in bodies)
+
+
+def test_no_cta_leaves_its_cluster_before_all_have_sent():
+    """Beam selection's CTAs send lists into one another's shared memory.  A CTA that gives up waiting for them, or has them all, waits at
+    the cluster's barrier, at which the others arrive when they have sent theirs, before it leaves."""
+    text = code(os.path.join(ROOT, "paper_2311_09445_b200", "csrc", "rows_beam.cu"))
+    kernel = text[text.index("select_kernel(const SelectArgs a)"):text.index("struct ReorderArgs")]
+    behind = kernel[kernel.index("cluster_arrive_relaxed();"):]
+    assert "send(" not in behind
+    assert re.search(r"if \(late\) \{\s*cluster_wait\(\);\s*if \(!arrived\(", behind)
+    assert re.search(r"if \(!late\) cluster_wait\(\);\s*\}\s*$", behind)
