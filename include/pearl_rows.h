@@ -17,8 +17,9 @@
  *     captured into a CUDA graph; graphs of one handle may be replayed side by side (they share the status word, which
  *     only collects bits).
  *   - Outputs must not overlap inputs or each other, except where a call says so.
- *   - `dtype` names the element type of logits and rows; sums, softmax statistics, weights and scores are binary32 or
- *     wider, each result is rounded once.
+ *   - `dtype` names the element type of logits and rows.  Sums, softmax statistics, weights and scores are computed in
+ *     binary32 or wider, the router's exponentials within 2 units of the last place; what is handed out in a narrower type is
+ *     rounded to it once.
  *   - Rows of a matrix may lie apart (the ld_* arguments, in elements, at least the row's length); the elements of
  *     a row are consecutive.  The bytes between rows are never written; up to 16 of them beside a row may be read.
  *     Pointers must be aligned to their element size, else PEARL_ERR_ALIGN.  Rows whose start and length are multiples of

@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(kThreads) rounds_kernel(unsigned* status, uint
     float sum = 0.0f;
     if (!over_chosen) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) sum = __fadd_rn(sum, __expf(__fsub_rn(x[i], shift)));
+        for (int i = 0; i < N; ++i) sum = __fadd_rn(sum, expf(__fsub_rn(x[i], shift)));
         sum = over_lanes_sum<L>(sum);
     }
     // choice j is kept by lane j % L of the row, in held[j / L]
@@ -109,7 +109,7 @@ __global__ void __launch_bounds__(kThreads) rounds_kernel(unsigned* status, uint
             at = __shfl_sync(0xFFFFFFFFu, at, (int)owner, L);
             const bool shut = gmax == -kInf;
             if (lane == j - h * L) { held_x[h] = gmax; held_id[h] = shut ? -1 : at; }
-            chosen_sum = __fadd_rn(chosen_sum, __expf(__fsub_rn(gmax, shift)));
+            chosen_sum = __fadd_rn(chosen_sum, expf(__fsub_rn(gmax, shift)));
             gmax = over_lanes_max<L>(best);
         }
     }
@@ -120,7 +120,7 @@ __global__ void __launch_bounds__(kThreads) rounds_kernel(unsigned* status, uint
         const uint32_t j = h * L + lane;
         if (j < k) {
             ids[t * k + j] = held_id[h];
-            w[t * k + j] = held_id[h] < 0 ? 0.0f : __fdiv_rn(__expf(__fsub_rn(held_x[h], shift)), denominator);
+            w[t * k + j] = held_id[h] < 0 ? 0.0f : __fdiv_rn(expf(__fsub_rn(held_x[h], shift)), denominator);
         }
     }
 }
@@ -353,22 +353,21 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(unsigned* status, 
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
         if (lane * kEach + i >= k || Q::rising(mine[i]) <= Q::kNothing) mine[i] = 0;
-        e[i] = mine[i] ? __expf(__fsub_rn(Q::logit(mine[i]), shift)) : 0.0f;
+        e[i] = mine[i] ? expf(__fsub_rn(Q::logit(mine[i]), shift)) : 0.0f;
         if (over_chosen) sum = __fadd_rn(sum, e[i]);
     }
     if (!over_chosen) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) sum = __fadd_rn(sum, __expf(__fsub_rn(Q::value(x, i), shift)));
+        for (int i = 0; i < N; ++i) sum = __fadd_rn(sum, expf(__fsub_rn(Q::value(x, i), shift)));
     }
     sum = over_lanes_sum<L>(sum);
     if (t >= T) return;
-    const float scale = sum > 0.0f ? __fdiv_rn(1.0f, sum) : 0.0f;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
         const uint32_t j = lane * kEach + i;
         if (j < k) {
             ids[t * k + j] = mine[i] ? (int32_t)(0xFFFFu - (uint32_t)(mine[i] & 0xFFFFu)) : -1;
-            w[t * k + j] = __fmul_rn(e[i], scale);
+            w[t * k + j] = mine[i] ? __fdiv_rn(e[i], sum) : 0.0f;
         }
     }
 }
@@ -490,10 +489,11 @@ __global__ void __launch_bounds__(kThreads) route_grad_kernel(unsigned* status, 
             for (int n = 0; n < H / B; ++n)
 #pragma unroll
                 for (int i = 0; i < B; ++i) {
-                    held[n][i] = __expf(__fsub_rn(held[n][i], shift));
+                    held[n][i] = expf(__fsub_rn(held[n][i], shift));
                     sum = __fadd_rn(sum, held[n][i]);
                 }
             for (uint32_t q = 1; q < 1u << log_lr; q *= 2) sum = __fadd_rn(sum, __shfl_xor_sync(0xFFFFFFFFu, sum, q));
+            // (a product with the rounded reciprocal instead of a division a logit: one half step of binary32 more)
             const float p_scale = sum > 0.0f ? __fdiv_rn(1.0f, sum) : 0.0f;
 #pragma unroll
             for (int n = 0; n < H / B; ++n)

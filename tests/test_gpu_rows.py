@@ -885,3 +885,38 @@ def test_beam_select_waits_for_rows_that_are_searched_long(rows):
     assert (beam[0] == 0).all() and token[0].tolist() == list(range(C))       # four equal beams: the lowest one's lowest tokens
     assert np.abs(score[0] + lse).max() <= 25 * U + 2.0 ** -26 + lse * U
     assert rows.sync() == 0
+
+
+@pytest.mark.parametrize("kind", ["fp32", "fp16", "bf16"])
+@pytest.mark.parametrize("E,k", [(8, 8), (64, 6), (128, 8), (500, 8), (60, 20), (1024, 32)])
+def test_route_small_weights_keep_their_digits(rows, kind, E, k):
+    """One logit far above the others: a row's sum is 1, and a weight is the exponential itself, of a difference that is exact."""
+    far = torch.randint(0, 33, (70, E), generator=gen(77, E)).double() / 4            # 27 to 35 below the largest
+    l = -23.0 - far
+    l[torch.arange(70), torch.randint(0, E, (70,), generator=gen(78, E))] = 4.0
+    logits = l.to(TYPES[kind])
+    assert torch.equal(logits.double(), l)
+    for chosen in (False, True):
+        w, ids = run_route(rows, logits.cuda(), k, chosen)
+        want_w, want_ids = ref.route(l.numpy(), k, chosen)
+        assert (ids.cpu().numpy() == want_ids).all()
+        # expf is within 2 units of the last place, 2 * 2^-23 of the value at most: 4 half steps; the sum is 1 + E e^-27 (2^-28); the division 1
+        np.testing.assert_allclose(f64(w), want_w, rtol=5.1 * U, atol=0)
+
+
+@pytest.mark.parametrize("E,k", [(8, 2), (64, 6), (128, 8), (129, 3), (500, 8), (1024, 32)])
+def test_route_grad_small_parts_keep_their_digits(rows, E, k):
+    """The same rows with dw = 1 for the first choice, whose weight is 1: the gradient of every other expert is -p, its exponential."""
+    l = -23.0 - torch.randint(0, 33, (70, E), generator=gen(79, E)).float() / 4
+    top = torch.randint(0, E, (70,), generator=gen(80, E))
+    l[torch.arange(70), top] = 4.0
+    w, ids = run_route(rows, l.cuda(), k, False)
+    dw = torch.zeros(70, k)
+    dw[:, 0] = 1.0
+    d = torch.zeros(70, E, device="cuda")
+    rows.route_grad(l.cuda(), w, ids, dw.cuda(), d)
+    p = torch.softmax(l.double(), 1).numpy()
+    others = np.ones((70, E), bool)
+    others[np.arange(70), top.numpy()] = False
+    # expf 4 half steps, the sum (1) and its reciprocal and the first weight 1 each, two products 1 each
+    np.testing.assert_allclose(f64(d)[others], -p[others], rtol=8.1 * U, atol=0)
