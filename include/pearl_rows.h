@@ -143,9 +143,10 @@ int pearl_rows_beam_reorder(pearl_rows_t* rows, uint32_t blocks, uint32_t G, uin
                             const int32_t* d_parent, const void* d_src, const pearl_states_t* src, void* d_dst,
                             const pearl_states_t* dst);
 
-/* Waits for the stream; returns the accumulated PEARL_ST_* bits in *status_bits (may be NULL) and clears them. */
+/* Waits for the handle's stream; returns the accumulated PEARL_ST_* bits in *status_bits (may be NULL) and clears them.  A bit that
+ * a graph on another stream raises meanwhile is in this answer or in the next one. */
 int pearl_rows_sync(pearl_rows_t* rows, uint32_t* status_bits);
-/* Number of kernels this handle has launched so far. */
+/* Number of kernels this handle has launched so far (among them the one that clears the bits, where sync found any). */
 uint64_t pearl_rows_kernel_launches(pearl_rows_t* rows);
 
 #ifdef __cplusplus

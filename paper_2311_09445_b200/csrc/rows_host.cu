@@ -5,7 +5,7 @@
 #include "rows_internal.cuh"
 
 struct pearl_rows {
-    unsigned* status;
+    unsigned* status;           // two words: the status bits, and those that pearl_rows_sync() has taken
     bool owns_slab;
     int device;
     cudaStream_t stream;
@@ -15,6 +15,13 @@ struct pearl_rows {
 namespace {
 
 constexpr uint64_t kSlabBytes = 256;
+
+// The bits so far, and none from here on, in one step: one that another stream raises meanwhile is among them or stays.
+__global__ void take_status_kernel(unsigned* status)
+{
+    rows_begin();
+    status[1] = atomicExch(status, 0u);
+}
 
 // Makes `dev` the current device for a call; the device that was current is so again afterwards.
 struct DeviceGuard {
@@ -246,10 +253,16 @@ int pearl_rows_sync(pearl_rows_t* h, uint32_t* status_bits)
     DeviceGuard guard(h->device);
     if (!guard.ok) return PEARL_ERR_CUDA;
     uint32_t st = 0;
-    if (cudaMemcpyAsync(&st, h->status, 4, cudaMemcpyDeviceToHost, h->stream) != cudaSuccess ||
-        cudaStreamSynchronize(h->stream) != cudaSuccess)
-        return PEARL_ERR_CUDA;
-    if (st && (cudaMemsetAsync(h->status, 0, 4, h->stream) != cudaSuccess || cudaStreamSynchronize(h->stream) != cudaSuccess)) return PEARL_ERR_CUDA;
+    const auto read = [&](const unsigned* word) {
+        return cudaMemcpyAsync(&st, word, 4, cudaMemcpyDeviceToHost, h->stream) == cudaSuccess && cudaStreamSynchronize(h->stream) == cudaSuccess;
+    };
+    if (!read(h->status)) return PEARL_ERR_CUDA;
+    if (st) {
+        const int n = rows_launch(take_status_kernel, dim3(1), dim3(1), 0, h->stream, 0, h->status);
+        if (n < 0) { cudaGetLastError(); return PEARL_ERR_CUDA; }
+        h->launches += (uint64_t)n;
+        if (!read(h->status + 1)) return PEARL_ERR_CUDA;
+    }
     if (status_bits) *status_bits = st;
     return PEARL_OK;
 }

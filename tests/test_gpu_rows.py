@@ -920,3 +920,34 @@ def test_route_grad_small_parts_keep_their_digits(rows, E, k):
     others[np.arange(70), top.numpy()] = False
     # expf 4 half steps, the sum (1) and its reciprocal and the first weight 1 each, two products 1 each
     np.testing.assert_allclose(f64(d)[others], -p[others], rtol=8.1 * U, atol=0)
+
+
+def test_no_status_bit_is_lost_between_streams():
+    """A graph of the handle, replayed on another stream, raises its bit at any moment of sync(): this answer or the next one has it."""
+    from paper_2311_09445_b200 import RowRouter
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    with torch.cuda.stream(a):
+        r = RowRouter(stream=a)
+        logits = torch.full((1, 4), math.nan, device="cuda")
+        w, ids = torch.zeros(1, 1, device="cuda"), torch.zeros(1, 1, dtype=torch.int32, device="cuda")
+        bad, offsets, place = torch.full((1,), 9, dtype=torch.int32, device="cuda"), torch.zeros(5, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+        r.route(logits, w, ids)
+        r.sort(bad, 4, offsets, None, place)
+        assert r.sync() == BAD_SCORE | BAD_INDEX
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=a):
+            r.route(logits, w, ids)
+    assert r.sync() == 0
+    for delay in range(0, 120000, 400):                     # (cycles: from before the copy of the word to behind its clearing)
+        with torch.cuda.stream(b):
+            torch.cuda._sleep(delay)
+            graph.replay()
+        r.sort(bad, 4, offsets, None, place)
+        first = r.sync()
+        b.synchronize()
+        second = r.sync()
+        assert first & BAD_INDEX and not second & BAD_INDEX
+        assert (first | second) == BAD_SCORE | BAD_INDEX, delay
+        assert r.sync() == 0
+    graph.reset()
+    r.close()
