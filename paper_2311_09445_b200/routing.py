@@ -58,6 +58,12 @@ def load_library():
     return _lib
 
 
+def _room(counts: int) -> None:
+    """counts: sizes that go to the library as 32-bit numbers, OR'ed together.  ctypes would hand on the low bits of a larger one."""
+    if counts >> 32:
+        raise ValueError("a size is negative or above 2^32 - 1")
+
+
 def _pieces(shape, stride):
     """A state's axes (those from the fourth on) as (pieces, elements of a piece, distance of pieces)."""
     width, i = 1, len(shape)
@@ -98,6 +104,7 @@ def _move(shape, stride, stride_out, size):
             pitch_out = width
         else:
             raise ValueError("states and out must be cut into the same pieces")
+    _room(shape[0] | shape[1] | shape[2] | pieces)
     src, dst = (_States(block * size, state * size, p * size) for (block, state), p in
                 ((_distances(shape, stride), pitch), (_distances(shape, stride_out), pitch_out)))
     return pieces, width * size, C.byref(src), C.byref(dst)
@@ -147,6 +154,7 @@ class RowRouter:
         if t.dim() != 2 or t.get_device() != self._ordinal:
             raise ValueError("%s must be a 2-D tensor on %s with contiguous rows" % (what, self.device))
         rows, cols = t.shape
+        _room(rows | cols)
         if t.is_contiguous():
             return t.data_ptr(), rows, cols, cols
         ld, step = t.stride()
@@ -171,6 +179,7 @@ class RowRouter:
         if ids.dim() != 2 or ids.shape[0] != T:
             raise ValueError("ids must be [%d, k]" % T)
         k = ids.shape[1]
+        _room(k)
         rc = self._lib.pearl_rows_route(self._h, T, E, k, self._type(logits, "logits"), p, ld, 1 if over_chosen else 0,
                                         self._dense(w, "w", _F32, T * k), self._dense(ids, "ids", _I32, T * k))
         if rc != 0:
@@ -186,6 +195,7 @@ class RowRouter:
                 raise ValueError("logits and dlogits must have one shape and type")
         if ids.dim() != 2 or ids.shape[0] != T:
             raise ValueError("ids must be [%d, k]" % T)
+        _room(ids.shape[1])
         n = T * ids.shape[1]
         rc = self._lib.pearl_rows_route_grad(self._h, T, E, ids.shape[1], self._type(dlogits, "dlogits"), p, ld,
                                              1 if over_chosen else 0, self._dense(w, "w", _F32, n),
@@ -196,6 +206,7 @@ class RowRouter:
     def sort(self, ids, experts: int, offsets, order, place) -> None:
         """ids (any shape, int32) -> offsets [experts + 1], order and place (as many as ids; order may be None)."""
         n = ids.numel()
+        _room(n | experts)
         rc = self._lib.pearl_rows_sort(self._h, n, experts, self._dense(ids, "ids", _I32, n),
                                        self._dense(offsets, "offsets", _I32, experts + 1),
                                        None if order is None else self._dense(order, "order", _I32, n),
@@ -208,11 +219,13 @@ class RowRouter:
         if (t.dim() != 2 or t.shape[1] != width or t.dtype is not like.dtype or not t.is_contiguous() or
                 t.get_device() != self._ordinal):
             raise ValueError("%s must be a contiguous [rows, %d] tensor on %s of the type of %s" % (what, width, self.device, name))
+        _room(t.shape[0])
         return t.data_ptr(), t.shape[0]
 
     def _place(self, place: torch.Tensor, T: int):
         if place.dim() != 2 or place.shape[0] != T:
             raise ValueError("place must be [%d, k]" % T)
+        _room(place.shape[1])
         return self._dense(place, "place", _I32, place.numel()), place.shape[1]
 
     def dispatch(self, x, place, xs) -> None:
@@ -221,6 +234,7 @@ class RowRouter:
         at, k = self._place(place, T)
         to, rows = self._sorted(xs, "xs", width, x, "x")
         size = x.element_size()
+        _room(width * size)
         rc = self._lib.pearl_rows_dispatch(self._h, T, k, width * size, p, ld * size, at, rows, to)
         if rc != 0:
             raise PearlError(rc, "pearl_rows_dispatch")
@@ -269,6 +283,9 @@ class RowRouter:
         if best_token.dim() != 2 or best_token.shape[0] != G:
             raise ValueError("best_token must be [%d, C]" % G)
         best = best_token.shape[1]
+        _room(G | W | V | best)
+        if not -(1 << 31) <= end_token < 1 << 31:
+            raise ValueError("end_token must be a 32-bit number")
         if done is not None and done.dtype is torch.bool:
             done = done.view(torch.uint8)
         rc = self._lib.pearl_rows_beam_select(self._h, G, W, V, best, self._type(logits, "logits"), logits.data_ptr(), ld,
