@@ -147,16 +147,29 @@ template <> struct Word<__nv_bfloat16> {
 // what a thread adds up does not depend on where a row lies in memory.  Where the start is `off` bytes past a boundary, an
 // access is the two 16-byte words that hold it, shifted together; those may hold logits of the rows beside this one, and stay
 // within [the first row's start, the last row's end): an access that would leave that is read logit by logit.
+// What the checked build knows of the array that a run is in.
+struct Extent {
+#ifdef PEARL_CHECKED
+    const void *lo, *hi;
+    unsigned* status;
+    __device__ __forceinline__ bool holds(const void* p, uint32_t bytes) const { return ROWS_IN_ARRAY(status, p, bytes, lo, hi); }
+    __device__ __forceinline__ void know(const void* from, const void* to, unsigned* word) { lo = from; hi = to; status = word; }
+#else
+    __device__ __forceinline__ bool holds(const void*, uint32_t) const { return true; }
+    __device__ __forceinline__ void know(const void*, const void*, unsigned*) {}
+#endif
+};
 template <typename E>
-struct Run {
+struct Run : Extent {
     static constexpr int N = 16 / (int)sizeof(E);
     const E* run;
     uint32_t n, off;
     uint32_t accesses, full;        // ceil and floor of n / N
     uint32_t from, upto;            // accesses from .. upto - 1 may be read as 16-byte words
 
-    __device__ __forceinline__ Run(const E* start, uint32_t count, const E* all, const E* all_end) : run(start), n(count)
+    __device__ __forceinline__ Run(const E* start, uint32_t count, const E* all, const E* all_end, unsigned* status) : run(start), n(count)
     {
+        know(all, all_end, status);
         off = (uint32_t)((uintptr_t)start & 15u);
         accesses = (n + N - 1) / N;
         full = n / N;
@@ -195,7 +208,7 @@ struct Run {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             if ((uint32_t)i >= past) Word<E>::set(w.r, i, Word<E>::kMinusInf);
-            else if (!there) Word<E>::set(w.r, i, Word<E>::bits_of(run + (uint64_t)v * N + i));
+            else if (!there && holds(run + (uint64_t)v * N + i, sizeof(E))) Word<E>::set(w.r, i, Word<E>::bits_of(run + (uint64_t)v * N + i));
         }
     }
     __device__ __forceinline__ bool whole(uint32_t v) const { return readable(v) && v < full; }
@@ -340,8 +353,9 @@ template <typename E> __device__ __forceinline__ void take(Stats& s, RowsRaw<16>
     add(s, top, sum, p);
 }
 
-__device__ __forceinline__ void copy_16(uint32_t to, const unsigned char* from)
+__device__ __forceinline__ void copy_16(const Extent& in, uint32_t to, const unsigned char* from)
 {
+    if (!in.holds(from, 16)) return;
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
 __device__ __forceinline__ RowsRaw<16> ring_word(uint32_t at)
@@ -360,9 +374,9 @@ __device__ __noinline__ double far_sum(const Run<E> r, float best)
 #pragma unroll 1
     for (uint32_t v = threadIdx.x; v < r.accesses; v += kThreads) {
         RowsRaw<16> w, hi;
-        rows_load_if<false>(r.readable(v), w, r.words(v));
+        rows_load_if<false>(r.readable(v) && r.holds(r.words(v), r.off ? 32 : 16), w, r.words(v));
         if (r.off) {
-            rows_load_if<false>(r.readable(v), hi, r.words(v) + 16);
+            rows_load_if<false>(r.readable(v) && r.holds(r.words(v), 32), hi, r.words(v) + 16);
             Run<E>::shift(r.off, w, hi);
         }
         if (!r.whole(v)) r.mend(v, w);
@@ -388,8 +402,8 @@ struct Stream {
 #pragma unroll
         for (uint32_t i = 0; i < 2; ++i) {
             if (both || r.readable(threadIdx.x + (2 * p + i) * kThreads)) {
-                copy_16(slot + i * kStep, at + i * kThreads * 16u);
-                if (kShifted) copy_16(slot + i * kStep + kThreads * 16u, at + i * kThreads * 16u + 16);
+                copy_16(r, slot + i * kStep, at + i * kThreads * 16u);
+                if (kShifted) copy_16(r, slot + i * kStep + kThreads * 16u, at + i * kThreads * 16u + 16);
             }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
@@ -423,7 +437,7 @@ struct Stream {
     }
     // Pairs from p on, all whole, up to `end` or to one that take() has to look at for a lane of the warp; p becomes the next pair.
     // (Accesses first .. first + span - 1 may be read as 16-byte words.)
-    static __device__ __forceinline__ Stats whole_pairs(const unsigned char* at, uint32_t off, uint32_t first, uint32_t span, uint32_t ring, uint32_t& p,
+    static __device__ __forceinline__ Stats whole_pairs(const Extent in, const unsigned char* at, uint32_t off, uint32_t first, uint32_t span, uint32_t ring, uint32_t& p,
                                                         uint32_t end, Stats s)
     {
         const uint32_t last = ring + (kDepth - 1) * 2 * kStep;
@@ -439,8 +453,8 @@ struct Stream {
 #pragma unroll
             for (uint32_t i = 0; i < 2; ++i)                               // (into the slots that have just been read)
                 if (v + i * kThreads < span) {
-                    copy_16(slot + i * kStep, at + i * kThreads * 16u);
-                    if (kShifted) copy_16(slot + i * kStep + kThreads * 16u, at + i * kThreads * 16u + 16);
+                    copy_16(in, slot + i * kStep, at + i * kThreads * 16u);
+                    if (kShifted) copy_16(in, slot + i * kStep + kThreads * 16u, at + i * kThreads * 16u + 16);
                 }
             asm volatile("cp.async.commit_group;" ::: "memory");
             v += 2 * kThreads;
@@ -467,10 +481,10 @@ struct Stream {
         }
         return s;
     }
-    static __device__ __noinline__ Stats whole_call(const unsigned char* at, uint32_t off, uint32_t first, uint32_t span, uint32_t ring, uint32_t& p,
+    static __device__ __noinline__ Stats whole_call(const Extent in, const unsigned char* at, uint32_t off, uint32_t first, uint32_t span, uint32_t ring, uint32_t& p,
                                                     uint32_t end, Stats s)
     {
-        return whole_pairs(at, off, first, span, ring, p, end, s);
+        return whole_pairs(in, at, off, first, span, ring, p, end, s);
     }
     static __device__ __noinline__ Stats any_call(const Run<E> r, uint32_t ring, uint32_t p, uint32_t end, Stats s) { return any_pairs(r, ring, p, end, s); }
 
@@ -484,8 +498,8 @@ struct Stream {
 #pragma unroll 1
         while (p < all) {
             if (p >= first && p + kLeast <= whole) {
-                if constexpr (kCalls) s = whole_call(r.words(threadIdx.x), r.off, first, r.upto - first, ring, p, whole, s);
-                else s = whole_pairs(r.words(threadIdx.x), r.off, first, r.upto - first, ring, p, whole, s);
+                if constexpr (kCalls) s = whole_call(r, r.words(threadIdx.x), r.off, first, r.upto - first, ring, p, whole, s);
+                else s = whole_pairs(r, r.words(threadIdx.x), r.off, first, r.upto - first, ring, p, whole, s);
             }
             if (p >= all) break;
             const uint32_t to = p + kLeast <= whole ? p + 1 : all;
@@ -524,8 +538,10 @@ __device__ __noinline__ void collect(const Run<E> r, uint32_t access, uint64_t a
     RowsRaw<16> w[2], hi[2];
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
-        rows_load_if<false>(r.readable(access + m * kThreads), w[m], r.words(access + m * kThreads));
-        if (r.off) rows_load_if<false>(r.readable(access + m * kThreads), hi[m], r.words(access + m * kThreads) + 16);
+        const unsigned char* at = r.words(access + m * kThreads);
+        const bool there = r.readable(access + m * kThreads) && r.holds(at, r.off ? 32 : 16);
+        rows_load_if<false>(there, w[m], at);
+        if (r.off) rows_load_if<false>(there, hi[m], at + 16);
     }
     // (no branch a logit: a few cycles each instead of some hundred)
     const float low = logit_of_bound(at_least), above = low > -kInf ? from_rising((uint32_t)(at_least >> 32) + 1u) : kLowest;
@@ -678,7 +694,7 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const SelectArgs a)
         const uint64_t first = (uint64_t)part * a.run;
         const bool any = u < units && first < a.V;
         const Run<E> r(all + ((uint64_t)g * a.W + b) * a.ld + (any ? first : 0), any ? (uint32_t)(a.V - first < a.run ? a.V - first : a.run) : 0u, all,
-                       all_end);
+                       all_end, a.status);
         if (r.off) Stream<true, E>::start(r, ring);
         else Stream<false, E>::start(r, ring);
         if (q == 0) {
@@ -761,7 +777,10 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const SelectArgs a)
             if (s.best > -kInf && s.best >= low_logit) {
                 collect<E>(r, s.best_at, at_least, (uint32_t)first, work, &n_offers);
                 if (s.second > -kInf && s.second >= low_logit) collect<E>(r, s.second_at, at_least, (uint32_t)first, work, &n_offers);
-                if (s.third > -kInf && s.third >= low_logit) deep[atomicAdd(&n_deep, 1u)] = make_uint2(s.best_at, s.second_at);
+                if (s.third > -kInf && s.third >= low_logit) {
+                    const uint32_t to = atomicAdd(&n_deep, 1u);
+                    if (ROWS_IN_BOUNDS(a.status, to < kThreads)) deep[to] = make_uint2(s.best_at, s.second_at);
+                }
             }
             __syncthreads();
             const uint32_t a_thread = Stream<false, E>::pairs(r), all_deep = n_deep * a_thread;
@@ -808,7 +827,7 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const SelectArgs a)
 #pragma unroll 4
             for (uint32_t o = sub; o < n; o += each) ahead += work[o] > k;
             for (uint32_t d = 1; d < each; d *= 2) ahead += __shfl_xor_sync(0xFFFFFFFFu, ahead, d);
-            if (i < n && ahead < C)
+            if (i < n && ahead < C && ROWS_IN_BOUNDS(a.status, u * C + ahead < units * C))
                 for (uint32_t c = sub; c < ctas; c += each) send(mine + ahead * 8u, bar, c, k);
         } else {
             uint32_t size = kThreads;
@@ -883,11 +902,12 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const SelectArgs a)
                     place += larger_than((same ? all_keys : all_totals) + o * C, C, top, same ? key : total - (o < u ? 1u : 0u));
                 }
             for (uint32_t d = 1; d < each; d *= 2) place += __shfl_xor_sync(0xFFFFFFFFu, place, d);
-            if (key && sub == 0 && place < C) {
+            const uint32_t token = 0xFFFFFFFFu - (uint32_t)key;
+            if (key && sub == 0 && place < C && ROWS_IN_BOUNDS(a.status, b < a.W && (done_of[b] || token < a.V))) {
                 const uint64_t to = (uint64_t)g * C + place;
                 a.best_score[to] = (float)from_rising64(total);
                 a.best_beam[to] = (int32_t)b;
-                a.best_token[to] = done_of[b] ? a.end_token : (int32_t)(0xFFFFFFFFu - (uint32_t)key);
+                a.best_token[to] = done_of[b] ? a.end_token : (int32_t)token;
             }
         }
     }
@@ -918,6 +938,12 @@ struct ReorderArgs {
     unsigned char* dst;
     pearl_states_t sp, dp;
     bool in_place;
+#ifdef PEARL_CHECKED
+    const unsigned char *src_end, *dst_end;           // behind the last state's last byte
+#else
+    // (nobody asks; two members more cost the 1 GB move below 16 %)
+    static constexpr const unsigned char *src_end = nullptr, *dst_end = nullptr;
+#endif
 };
 constexpr uint32_t kMoveThreads = 256;
 
@@ -947,11 +973,12 @@ __global__ void __launch_bounds__(kMoveThreads) reorder_kernel(const ReorderArgs
     for (int i = 0; i < M; ++i) {
         bad |= from[i] < -1 || from[i] >= (int32_t)a.W;
         if ((uint32_t)from[i] >= a.W || (a.in_place && from[i] == i)) from[i] = -1;
+        if (from[i] >= 0 && !ROWS_IN_ARRAY(a.status, src + (uint64_t)(uint32_t)from[i] * a.sp.state_pitch, B, a.src, a.src_end)) from[i] = -1;
         rows_load_if<true>(from[i] >= 0, v[i], src + (uint64_t)(uint32_t)from[i] * a.sp.state_pitch);
     }
 #pragma unroll
     for (int i = 0; i < M; ++i)
-        if (from[i] >= 0) rows_store(dst + (uint64_t)i * a.dp.state_pitch, v[i]);
+        if (from[i] >= 0 && ROWS_IN_ARRAY(a.status, dst + (uint64_t)i * a.dp.state_pitch, B, a.dst, a.dst_end)) rows_store(dst + (uint64_t)i * a.dp.state_pitch, v[i]);
     if (bad && col == 0) atomicOr(a.status, PEARL_ST_BAD_INDEX);
 }
 
@@ -983,7 +1010,7 @@ __global__ void __launch_bounds__(kMoveThreads) reorder_any_kernel(const Reorder
         bad |= from[i] < -1 || from[i] >= (int32_t)a.W;
         if ((uint32_t)from[i] >= a.W || (a.in_place && from[i] == i)) from[i] = -1;
         const int first = (int)(threadIdx.x * 16) - (int)((uint32_t)(uintptr_t)(dst + (uint64_t)i * a.dp.state_pitch) & 15u);
-        v[i].fetch(from[i] >= 0 && first < bytes, src + (uint64_t)(uint32_t)from[i] * a.sp.state_pitch + first, a.src, a.src + src_bytes);
+        v[i].fetch(a.status, from[i] >= 0 && first < bytes, src + (uint64_t)(uint32_t)from[i] * a.sp.state_pitch + first, a.src, a.src + src_bytes);
     }
 #pragma unroll
     for (int i = 0; i < M; ++i) {
@@ -996,7 +1023,7 @@ __global__ void __launch_bounds__(kMoveThreads) reorder_any_kernel(const Reorder
     for (int i = 0; i < M; ++i) {
         unsigned char* to = dst + (uint64_t)i * a.dp.state_pitch;
         const int first = (int)(threadIdx.x * 16) - (int)((uint32_t)(uintptr_t)to & 15u);
-        if (from[i] >= 0 && first < bytes) rows_store_part<S>(to + first, v[i].v, -first, bytes - first);
+        if (from[i] >= 0 && first < bytes) rows_store_part<S>(a.status, to + first, v[i].v, -first, bytes - first, a.dst, a.dst_end);
     }
     if (bad && of == 0 && threadIdx.x == 0) atomicOr(a.status, PEARL_ST_BAD_INDEX);
 }
@@ -1056,20 +1083,26 @@ int rows_launch_beam_reorder(unsigned* status, uint32_t blocks, uint32_t G, uint
     a.sp = sp; a.dp = dp;
     a.in_place = src == dst;
     if (pieces > 1 && sp.piece_pitch == piece_bytes && dp.piece_pitch == piece_bytes) { piece_bytes *= pieces; pieces = 1; }
+    const auto extent = [&](const pearl_states_t& p) {
+        return (uint64_t)(blocks - 1) * p.block_pitch + ((uint64_t)G * W - 1) * p.state_pitch + (uint64_t)(pieces - 1) * p.piece_pitch + piece_bytes;
+    };
+#ifdef PEARL_CHECKED
+    a.src_end = a.src + extent(sp);
+    a.dst_end = a.dst + extent(dp);
+#endif
     uint64_t all = piece_bytes | (uintptr_t)src | (uintptr_t)dst | sp.state_pitch | dp.state_pitch;
     if (pieces > 1) all |= sp.piece_pitch | dp.piece_pitch;
     if (blocks > 1) all |= sp.block_pitch | dp.block_pitch;
     uint32_t g = rows_granule(all);
     if (g == 32 && W > 16) g = 16;          // (32 states of 32 bytes are more than a thread's registers)
     if (g <= 2 && piece_bytes >= kRowsAnyBytes && W <= 8) {            // (more beams' words are more than a thread's registers)
-        const uint64_t src_bytes = (uint64_t)(blocks - 1) * sp.block_pitch + ((uint64_t)G * W - 1) * sp.state_pitch + (uint64_t)(pieces - 1) * sp.piece_pitch + piece_bytes;
         a.piece_cols = piece_bytes;
         a.cols = piece_bytes * pieces;
         a.col_blocks = (piece_bytes + kAnyTile - 1) / kAnyTile * pieces;
         const uint64_t groups = (uint64_t)blocks * G;
         if (a.col_blocks > 0x7FFFFFFFull / groups) return -1;
         const dim3 tiles((uint32_t)(a.col_blocks * groups));
-        return g == 2 ? launch_reorder_any<2>(a, src_bytes, tiles, s) : launch_reorder_any<1>(a, src_bytes, tiles, s);
+        return g == 2 ? launch_reorder_any<2>(a, extent(sp), tiles, s) : launch_reorder_any<1>(a, extent(sp), tiles, s);
     }
     a.piece_cols = piece_bytes / g;
     a.cols = a.piece_cols * pieces;

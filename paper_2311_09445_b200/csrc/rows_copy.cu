@@ -87,13 +87,14 @@ __global__ void __launch_bounds__(kThreads) dispatch_any_kernel(unsigned* status
             // the word's first byte is byte 16 col - shift of the row
             shift[j] = at[j] < 0 ? 0 : (int)((uint32_t)(uintptr_t)(xs + (uint64_t)(uint32_t)at[j] * row_bytes) & 15u);
             if (at[j] >= 0 && (int)(col * 16) - shift[j] >= (int)row_bytes) at[j] = -1;
-            v[j].fetch(at[j] >= 0, row + (int)(col * 16) - shift[j], x, end);
+            v[j].fetch(status, at[j] >= 0, row + (int)(col * 16) - shift[j], x, end);
         }
 #pragma unroll
         for (int j = 0; j < KC; ++j) {
             if (at[j] < 0) continue;
             const int first = (int)(col * 16) - shift[j];
-            rows_store_part<S>(xs + (uint64_t)(uint32_t)at[j] * row_bytes + first, v[j].get(row + first, x, end), -first, (int)row_bytes - first);
+            rows_store_part<S>(status, xs + (uint64_t)(uint32_t)at[j] * row_bytes + first, v[j].get(row + first, x, end), -first,
+                               (int)row_bytes - first, xs, xs + (uint64_t)sorted_rows * row_bytes);
         }
     }
 }
@@ -168,7 +169,7 @@ __global__ void __launch_bounds__(kThreads) combine_any_kernel(unsigned* status,
 #pragma unroll
         for (int j = 0; j < KC; ++j) {
             wt[j] = kWeights ? rows_read_if(j0 + j < k, w + t * k + j0 + j, 1.0f) : 1.0f;
-            any[j].fetch(at[j] >= 0, from + (uint64_t)(uint32_t)at[j] * row_bytes + first, from, end);
+            any[j].fetch(status, at[j] >= 0, from + (uint64_t)(uint32_t)at[j] * row_bytes + first, from, end);
         }
 #pragma unroll
         for (int j = 0; j < KC; ++j) {
@@ -181,7 +182,7 @@ __global__ void __launch_bounds__(kThreads) combine_any_kernel(unsigned* status,
     }
     RowsVec<E, N> o;
     o.set(sum);
-    rows_store_part<S>(out + first, o.raw, -first, row_bytes - first);
+    rows_store_part<S>(status, out + first, o.raw, -first, row_bytes - first, y, y + (T - 1) * ld_y + D);
 }
 
 // ---- the gradient of combine -----------------------------------------------------------------------------------------

@@ -10,14 +10,19 @@
 
 #include "../../include/pearl_rows.h"
 
-// The checked build (-DPEARL_CHECKED): an index into an array that the kernel computed is compared with its extent before it
-// is used; one out of range raises PEARL_ST_INTERNAL and the access is skipped.  (Indices that the caller gives -- ids, places,
-// parents -- are compared in every build.)
+// The checked build (-DPEARL_CHECKED) compares what kernels compute with the extents: the 16-byte words of rows at odd places, read and
+// stored (RowsAny, rows_store_part), and the words of a selection's ring; the moved states' accesses; the router's logits and gradients at a
+// row's end and its experts' places in shared memory; the sort's staged slots and places; a selection's lists; and the experts, places
+// and tokens that are handed out.  One out of range raises PEARL_ST_INTERNAL and the access is skipped.  (Indices that the caller gives --
+// ids, places, parents -- are compared in every build.)
 #ifdef PEARL_CHECKED
 #define ROWS_IN_BOUNDS(status, cond) ((cond) ? true : (atomicOr((status), PEARL_ST_INTERNAL), false))
 #else
 #define ROWS_IN_BOUNDS(status, cond) (true)
 #endif
+// Whether `bytes` bytes from p on lie in [lo, hi).
+#define ROWS_IN_ARRAY(status, p, bytes, lo, hi)                                                                      \
+    ROWS_IN_BOUNDS(status, (uintptr_t)(p) >= (uintptr_t)(lo) && (uintptr_t)(p) + (uintptr_t)(bytes) <= (uintptr_t)(hi))
 
 // Kernel launchers; each returns the number of kernels launched (0: nothing to do), or -1 on a launch error.
 int rows_launch_route(unsigned* status, uint32_t T, uint32_t E, uint32_t k, uint32_t dtype, const void* logits, uint64_t ld,
@@ -231,10 +236,11 @@ struct RowsAny {
         const uint32_t off = (uint32_t)(uintptr_t)p & 15u;
         return (p - off >= lo) & (p - off + (off ? 32 : 16) <= hi);
     }
-    __device__ __forceinline__ void fetch(bool there, const unsigned char* p, const unsigned char* lo, const unsigned char* hi)
+    __device__ __forceinline__ void fetch(unsigned* status, bool there, const unsigned char* p, const unsigned char* lo, const unsigned char* hi)
     {
         const uint32_t off = (uint32_t)(uintptr_t)p & 15u;
-        const bool words = there & whole(p, lo, hi);
+        bool words = there & whole(p, lo, hi);
+        if (words) words = ROWS_IN_ARRAY(status, p - off, off ? 32 : 16, lo, hi);
         rows_load_if<kKept>(words, v, p - off);
         rows_load_if<kKept>(words & (off != 0), w, p - off + 16);
     }
@@ -262,10 +268,11 @@ struct RowsAny {
         return v;
     }
 };
-// Bytes [from, to) of a word, to the 16-byte boundary p.
+// Bytes [from, to) of a word, to the 16-byte boundary p, which is in (or beside) an array [lo, hi).
 template <int S>
-__device__ __forceinline__ void rows_store_part(unsigned char* p, const RowsRaw<16>& v, int from, int to)
+__device__ __forceinline__ void rows_store_part(unsigned* status, unsigned char* p, const RowsRaw<16>& v, int from, int to, const void* lo, const void* hi)
 {
+    if (!ROWS_IN_ARRAY(status, p + (from > 0 ? from : 0), (to < 16 ? to : 16) - (from > 0 ? from : 0), lo, hi)) return;
     if (from <= 0 && to >= 16) {
         rows_store(p, v);
         return;

@@ -118,7 +118,7 @@ __global__ void __launch_bounds__(kThreads) rounds_kernel(unsigned* status, uint
 #pragma unroll
     for (int h = 0; h < kHeld; ++h) {
         const uint32_t j = h * L + lane;
-        if (j < k) {
+        if (j < k && ROWS_IN_BOUNDS(status, held_id[h] >= -1 && held_id[h] < (int32_t)experts)) {
             ids[t * k + j] = held_id[h];
             w[t * k + j] = held_id[h] < 0 ? 0.0f : __fdiv_rn(expf(__fsub_rn(held_x[h], shift)), denominator);
         }
@@ -365,7 +365,7 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(unsigned* status, 
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
         const uint32_t j = lane * kEach + i;
-        if (j < k) {
+        if (j < k && ROWS_IN_BOUNDS(status, !mine[i] || 0xFFFFu - (uint32_t)(mine[i] & 0xFFFFu) < experts)) {
             ids[t * k + j] = mine[i] ? (int32_t)(0xFFFFu - (uint32_t)(mine[i] & 0xFFFFu)) : -1;
             w[t * k + j] = mine[i] ? __fdiv_rn(e[i], sum) : 0.0f;
         }
@@ -379,12 +379,12 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(unsigned* status, 
 // B logits of a row from c on, by accesses of M (which a row's length is a multiple of): -infinity behind the last expert, and for NaN
 // and +infinity, of which it tells.
 template <typename E, int M, int B>
-__device__ __forceinline__ bool load_block(const E* x, uint32_t c, uint32_t experts, float (&v)[B])
+__device__ __forceinline__ bool load_block(unsigned* status, const E* x, uint32_t c, uint32_t experts, float (&v)[B])
 {
     bool bad = false;
 #pragma unroll
     for (int i = 0; i < B; i += M) {
-        if (c + i < experts) {
+        if (c + i < experts && ROWS_IN_BOUNDS(status, c + i + M <= experts)) {
             const RowsVec<E, M> a = rows_load_vec<E, M>(x + c + i);
 #pragma unroll
             for (int m = 0; m < M; ++m) v[i + m] = a.get(m);
@@ -438,6 +438,7 @@ __global__ void __launch_bounds__(kThreads) route_grad_kernel(unsigned* status, 
             if (id != -1) atomicOr(status, PEARL_ST_BAD_INDEX);
             id = -1;
         }
+        if (id >= 0 && !ROWS_IN_BOUNDS(status, r * pitch + (uint32_t)id < rows * pitch)) id = -1;
         float mean = id >= 0 ? __fmul_rn(weight, d) : 0.0f;
         for (uint32_t q = 1; q < 1u << log_kl; q *= 2) mean = __fadd_rn(mean, __shfl_xor_sync(0xFFFFFFFFu, mean, q));
         const float add = kChosen ? __fmul_rn(weight, __fsub_rn(d, mean)) : d;
@@ -472,7 +473,7 @@ __global__ void __launch_bounds__(kThreads) route_grad_kernel(unsigned* status, 
             for (int n = 0; n < H / B; ++n) {
                 const uint32_t c = from + n * step;
                 if (c < experts && there) {
-                    bad |= load_block<E, M, B>(x, c, experts, held[n]);
+                    bad |= load_block<E, M, B>(status, x, c, experts, held[n]);
                 } else {
 #pragma unroll
                     for (int i = 0; i < B; ++i) held[n][i] = -kInf;
@@ -506,7 +507,7 @@ __global__ void __launch_bounds__(kThreads) route_grad_kernel(unsigned* status, 
 #pragma unroll
             for (int i = 0; i < B; i += 4) {
                 float4 four = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                if (c + i < experts) four = *reinterpret_cast<const float4*>(mine + c + i);
+                if (c + i < experts && ROWS_IN_BOUNDS(status, row * pitch + c + i + 4 <= rows * pitch)) four = *reinterpret_cast<const float4*>(mine + c + i);
                 part[i] = four.x; part[i + 1] = four.y; part[i + 2] = four.z; part[i + 3] = four.w;
             }
             if (!kChosen) {
@@ -517,7 +518,7 @@ __global__ void __launch_bounds__(kThreads) route_grad_kernel(unsigned* status, 
             for (int i = 0; i < B; i += M) {
                 RowsVec<E, M> out;
                 out.set(part + i);
-                if (c + i < experts) rows_store_vec<E, M>(dlogits + t * ld_d + c + i, out);
+                if (c + i < experts && ROWS_IN_BOUNDS(status, c + i + M <= experts)) rows_store_vec<E, M>(dlogits + t * ld_d + c + i, out);
             }
         };
         if constexpr (kChosen) {

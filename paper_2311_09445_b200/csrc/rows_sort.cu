@@ -145,8 +145,9 @@ __global__ void __launch_bounds__(kMostThreads) sort_kernel(unsigned* status, ui
             const uint32_t s = begin + q * 32 + lane;
             if (s >= end) continue;
             const uint32_t at = e[q] >= 0 ? start[e[q]] + tally[(uint32_t)e[q] * pitch + warp].y + rank[q] : 0u;
+            if (!ROWS_IN_BOUNDS(status, at < slots)) continue;
             place[s] = e[q] >= 0 ? (int32_t)at : -1;
-            if (e[q] >= 0 && order != nullptr && ROWS_IN_BOUNDS(status, at < slots)) order[at] = (int32_t)s;
+            if (e[q] >= 0 && order != nullptr) order[at] = (int32_t)s;
         }
         return;
     }
@@ -188,16 +189,17 @@ __global__ void __launch_bounds__(kMostThreads) sort_kernel(unsigned* status, ui
                 place[s] = -1;
                 continue;
             }
-            const uint32_t within = tally[(uint32_t)e[q] * pitch + warp].y + rank[q];
+            const uint32_t within = tally[(uint32_t)e[q] * pitch + warp].y + rank[q], to = local[e[q]] + within;
+            if (!ROWS_IN_BOUNDS(status, start[e[q]] + within < slots && to < warps * kHeld * 32u)) continue;
             place[s] = (int32_t)(start[e[q]] + within);
-            staged[local[e[q]] + within] = (uint32_t)(s - cta_first) << 10 | (uint32_t)e[q];      // (at most 8192 slots, 1024 experts)
+            staged[to] = (uint32_t)(s - cta_first) << 10 | (uint32_t)e[q];      // (at most 8192 slots, 1024 experts)
         }
         if (order == nullptr) return;
         __syncthreads();
         const uint32_t n = local[E - 1] + total[E - 1];
         for (uint32_t i = threadIdx.x; i < n; i += blockDim.x) {
             const uint32_t v = staged[i], x = v & 1023u, to = start[x] + i - local[x];
-            if (ROWS_IN_BOUNDS(status, to < slots)) order[to] = (int32_t)(cta_first + (v >> 10));
+            if (ROWS_IN_BOUNDS(status, x < E && to < slots && cta_first + (v >> 10) < slots)) order[to] = (int32_t)(cta_first + (v >> 10));
         }
         return;
     }
@@ -214,8 +216,9 @@ __global__ void __launch_bounds__(kMostThreads) sort_kernel(unsigned* status, ui
             const uint32_t s = s0 + q * 32 + lane;
             if (s >= end || e[q] < 0) continue;
             const uint32_t at = start[e[q]] + tally[(uint32_t)e[q] * pitch + warp].y + rank[q];
+            if (!ROWS_IN_BOUNDS(status, at < slots)) continue;
             place[s] = (int32_t)at;
-            if (order != nullptr && ROWS_IN_BOUNDS(status, at < slots)) order[at] = (int32_t)s;
+            if (order != nullptr) order[at] = (int32_t)s;
         }
     }
 }

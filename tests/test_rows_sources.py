@@ -39,3 +39,19 @@ def test_no_cta_leaves_its_cluster_before_all_have_sent():
     assert "send(" not in behind
     assert re.search(r"if \(late\) \{\s*cluster_wait\(\);\s*if \(!arrived\(", behind)
     assert re.search(r"if \(!late\) cluster_wait\(\);\s*\}\s*$", behind)
+
+
+@pytest.mark.parametrize("name,checked", [
+    ("rows_route.cu", ["held_id", "mine", "experts", "pitch"]), ("rows_sort.cu", ["slots", "kHeld"]), ("rows_copy.cu", []),
+    ("rows_beam.cu", ["kThreads", "a.src_end", "a.dst_end", "units", "a.V"]), ("rows_internal.cuh", ["lo, hi"])])
+def test_the_checked_build_has_something_to_check(name, checked):
+    """tests/test_checked_rows.py runs the row operators' tests on a build that compares computed indices with their extents: it says
+    something about a kernel only where that is written."""
+    text = code(os.path.join(ROOT, "paper_2311_09445_b200", "csrc", name))
+    checks = re.findall(r"ROWS_IN_(?:BOUNDS|ARRAY)\((.*)", text)
+    for what in checked:
+        assert any(what in c for c in checks), what
+    if "RowsAny<" in text:                                   # rows at odd places: read and stored through the checked helpers, with their extents
+        assert re.search(r"\.fetch\((?:a\.)?status, ", text)
+        if name != "rows_internal.cuh":
+            assert all(c.count(",") >= 6 for c in re.findall(r"rows_store_part<S>\((.*?)\);", text, flags=re.S))
