@@ -951,3 +951,77 @@ def test_no_status_bit_is_lost_between_streams():
         assert r.sync() == 0
     graph.reset()
     r.close()
+
+
+# ---- loops that only larger calls reach ------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("kind", ["fp32", "fp16", "bf16"])
+@pytest.mark.parametrize("T,k,D", [(3, 2, 8200), (2, 1, 12289), (2, 3, 4097), (5, 2, 2047), (2, 9, 1031), (1, 1, 40000)])
+def test_combine_grad_sums_every_element(rows, kind, T, k, D):
+    """Small whole numbers: every product and every sum is exact, in any order, so a left out or doubled element shows."""
+    z = torch.randint(1, 5, (T * k, D), generator=gen(81, T, k, D)).to(TYPES[kind])
+    dy = torch.randint(1, 5, (T, D), generator=gen(82, T, k, D)).to(TYPES[kind])
+    place = places(T, k, 0.0, 4)
+    want = torch.einsum("td,tkd->tk", dy.double(), z.double()[place.long()])
+    assert want.max() < 2 ** 24
+    for g in (dy.cuda(), strided(dy, 5, 3), strided(dy, 8, 8)):
+        dw = torch.zeros(T, k, device="cuda")
+        rows.combine_grad(g, z.cuda(), place.cuda(), None, None, dw)
+        assert torch.equal(dw.double().cpu(), want)
+    assert rows.sync() == 0
+
+
+@pytest.mark.parametrize("kind", ["fp32", "bf16"])
+@pytest.mark.parametrize("T,E,k,chosen", [(20011, 40, 20, True), (20011, 40, 20, False), (12011, 600, 2, False), (12011, 1024, 8, True), (330011, 8, 2, False),
+                                          (330011, 16, 1, True), (90011, 128, 8, False)])
+def test_router_with_more_rows_than_the_gpu_holds_at_once(rows, kind, T, E, k, chosen):
+    """The gradient's warps take several groups of rows each, one after the other, through the same shared memory; the choice has that
+    many blocks.  Against the definition in 64 bits, and the same rows in smaller calls."""
+    dev = torch.device("cuda")
+    g = torch.Generator(device=dev)
+    g.manual_seed(83)
+    l = (torch.randn(T, E, device=dev, generator=g) * 1.5).clamp(-5, 5).to(TYPES[kind])
+    l.masked_fill_(torch.rand(T, E, device=dev, generator=g) < 0.1, -math.inf)
+    l[T // 2] = -math.inf                                   # a row without experts
+    dw = torch.randn(T, k, device=dev, generator=g)
+    w, ids = run_route(rows, l, k, chosen)
+    d = torch.full((T, E), 3.0, dtype=TYPES[kind], device=dev)
+    rows.route_grad(None if chosen else l, w, ids, dw, d, over_chosen=chosen)
+    step = 1009
+    for a in list(range(0, T, step))[::7] + [T - step]:
+        part = l[a:a + step].contiguous()
+        part_w, part_ids = run_route(rows, part, k, chosen)
+        assert torch.equal(part_w, w[a:a + step]) and torch.equal(part_ids, ids[a:a + step])
+        part_d = torch.full_like(part, 3.0)
+        rows.route_grad(None if chosen else part, part_w, part_ids, dw[a:a + step].contiguous(), part_d, over_chosen=chosen)
+        assert torch.equal(part_d, d[a:a + step])
+
+    x = l.double()
+    left, at, best = x.clone(), [], []
+    for _ in range(k):                                      # the largest that is left, the first of equal ones
+        top = left.amax(1, keepdim=True)
+        first = torch.where(left == top, torch.arange(E, device=dev), E).amin(1, keepdim=True)
+        at.append(torch.where(top == -math.inf, -1, first))
+        best.append(top)
+        left.scatter_(1, first, -math.inf)
+    at, best = torch.cat(at, 1), torch.cat(best, 1)
+    assert torch.equal(ids.long(), at)
+    top = torch.where(best[:, :1] == -math.inf, 0.0, best[:, :1])
+    e = (x - top).exp()
+    member = torch.zeros_like(x).scatter_add_(1, at.clamp_min(0), (at >= 0).double())
+    p = e * member if chosen else e
+    p = p / p.sum(1, keepdim=True).clamp_min(1e-300)
+    want_w = torch.where(at < 0, 0.0, p.gather(1, at.clamp_min(0)))
+    # two exponentials within 2 units of the last place (4 half steps) of differences (|x| <= 10 half steps), additions, the division
+    rel = (2 * (4 + 10) + E + 1) * U
+    assert ((w.double() - want_w).abs() <= rel * want_w).all()
+    part = want_w * dw.double()
+    mean, size = part.sum(1, keepdim=True), part.abs().sum(1, keepdim=True)
+    grad = torch.zeros_like(x).scatter_add_(1, at.clamp_min(0), dw.double() * (at >= 0))
+    want = p * (grad - mean)
+    # p and the weights within that, and the mean's products and additions: k + 1 half steps of its magnitude; the difference, the product and
+    # the reciprocal one each; a rounding to the type
+    tol = p * ((2 * rel + (k + 5) * U) * (grad.abs() + size))
+    small = 2.0 ** -25 if kind == "fp16" else 0.0
+    assert ((d.double() - want).abs() <= tol + ref.HALF_STEP[kind] * (want.abs() + tol) + small).all()
+    assert rows.sync() == 0
