@@ -950,6 +950,7 @@ constexpr uint32_t kMoveThreads = 256;
 template <int B, int M>
 __global__ void __launch_bounds__(kMoveThreads) reorder_kernel(const ReorderArgs a)
 {
+    static_assert(B < 32 || M <= 16, "32 states of 32 bytes are more than a thread's registers");
     rows_begin();
     const uint64_t og = blockIdx.x / a.col_blocks;
     const uint32_t g = (uint32_t)(og % a.G);
@@ -1040,7 +1041,8 @@ int launch_reorder(const ReorderArgs& a, dim3 grid, cudaStream_t s)
     if (a.W <= 4) return rows_launch(reorder_kernel<B, 4>, grid, dim3(kMoveThreads), 0, s, 0, a);
     if (a.W <= 8) return rows_launch(reorder_kernel<B, 8>, grid, dim3(kMoveThreads), 0, s, 0, a);
     if (a.W <= 16) return rows_launch(reorder_kernel<B, 16>, grid, dim3(kMoveThreads), 0, s, 0, a);
-    return rows_launch(reorder_kernel<B, 32>, grid, dim3(kMoveThreads), 0, s, 0, a);
+    if constexpr (B < 32) return rows_launch(reorder_kernel<B, 32>, grid, dim3(kMoveThreads), 0, s, 0, a);
+    else return -1;
 }
 
 }  // namespace
@@ -1094,7 +1096,7 @@ int rows_launch_beam_reorder(unsigned* status, uint32_t blocks, uint32_t G, uint
     if (pieces > 1) all |= sp.piece_pitch | dp.piece_pitch;
     if (blocks > 1) all |= sp.block_pitch | dp.block_pitch;
     uint32_t g = rows_granule(all);
-    if (g == 32 && W > 16) g = 16;          // (32 states of 32 bytes are more than a thread's registers)
+    if (g == 32 && W > 16) g = 16;          // (see reorder_kernel)
     if (g <= 2 && piece_bytes >= kRowsAnyBytes && W <= 8) {            // (more beams' words are more than a thread's registers)
         a.piece_cols = piece_bytes;
         a.cols = piece_bytes * pieces;
