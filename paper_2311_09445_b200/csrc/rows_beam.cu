@@ -523,7 +523,9 @@ struct Stream {
         return s;
     }
     // Long runs call a function for the loop, because inlined the registers of what follows in the kernel are spilled inside it (42 us
-    // instead of 40); short ones are a function as a whole, whose way is shorter (8.7 us for 4 rows of 32003 instead of 9.1).
+    // instead of 40); short ones are a function as a whole, whose way is shorter (8.8 us for 4 rows of 32003 instead of 9.1).  From 9
+    // whole pairs on a run is long: of 3, 5, 9, 17 and 33, 3 makes those rows long (9.1), and the others are within 3 % of one another from 64 x 8 rows
+    // of 10000 logits to 131072.
     static constexpr uint32_t kLong = 9;
     static __device__ __noinline__ Stats short_run(const Run<E> r, uint32_t ring) { return walk<false>(r, ring); }
     static __device__ __forceinline__ Stats run(const Run<E>& r, uint32_t ring) { return plain(r) < kLong ? short_run(r, ring) : walk<true>(r, ring); }
@@ -1052,12 +1054,14 @@ int rows_launch_beam_select(unsigned* status, uint32_t G, uint32_t W, uint32_t V
                             int32_t* best_beam, int32_t* best_token, cudaStream_t s)
 {
     if (G == 0) return 0;
-    // Rows are cut into parts where there are too few of them to occupy the GPU; a part has 1024 logits at least.
+    // Rows are cut into parts where there are too few of them to occupy the GPU, fewer than two an SM (148 rows of 131072 bfloat16 logits
+    // 18.6 us; cut below one an SM 20.0, below four 24.8; 100 rows of 50257: 15.5, 14.5, 23.2; 296 of 131072: 24.6, 24.6, 26.5).  A part has 1024
+    // logits at least (4 rows of 8000 binary32 logits 7.1 us; with 2048 7.6, with 512 7.2; 1 row of 4000: 7.1, 7.6, 7.2).
     SelectArgs a;
     const uint32_t most = (uint64_t)G * kMostCtas <= (uint64_t)rows_sm_count() && W <= kMostCtas ? kMostCtas : 8u;
     a.units_per_cta = (W + most - 1) / most;
     a.parts = 1;
-    while ((a.parts + 1) * W <= most && (uint64_t)G * W * a.parts < 592 && V / (a.parts + 1) >= 1024) ++a.parts;
+    while ((a.parts + 1) * W <= most && (uint64_t)G * W * a.parts < 2u * rows_sm_count() && V / (a.parts + 1) >= 1024) ++a.parts;
     a.run = ((V + a.parts - 1) / a.parts + 7) / 8 * 8;
     const uint32_t units = W * a.parts, ctas = (units + a.units_per_cta - 1) / a.units_per_cta;
     if ((uint64_t)G * ctas > 0x7FFFFFFFull) return -1;
