@@ -135,7 +135,7 @@ int pearl_rows_beam_select(pearl_rows_t* rows, uint32_t G, uint32_t W, uint32_t 
  * overlap those of dst (PEARL_ERR_BAD_ARG).  A parent of -1 leaves the
  * state (of dst) as it was; any other parent outside [0, W) does so too and raises PEARL_ST_BAD_INDEX.
  * The pieces of different states must not overlap in dst.  1 <= W <= PEARL_ROWS_MAX_BEAMS; blocks, G, pieces or piece_bytes
- * of 0 is a call with nothing to do. */
+ * of 0 is a call with nothing to do; blocks * G < 2^31 (PEARL_ERR_BAD_BATCH). */
 typedef struct pearl_states {
     uint64_t block_pitch, state_pitch, piece_pitch;      /* bytes */
 } pearl_states_t;

@@ -215,6 +215,7 @@ int pearl_rows_beam_reorder(pearl_rows_t* h, uint32_t blocks, uint32_t G, uint32
     if (!h) return PEARL_ERR_NULL;
     if (W < 1 || W > PEARL_ROWS_MAX_BEAMS) return PEARL_ERR_BAD_ARG;
     if (blocks == 0 || G == 0 || pieces == 0 || piece_bytes == 0) return PEARL_OK;
+    if ((uint64_t)blocks * G > 0x7FFFFFFFull) return PEARL_ERR_BAD_BATCH;           // (each has a block of threads at least)
     if (!parent || !src || !dst || !sp || !dp) return PEARL_ERR_NULL;
     if (misaligned(parent, 4)) return PEARL_ERR_ALIGN;
     uint64_t sb = 0, db = 0;

@@ -1,4 +1,6 @@
 """RowRouter's checks of sizes, on tensors without memory (no GPU needed)."""
+import ctypes as C
+
 import pytest
 import torch
 
@@ -92,3 +94,13 @@ def test_unsigned_arguments_are_the_ones_checked():
     assert {n: routing.SIGNATURES[n][1].count(routing._u32) for n in names if routing._u32 in routing.SIGNATURES[n][1]} == {
         "pearl_rows_route": 4, "pearl_rows_route_grad": 4, "pearl_rows_sort": 2, "pearl_rows_dispatch": 4, "pearl_rows_combine": 5,
         "pearl_rows_combine_grad": 5, "pearl_rows_beam_select": 5, "pearl_rows_beam_reorder": 4}
+
+
+def test_states_of_more_groups_than_a_grid_has_blocks_are_refused():
+    """pearl_rows_beam_reorder refuses them by its own check, before it looks into the handle, and not by a failed launch."""
+    from paper_2311_09445_b200 import build
+    build.build()
+    lib, handle = routing.load_library(), C.cast(C.create_string_buffer(256), C.c_void_p)
+    for blocks, G in ((1 << 16, 1 << 15), (1, 1 << 31), (3, (1 << 30) + 1)):
+        states = routing._States(8 * G, 8, 8)
+        assert lib.pearl_rows_beam_reorder(handle, blocks, G, 1, 1, 8, 4096, 4096, C.byref(states), 4096, C.byref(states)) == -3
