@@ -21,7 +21,7 @@
  *     binary32 or wider, the router's exponentials within 2 units of the last place; what is handed out in a narrower type is
  *     rounded to it once.
  *   - Rows of a matrix may lie apart (the ld_* arguments, in elements, at least the row's length); the elements of
- *     a row are consecutive.  The bytes between rows are never written; up to 16 of them beside a row may be read.
+ *     a row are consecutive.  The bytes between rows are never written; up to 31 of them beside a row may be read.
  *     Pointers must be aligned to their element size, else PEARL_ERR_ALIGN.  Rows whose start and length are multiples of
  *     16 bytes move fastest.
  *   - Results do not depend on timing: the same inputs give the same bits.
@@ -59,7 +59,8 @@ uint64_t pearl_rows_slab_bytes(void);
  * stream).  slab: optional caller-owned device memory of at least pearl_rows_slab_bytes() bytes, 256-byte aligned; NULL
  * lets the library allocate (and free in destroy).  It is zeroed on the stream. */
 int pearl_rows_create(pearl_rows_t** out, int device, void* cuda_stream, void* slab, uint64_t slab_bytes);
-/* Synchronises the stream, frees what the library owns. */
+/* Synchronises the stream, frees what the library owns.  Graphs captured from the handle's calls must not run after this: their kernels
+ * raise bits in its status word. */
 int pearl_rows_destroy(pearl_rows_t* rows);
 
 /* The router.  Of row t's E logits the k largest are chosen, in falling order, the lower expert first among equal ones:
