@@ -317,13 +317,16 @@ _routers = {}
 
 def _router(s):
     """The program's handle of the current stream: made once for it, and kept where the program keeps its tensors."""
-    stream = torch.cuda.current_stream()
-    key = (stream.device_index, stream.cuda_stream)
-    if s.get("stream") != key:
+    device = s.get("device")
+    if device is None:
+        device = s["device"] = torch.cuda.current_device()
+    stream = torch._C._cuda_getCurrentRawStream(device)      # (as a number: a stream object takes as long as a small call)
+    if s.get("stream") != stream:
+        key = (device, stream)
         if key not in _routers:
             from paper_2311_09445_b200 import RowRouter
-            _routers[key] = RowRouter(stream=stream)
-        s["stream"], s["router"] = key, _routers[key]
+            _routers[key] = RowRouter(stream=torch.cuda.current_stream(device))
+        s["stream"], s["router"] = stream, _routers[key]
     return s["router"]
 
 
