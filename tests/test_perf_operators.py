@@ -19,14 +19,18 @@ def operators():
 def test_a_pass_uses_the_handle_of_the_current_stream(operators, monkeypatch):
     """A state that is run on one stream and then, or captured, on another: its calls go where the current stream is."""
     import paper_2311_09445_b200 as package
-    current = []
-    monkeypatch.setattr(operators.torch.cuda, "current_stream", lambda device=None: current[-1])
+    streams, device = {0: 16, 1: 16}, [0]                            # (two devices' streams may have one number)
+    cuda = operators.torch.cuda
+    monkeypatch.setattr(cuda, "current_device", lambda: device[0])
+    monkeypatch.setattr(cuda, "current_stream", lambda d=None: (device[0] if d is None else d, streams[device[0] if d is None else d]))
+    monkeypatch.setattr(operators.torch._C, "_cuda_getCurrentRawStream", lambda d: streams[d], raising=False)
     monkeypatch.setattr(package, "RowRouter", lambda device=None, stream=None: types.SimpleNamespace(stream=stream))
-    a, b, other_device = (types.SimpleNamespace(device_index=d, cuda_stream=p) for d, p in ((0, 16), (0, 32), (1, 16)))
     state, handles = {"case": {}}, []
-    for s in (a, a, b, a, other_device):
-        current.append(s)
+    for raw in (16, 16, 32, 16):
+        streams[0] = raw
         handles.append(operators._router(state))
-        assert handles[-1].stream is s
+        assert handles[-1].stream == (0, raw)
     assert handles[0] is handles[1] is handles[3]
-    assert operators._router({"case": {}}) is handles[4]            # another program's state shares the stream's handle
+    assert operators._router({"case": {}}) is handles[3]            # another program's state shares the stream's handle
+    device[0] = 1
+    assert operators._router({"case": {}}).stream == (1, 16)
