@@ -30,7 +30,7 @@ constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
 // What bounds it.  64 groups of 8 beams over 131072 bfloat16 logits (121 MB, 18 us at the rate of a copy): 40 us.  Reading takes
 // some 26 where four CTAs share an SM, 0.84 for 16 logits of each of its threads: 114 instructions a warp, half of what the SM can issue
 // in that time, and 17 for the unit of the exponentials, two thirds of what that can.  The rest are some 1700 instructions a warp in a
-// row, and nothing left to hide them behind, because all CTAs run at once.  4 rows of 32003 binary32 logits: 8.7 us, which are those
+// row, and nothing left to hide them behind, because all CTAs run at once.  4 rows of 32003 binary32 logits: 8.8 us, which are those
 // instructions.  Tried and not kept: four accesses at a time (63 us: spilled), clusters of 16 CTAs for the large case (70 us against
 // 48 then), the best pairs asked for again ahead of time (49 us against 48).
 constexpr uint32_t kThreads = 256, kWarps = kThreads / 32;
@@ -927,8 +927,8 @@ __global__ void __launch_bounds__(kThreads, 4) select_kernel(const SelectArgs a)
 // ---- the states ------------------------------------------------------------------------------------------------------
 // state[o, g, i] <- state[o, g, parent[g, i]].  A thread has one access's worth of all W states of a block and group: it reads
 // what the moved states need, all at once (a state with several children comes from a cache the second time), then writes.  No other
-// thread touches those bytes, so the move can be made in place.  1 GB of states of 8 beams, 5 of which survive, in place: 230 us for
-// 1.57 GB that have to move, 6.8 TB/s (branches around the loads, and 16-byte accesses: 400).
+// thread touches those bytes, so the move can be made in place.  1 GB of states of 8 beams, 5 of which survive, in place: 230 us, in
+// which DRAM moves 1.53 GB, 6.66 TB/s (branches around the loads, and 16-byte accesses: 400).
 struct ReorderArgs {
     unsigned* status;
     uint32_t G, W;

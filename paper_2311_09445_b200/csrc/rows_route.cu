@@ -4,10 +4,12 @@
 // orders like (larger logit, lower expert): for 16-bit logits 32 bits, so that a comparison and exchange is one maximum and two
 // multiply-adds.  A lane sorts its logits KP at a time by a network (KP: k rounded up to a power of two), keeps the KP best of them by
 // bitonic merges, and merges with the other lanes' lists by exchanges.  No branch depends on the data.  65521 rows of 128 bfloat16
-// logits, k = 8, over the chosen ones: 8.2 us, bound by these exchanges; the 21 MB it moves are 3.2.  Its gradient 5.5 us, of which the
-// 23 MB it reads and writes are 3.5 (both: 13.8; by rounds, below: 49).  binary32 logits cost more, because a 64-bit exchange is four
-// such instructions and four multiply-adds: 65521 rows of 64, k = 6: 11.1 us.
-// More choices (rounds_kernel): k rounds of "largest that is left" over the row's lanes.
+// logits, k = 8, over the chosen ones: 8.2 us, bound by these exchanges; the 21 MB it moves are 3.2.  Its gradient 6.1 us, the 23 MB it
+// reads and writes are 3.5.  (By rounds, below, choice and gradient took 49 where this way took 13.8; they are 14.3 now.)  Over all experts
+// 10.7 and 13.7 us: an exponential a logit in each.  binary32 logits cost more, because a 64-bit exchange is four such instructions and
+// four multiply-adds: 65521 rows of 64, k = 6: 10.7 us.
+// More choices (rounds_kernel): k rounds of "largest that is left" over the row's lanes, so bound by k chains of warp maxima: 65521 rows of 128
+// bfloat16 logits 55 us with k = 16 and 103 with k = 32, of 64 binary32 ones 28 with k = 16.
 #include "rows_internal.cuh"
 
 namespace {
@@ -399,7 +401,7 @@ __device__ __forceinline__ bool load_block(unsigned* status, const E* x, uint32_
     return bad;
 }
 // Where the softmax runs over all experts a lane holds its logits, H = 16 or 32 of them, and then their exponentials (read again for the
-// maximum, the sum and the gradient: 16.1 us instead of 12.6 for 65521 rows of 128 bfloat16 logits).
+// maximum, the sum and the gradient: 16.1 us instead of 12.6 for 65521 rows of 128 bfloat16 logits, when the exponentials were shorter; 13.7 now).
 constexpr uint32_t kRowFloats = 1024;                // of shared memory per warp at most: R rows of the experts, rounded up to 4; so 32 a lane
 template <typename E, int M, bool kChosen, int H>
 __global__ void __launch_bounds__(kThreads) route_grad_kernel(unsigned* status, uint32_t T, uint32_t experts, uint32_t k, uint32_t log_kl,
