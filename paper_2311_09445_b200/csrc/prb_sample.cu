@@ -114,7 +114,7 @@ __device__ __forceinline__ void descend(const PrbView& v, const SamplePlan& plan
             __syncwarp();
             row = pf + (uint32_t)j * K;
         } else {
-            const float mine = __ldg(v.level[l] + g * K + lane);
+            const float mine = v.level[l][g * K + lane];
             if (pf != nullptr && l + 1 == v.depth) {
                 // the leaves under this group's K nodes: K*K/4 units of 16 bytes, dealt over the K lanes
                 // (fanout 2: one unit); units past the end of the leaf level are left out
@@ -272,13 +272,14 @@ prb_sample_kernel(const __grid_constant__ PrbView v, uint32_t B, float beta, uin
     const bool ring_lane = bulk && tid < plan.ring_stages;
     if (ring_lane) ring.init(s_ring + 8u * tid, s_ring + kRingBarBytes + tid * plan.ring_stage_bytes);
     // (launched as a programmatic dependent of the kernel before it on the stream: up to here it may have run
-    // beside that kernel; nothing has been read or written yet)
+    // beside that kernel; nothing has been read or written yet.  The tree, which that kernel may have written, is read
+    // by plain loads, which stay behind the wait; those of the read-only path need not.)
     prb_dep_wait();
     // every thread reads the state it needs itself (same addresses: one request per warp), so the
     // targets can be formed while the staged levels are still on their way
     const unsigned long long calls = v.state->sample_calls;
     const unsigned long long fill = v.state->fill;
-    const float total32 = __ldg(v.level[0]);
+    const float total32 = *v.level[0];
     const float pmin = plan.buffer_norm ? prb_buffer_pmin(v) : 0.0f;
     {
         // stage the top levels: one contiguous run of the slab starting at level 1, 16 bytes at a time
@@ -287,7 +288,7 @@ prb_sample_kernel(const __grid_constant__ PrbView v, uint32_t B, float beta, uin
         float4 t[kPerThread];
 #pragma unroll
         for (uint32_t u = 0; u < kPerThread; ++u)
-            if (tid + u * kThreads < plan.top_vec4) t[u] = __ldg(src + tid + u * kThreads);
+            if (tid + u * kThreads < plan.top_vec4) t[u] = src[tid + u * kThreads];
 #pragma unroll
         for (uint32_t u = 0; u < kPerThread; ++u)
             if (tid + u * kThreads < plan.top_vec4) reinterpret_cast<float4*>(s_top)[tid + u * kThreads] = t[u];

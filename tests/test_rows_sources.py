@@ -55,3 +55,11 @@ def test_the_checked_build_has_something_to_check(name, checked):
         assert re.search(r"\.fetch\((?:a\.)?status, ", text)
         if name != "rows_internal.cuh":
             assert all(c.count(",") >= 6 for c in re.findall(r"rows_store_part<S>\((.*?)\);", text, flags=re.S))
+
+
+def test_the_sample_kernel_reads_the_tree_behind_the_wait():
+    """prb_sample_kernel is launched in the same way, beside the kernel that may be writing the tree."""
+    text = code(os.path.join(ROOT, "paper_2311_09445_b200", "csrc", "prb_sample.cu"))
+    kernel = text[text.index("prb_sample_kernel(const __grid_constant__"):text.index("prb_leaf_min_kernel(")]
+    walk = text[:text.index("prb_sample_kernel(const __grid_constant__")]
+    assert "prb_dep_wait();" in kernel and "__ldg" not in kernel and "__ldg" not in walk
