@@ -10,7 +10,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpearl_prb.so")
 LIB_CHECKED = os.path.join(HERE, "libpearl_prb_checked.so")     # every index checked against its extent (-DPEARL_CHECKED)
 SOURCES = ["prb_host.cu", "prb_insert.cu", "prb_sample.cu", "prb_sample_short.cu", "prb_step.cu", "prb_tree.cu", "prb_update.cu", "prb_update_wide.cu",
-           "rows_host.cu", "rows_route.cu", "rows_sort.cu", "rows_copy.cu", "rows_beam.cu"]
+           "rows_host.cu", "rows_route.cu", "rows_sort.cu", "rows_copy.cu", "rows_beam.cu",
+           "layer_host.cu", "layer_norm.cu", "layer_dropout.cu", "layer_experts.cu"]
 
 NVCC_FLAGS = [
     "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
@@ -33,7 +34,7 @@ def needs_build(lib: str = LIB) -> bool:
         return True
     t = os.path.getmtime(lib)
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)]
-    deps += [os.path.join(os.path.dirname(HERE), "include", h) for h in ("pearl_prb.h", "pearl_rows.h")]
+    deps += [os.path.join(os.path.dirname(HERE), "include", h) for h in ("pearl_prb.h", "pearl_rows.h", "pearl_layers.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 
 

@@ -2,15 +2,7 @@
 #include <math.h>
 #include <new>
 
-#include "rows_internal.cuh"
-
-struct pearl_rows {
-    unsigned* status;           // two words: the status bits, and those that pearl_rows_sync() has taken
-    bool owns_slab;
-    int device;
-    cudaStream_t stream;
-    uint64_t launches;
-};
+#include "rows_handle.cuh"
 
 namespace {
 
@@ -23,35 +15,7 @@ __global__ void take_status_kernel(unsigned* status)
     status[1] = atomicExch(status, 0u);
 }
 
-// Makes `dev` the current device for a call; the device that was current is so again afterwards.
-struct DeviceGuard {
-    int prev;
-    bool ok, other;
-    explicit DeviceGuard(int dev) : prev(-1), ok(true), other(false)
-    {
-        if (cudaGetDevice(&prev) != cudaSuccess) { ok = false; return; }
-        other = prev != dev;
-        if (other && cudaSetDevice(dev) != cudaSuccess) ok = false;
-    }
-    ~DeviceGuard() { if (other) cudaSetDevice(prev); }
-};
-
-bool misaligned(const void* p, uint32_t to) { return ((uintptr_t)p & (to - 1)) != 0; }
 bool bad_slots(uint64_t T, uint64_t k) { return k < 1 || T * k > 0x7FFFFFFFull; }
-// (a matrix of T rows of `row`, `ld` apart; one row needs no distance)
-bool bad_ld(uint64_t T, uint64_t row, uint64_t ld) { return T > 1 && (ld < row || ld > (1ull << 40)); }
-bool bad_type(uint32_t dtype) { return dtype > PEARL_BF16; }
-
-// Enqueues `launch()` with the handle's device current and counts its kernels.
-template <typename F> int enqueue(pearl_rows* h, F launch)
-{
-    DeviceGuard guard(h->device);
-    if (!guard.ok) return PEARL_ERR_CUDA;
-    const int n = launch();
-    if (n < 0) { cudaGetLastError(); return PEARL_ERR_CUDA; }
-    h->launches += (uint64_t)n;
-    return PEARL_OK;
-}
 
 // The bytes [first, last) that states of this layout occupy.
 bool extent(uint32_t blocks, uint32_t G, uint32_t W, uint32_t pieces, uint64_t piece_bytes, const pearl_states_t* p, uint64_t* bytes)
