@@ -1,29 +1,45 @@
 // A whole expert layer for a few rows: the router's product and choice, the experts' two products, their weighted sum.
+//
+// With few rows the layer is the reading of the weights that the rows ask for: 2 n floating-point operations for each weight where n rows
+// ask for its expert.  So the weights are streamed once, straight from memory into the registers of the warps that multiply them,
+// as the 16-row operand of a matrix instruction whose other operand are the expert's rows in groups of 8 columns; the sums
+// are then so small that everything else is a chain of short steps.
 #include "layer_internal.cuh"
 
 namespace {
 
-constexpr uint32_t kWarps = 8;
+constexpr uint32_t kWarps = 8, kThreads = kWarps * 32;
+constexpr uint32_t kBlockBytes = 128;         // of a weight row: what a warp takes of 16 rows in one step, 32 bytes a lane of each of two rows
+constexpr uint32_t kMaxSlots = PEARL_LAYER_MAX_FEW * PEARL_ROWS_MAX_CHOICES;
+constexpr uint32_t kSpins = 1u << 21;
 
-// The parts of the scratch, in bytes from its start.
+// The parts of the scratch, in bytes from its start.  The counters are zero between calls.
+struct Counters {
+    uint32_t ticket, finished;
+    uint32_t up[PEARL_ROWS_MAX_EXPERTS];               // finished pieces of an expert's first product
+    uint32_t down[PEARL_LAYER_MAX_INNER / 16];         // experts that are through with a piece of y
+};
 struct Layout {
-    uint64_t logits, h, bytes;
+    uint64_t logits, h, z, bytes, pitch;
 };
 Layout layout_of(uint32_t T, uint32_t D, uint32_t H, uint32_t E, uint32_t k)
 {
-    (void)D;
+    const auto up = [](uint64_t n) { return (n + 255) / 256 * 256; };
     Layout l;
-    l.logits = 0;
-    l.h = l.logits + ((uint64_t)T * E * 4 + 255) / 256 * 256;
-    l.bytes = l.h + ((uint64_t)T * k * H * 4 + 255) / 256 * 256;
+    l.pitch = 2 * ((2ull * H + 127) / 128 * 128);       // of a slot's h: two rows of 16 bits, or one of 32
+    l.logits = up(sizeof(Counters));
+    l.h = l.logits + up((uint64_t)T * E * 4);
+    l.z = l.h + up((uint64_t)T * k * l.pitch);
+    l.bytes = l.z + up((uint64_t)T * k * D * 4);
     return l;
 }
 
 template <typename E> __device__ __forceinline__ float element(const E* p) { return RowsElem<E>::up(*p); }
 
+// ---- the router's product --------------------------------------------------------------------------------------------
 // logits[t, e]: a warp each, in binary64.
 template <typename T>
-__global__ void __launch_bounds__(kWarps * 32) logits_kernel(uint32_t rows, uint32_t D, uint32_t E, const T* x, uint64_t ld_x, const T* router, float* logits)
+__global__ void __launch_bounds__(kThreads) logits_kernel(uint32_t rows, uint32_t D, uint32_t E, const T* x, uint64_t ld_x, const T* router, float* logits)
 {
     rows_begin();
     const uint32_t i = blockIdx.x * kWarps + (threadIdx.x >> 5), lane = threadIdx.x & 31u;
@@ -35,73 +51,487 @@ __global__ void __launch_bounds__(kWarps * 32) logits_kernel(uint32_t rows, uint
     if (lane == 0) logits[i] = (float)s;
 }
 
-// h[slot, j]: a warp each.
-template <typename T>
-__global__ void __launch_bounds__(kWarps * 32) up_kernel(unsigned* status, uint32_t D, uint32_t H, uint32_t E, uint32_t k, uint32_t act, const T* x, uint64_t ld_x,
-                                                         const T* up, const int32_t* ids, float* h)
+// ---- 32 bytes of a row ---------------------------------------------------------------------------------------------
+// A piece: 16 (or 8) elements of a row, of which the first n are there; the others are 0.  kAlign: what rows and their lengths are multiples
+// of, 32 or 16 bytes; 0: nothing, the piece comes out of the aligned words around it.
+template <int kAlign> struct Piece {
+    RowsRaw<32> v;
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v.r[i] = 0u;
+    }
+    template <bool kOnce> __device__ __forceinline__ void fetch(const unsigned char* p, int bytes, const unsigned char*, const unsigned char*)
+    {
+        clear();
+        if constexpr (kAlign == 32) {
+            if constexpr (kOnce) {
+                rows_load_if<false>(bytes > 0, v, p);
+            } else {
+                asm volatile("{ .reg .pred q; setp.ne.u32 q, %9, 0; @q ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8]; }"
+                             : "+r"(v.r[0]), "+r"(v.r[1]), "+r"(v.r[2]), "+r"(v.r[3]), "+r"(v.r[4]), "+r"(v.r[5]), "+r"(v.r[6]), "+r"(v.r[7])
+                             : "l"(p), "r"((uint32_t)(bytes > 0)) : "memory");
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; i += 4) {
+                if constexpr (kOnce)
+                    asm volatile("{ .reg .pred q; setp.ne.u32 q, %5, 0; @q ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4]; }"
+                                 : "+r"(v.r[i]), "+r"(v.r[i + 1]), "+r"(v.r[i + 2]), "+r"(v.r[i + 3]) : "l"(p + i * 4), "r"((uint32_t)(bytes > i * 4)));
+                else
+                    asm volatile("{ .reg .pred q; setp.ne.u32 q, %5, 0; @q ld.global.v4.b32 {%0, %1, %2, %3}, [%4]; }"
+                                 : "+r"(v.r[i]), "+r"(v.r[i + 1]), "+r"(v.r[i + 2]), "+r"(v.r[i + 3]) : "l"(p + i * 4), "r"((uint32_t)(bytes > i * 4)) : "memory");
+            }
+        }
+    }
+    __device__ __forceinline__ const RowsRaw<32>& get(const unsigned char*, int, const unsigned char*, const unsigned char*) { return v; }
+};
+template <> struct Piece<0> {
+    uint32_t w[12];
+    RowsRaw<32> v;
+    // [lo, hi): the array that p points into; aligned words that are not wholly in it are not read as such.
+    __device__ __forceinline__ static bool whole(const unsigned char* p, const unsigned char* lo, const unsigned char* hi)
+    {
+        const uint32_t off = (uint32_t)(uintptr_t)p & 15u;
+        return (p - off >= lo) & (p - off + 48 <= hi);
+    }
+    template <bool kOnce> __device__ __forceinline__ void fetch(const unsigned char* p, int bytes, const unsigned char* lo, const unsigned char* hi)
+    {
+        const uint32_t off = (uint32_t)(uintptr_t)p & 15u;
+        const bool words = bytes > 0 && whole(p, lo, hi);
+        const unsigned char* q = p - off;
+#pragma unroll
+        for (int i = 0; i < 12; ++i) w[i] = 0u;
+#pragma unroll
+        for (int i = 0; i < 12; i += 4)
+            asm volatile("{ .reg .pred q; setp.ne.u32 q, %5, 0; @q ld.global.v4.b32 {%0, %1, %2, %3}, [%4]; }"
+                         : "+r"(w[i]), "+r"(w[i + 1]), "+r"(w[i + 2]), "+r"(w[i + 3])
+                         : "l"(q + i * 4), "r"((uint32_t)(words & (i < 8 || off > 0) & ((int)off + bytes > i * 4))) : "memory");
+    }
+    __device__ __forceinline__ const RowsRaw<32>& get(const unsigned char* p, int bytes, const unsigned char* lo, const unsigned char* hi)
+    {
+        const uint32_t off = (uint32_t)(uintptr_t)p & 15u;
+        if (bytes > 0 && !whole(p, lo, hi)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                v.r[i] = 0u;
+                if (4 * i < bytes) v.r[i] = *reinterpret_cast<const uint16_t*>(p + 4 * i);
+                if (4 * i + 2 < bytes) v.r[i] |= (uint32_t) * reinterpret_cast<const uint16_t*>(p + 4 * i + 2) << 16;
+            }
+            return v;
+        }
+#pragma unroll
+        for (int i = 0; i < 10; ++i) w[i] = off & 8u ? w[i + 2] : w[i];
+#pragma unroll
+        for (int i = 0; i < 9; ++i) w[i] = off & 4u ? w[i + 1] : w[i];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            v.r[i] = __funnelshift_r(w[i], w[i + 1], (off & 3u) * 8u);
+            if (4 * i >= bytes) v.r[i] = 0u;
+            else if (4 * i + 2 >= bytes) v.r[i] &= 0xFFFFu;
+        }
+        return v;
+    }
+};
+
+// ---- matrix instructions ----------------------------------------------------------------------------------------------
+// acc += A B for 16 rows of weights and 8 columns over a block of 128 bytes of each: lane (g, t), g = lane / 4, has piece t of rows g and
+// g + 8 of A and of column g of B.  Which element of a piece is which k of an instruction does not matter, as it is the same for both.
+__device__ __forceinline__ void mma16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, __half)
 {
-    rows_begin();
-    const uint32_t j = blockIdx.x * kWarps + (threadIdx.x >> 5), lane = threadIdx.x & 31u, slot = blockIdx.y;
-    if (j >= H) return;
-    const int32_t e = ids[slot];
-    if ((uint32_t)e >= E) {
-        if (e != -1 && j == 0 && lane == 0) atomicOr(status, PEARL_ST_BAD_INDEX);
-        return;
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, __nv_bfloat16)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma8(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+template <typename E>
+__device__ __forceinline__ void block_product(float (&c)[4], const RowsRaw<32>& a, const RowsRaw<32>& b, const RowsRaw<32>& x)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mma16(c, a.r[2 * i], b.r[2 * i], a.r[2 * i + 1], b.r[2 * i + 1], x.r[2 * i], x.r[2 * i + 1], E());
+}
+// binary32 as the sum of two numbers of 11 bits, each rounded to nearest: what is left out of a product is 2^-22 of it.
+__device__ __forceinline__ void split(RowsRaw<32>& high, RowsRaw<32>& low, const RowsRaw<32>& v)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(high.r[i]) : "f"(__uint_as_float(v.r[i])));
+        const float rest = __uint_as_float(v.r[i]) - __uint_as_float(high.r[i]);
+        asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(low.r[i]) : "f"(rest));
     }
-    const bool gated = act == PEARL_ACT_SILU_GATED;
-    const T* a = x + (uint64_t)(slot / k) * ld_x;
-    const T* g = up + ((uint64_t)(uint32_t)e * (gated ? 2 : 1) * H + j) * D;
-    const T* v = gated ? g + (uint64_t)H * D : g;
-    float sg = 0.0f, sv = 0.0f;
-    for (uint32_t d = lane; d < D; d += 32) {
-        const float f = element(a + d);
-        sg = __fmaf_rn(f, element(g + d), sg);
-        if (gated) sv = __fmaf_rn(f, element(v + d), sv);
-    }
-    sg = layer_warp_sum(sg);
-    sv = layer_warp_sum(sv);
-    if (lane == 0) h[(uint64_t)slot * H + j] = gated ? sg / (1.0f + expf(-sg)) * sv : (sg < 0.0f ? 0.0f : sg);
 }
 
-// y[t, d]: a warp each.
-template <typename T>
-__global__ void __launch_bounds__(kWarps * 32) down_kernel(uint32_t D, uint32_t H, uint32_t E, uint32_t k, const T* down, const float* w, const int32_t* ids,
-                                                           const float* h, T* y, uint64_t ld_y)
+// ---- the experts' products --------------------------------------------------------------------------------------------
+struct Args {
+    uint32_t T, D, H, E, k, act;
+    const unsigned char *x, *up, *down, *h_end, *x_end;
+    uint64_t ld_x, ld_y, pitch;         // bytes
+    const float* w;
+    const int32_t* ids;
+    unsigned char *y, *h;
+    float* z;
+    Counters* n;
+    unsigned* status;
+};
+struct Shared {
+    float part[kWarps][16 * 64];                       // the warps' sums of one strip
+    uint32_t count[PEARL_ROWS_MAX_EXPERTS];            // slots of an expert; then where its next one goes
+    uint16_t expert[PEARL_ROWS_MAX_EXPERTS], first[PEARL_ROWS_MAX_EXPERTS + 1];       // of the experts that are asked for
+    uint16_t slot[kMaxSlots];                          // by expert
+    uint32_t sums[2][kWarps];
+    uint32_t asked, task, last;
+};
+
+// The experts that are asked for, and their slots.
+__device__ void plan(const Args& a, Shared& s)
 {
-    rows_begin();
-    const uint32_t d = blockIdx.x * kWarps + (threadIdx.x >> 5), lane = threadIdx.x & 31u, t = blockIdx.y;
-    if (d >= D) return;
-    float sum = 0.0f;
-    for (uint32_t j = 0; j < k; ++j) {
-        const uint32_t slot = t * k + j;
-        const int32_t e = ids[slot];
-        if ((uint32_t)e >= E) continue;
-        const T* row = down + ((uint64_t)(uint32_t)e * D + d) * H;
-        float s = 0.0f;
-        for (uint32_t i = lane; i < H; i += 32) s = __fmaf_rn(h[(uint64_t)slot * H + i], element(row + i), s);
-        sum = __fmaf_rn(w[slot], layer_warp_sum(s), sum);
+    const uint32_t slots = a.T * a.k, tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5;
+    for (uint32_t e = tid; e < a.E; e += kThreads) s.count[e] = 0;
+    __syncthreads();
+    for (uint32_t i = tid; i < slots; i += kThreads) {
+        const int32_t e = a.ids[i];
+        if ((uint32_t)e < a.E) atomicAdd(&s.count[e], 1u);
+        else if (e != -1 && blockIdx.x == 0) atomicOr(a.status, PEARL_ST_BAD_INDEX);
     }
-    if (lane == 0) y[(uint64_t)t * ld_y + d] = RowsElem<T>::down(sum);
+    __syncthreads();
+    constexpr uint32_t kEach = PEARL_ROWS_MAX_EXPERTS / kThreads;
+    uint32_t mine[kEach], slots_here = 0, asked_here = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < kEach; ++i) {
+        const uint32_t e = tid * kEach + i;
+        mine[i] = e < a.E ? s.count[e] : 0u;
+        slots_here += mine[i];
+        asked_here += mine[i] != 0;
+    }
+    uint32_t slots_to = slots_here, asked_to = asked_here;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t p = __shfl_up_sync(0xFFFFFFFFu, slots_to, o), q = __shfl_up_sync(0xFFFFFFFFu, asked_to, o);
+        if (lane >= (uint32_t)o) { slots_to += p; asked_to += q; }
+    }
+    if (lane == 31) { s.sums[0][warp] = slots_to; s.sums[1][warp] = asked_to; }
+    __syncthreads();
+    uint32_t at = slots_to - slots_here, i_asked = asked_to - asked_here;
+    for (uint32_t w = 0; w < warp; ++w) { at += s.sums[0][w]; i_asked += s.sums[1][w]; }
+#pragma unroll
+    for (uint32_t i = 0; i < kEach; ++i) {
+        const uint32_t e = tid * kEach + i;
+        if (e >= a.E) continue;
+        s.count[e] = at;
+        if (mine[i]) {
+            s.expert[i_asked] = (uint16_t)e;
+            s.first[i_asked] = (uint16_t)at;
+            at += mine[i];
+            ++i_asked;
+        }
+    }
+    if (tid == kThreads - 1) { s.asked = i_asked; s.first[i_asked] = (uint16_t)at; }
+    __syncthreads();
+    for (uint32_t i = tid; i < slots; i += kThreads) {
+        const int32_t e = a.ids[i];
+        if ((uint32_t)e < a.E) s.slot[atomicAdd(&s.count[e], 1u)] = (uint16_t)i;      // (in any order: no sum runs over an expert's slots)
+    }
+    __syncthreads();
+}
+
+__device__ __forceinline__ uint32_t read_acquired(const uint32_t* p)
+{
+    uint32_t v;
+    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+
+// How a product is cut: pieces of `strips` strips of 16 weight rows; `ways` warps share a strip's blocks among them (strips * ways = 8).
+struct Cut {
+    uint32_t blocks, strips, ways, pieces;
+};
+__device__ __forceinline__ Cut cut_of(uint32_t rows, uint32_t row_bytes, uint32_t asked)
+{
+    Cut c;
+    c.blocks = (row_bytes + kBlockBytes - 1) / kBlockBytes;
+    const uint32_t strips = (rows + 15) / 16;
+    // two pieces a CTA where there are that many strips; else a strip is shared, down to a block a warp
+    c.strips = kWarps;
+    while (c.strips > 1 && (uint64_t)strips * asked < 2ull * c.strips * gridDim.x) c.strips /= 2;
+    c.ways = kWarps / c.strips;
+    while (c.ways > 1 && c.ways / 2 >= c.blocks) c.ways /= 2;
+    c.strips = kWarps / c.ways;
+    c.pieces = (strips + c.strips - 1) / c.strips;
+    return c;
+}
+
+__device__ __forceinline__ float activated(float gate, float value) { return gate / (1.0f + expf(-gate)) * value; }
+
+// One piece of a product of expert `i` (of those asked for) with `columns` of its slots from s.slot[first] on.
+template <typename E, int kAlign, int NT, bool kDown>
+__device__ void product(const Args& a, Shared& s, const Cut& c, uint32_t i, uint32_t piece, uint32_t first, uint32_t columns, uint32_t wait_for)
+{
+    constexpr int U = kAlign == 0 ? (NT > 2 ? 1 : 2) : NT == 8 ? 2 : NT == 4 ? 3 : 4;         // blocks on their way
+    constexpr bool k32 = sizeof(E) == 4;
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3u;
+    const uint32_t way = warp % c.ways, strip = piece * c.strips + warp / c.ways;
+    const uint32_t e = s.expert[i];
+    const bool gated = !kDown && a.act == PEARL_ACT_SILU_GATED;
+    const uint32_t length = kDown ? a.H : a.D, rows = kDown ? a.D : a.H;
+    const uint32_t row_bytes = length * (uint32_t)sizeof(E);
+    const uint32_t j0 = strip * (gated ? 8u : 16u), ja = j0 + g, jb = gated ? ja : j0 + 8 + g;
+    const unsigned char* m = kDown ? a.down : a.up;
+    const uint64_t matrix = (uint64_t)rows * (gated ? 2 : 1) * row_bytes;
+    const unsigned char *lo = m, *hi = m + matrix * a.E;
+    const unsigned char* row = m + matrix * e;
+    const unsigned char* pa = row + (uint64_t)ja * row_bytes + t * 32;
+    const unsigned char* pb = row + (uint64_t)(gated ? rows + jb : jb) * row_bytes + t * 32;
+    const int here = (int)row_bytes - (int)(t * 32);
+    const int la = ja < rows ? here : 0, lb = jb < rows ? here : 0;          // bytes from a lane's first piece on
+    Piece<kAlign> wa[U], wb[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int at = (int)((way + u * c.ways) * kBlockBytes);
+        wa[u].template fetch<true>(pa + at, la - at, lo, hi);
+        wb[u].template fetch<true>(pb + at, lb - at, lo, hi);
+    }
+    if constexpr (kDown) {
+        // h: wait for the expert's first product
+        if (wait_for && threadIdx.x == 0) {
+            uint32_t spins = 0;
+            while (read_acquired(&a.n->up[i]) < wait_for)
+                if (++spins > kSpins) { atomicOr(a.status, PEARL_ST_INTERNAL); break; }
+            __threadfence();
+        }
+        __syncthreads();
+    }
+    const unsigned char* px[NT];
+    int lx[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const uint32_t col = n * 8 + g;
+        const uint32_t slot = col < columns ? s.slot[first + col] : 0u;
+        px[n] = (kDown ? a.h + slot * a.pitch : a.x + (uint64_t)(slot / a.k) * a.ld_x) + t * 32;
+        lx[n] = col < columns ? here : 0;
+    }
+    const unsigned char *xlo = kDown ? a.h : a.x, *xhi = kDown ? a.h_end : a.x_end;
+    float acc[NT][4];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) acc[n][q] = 0.0f;
+    for (uint32_t b0 = way; b0 < c.blocks; b0 += U * c.ways) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t block = b0 + u * c.ways;
+            if (block >= c.blocks) break;
+            const int at = (int)(block * kBlockBytes), next = at + (int)(U * c.ways * kBlockBytes);
+            const RowsRaw<32> va = wa[u].get(pa + at, la - at, lo, hi), vb = wb[u].get(pb + at, lb - at, lo, hi);
+            if (block + U * c.ways < c.blocks) {
+                wa[u].template fetch<true>(pa + next, la - next, lo, hi);
+                wb[u].template fetch<true>(pb + next, lb - next, lo, hi);
+            }
+            if constexpr (k32) {
+                RowsRaw<32> ah, al, bh, bl;
+                split(ah, al, va);
+                split(bh, bl, vb);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    if (n > 0 && n * 8 >= (int)columns) break;
+                    Piece<kAlign> x;
+                    x.template fetch<false>(px[n] + at, lx[n] - at, xlo, xhi);
+                    RowsRaw<32> xh, xl;
+                    split(xh, xl, x.get(px[n] + at, lx[n] - at, xlo, xhi));
+                    float part[4] = { 0.0f, 0.0f, 0.0f, 0.0f };     // (the instruction cuts off where an addition rounds: sums of a block only)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        mma8(part, al.r[2 * q], bl.r[2 * q], al.r[2 * q + 1], bl.r[2 * q + 1], xh.r[2 * q], xh.r[2 * q + 1]);
+                        mma8(part, ah.r[2 * q], bh.r[2 * q], ah.r[2 * q + 1], bh.r[2 * q + 1], xl.r[2 * q], xl.r[2 * q + 1]);
+                        mma8(part, ah.r[2 * q], bh.r[2 * q], ah.r[2 * q + 1], bh.r[2 * q + 1], xh.r[2 * q], xh.r[2 * q + 1]);
+                    }
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) acc[n][q] += part[q];
+                }
+            } else {
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    if (n > 0 && n * 8 >= (int)columns) break;
+                    Piece<kAlign> x;
+                    x.template fetch<false>(px[n] + at, lx[n] - at, xlo, xhi);
+                    if constexpr (kDown) {
+                        Piece<kAlign> low;
+                        low.template fetch<false>(px[n] + a.pitch / 2 + at, lx[n] - at, xlo, xhi);
+                        block_product<E>(acc[n], va, vb, x.get(px[n] + at, lx[n] - at, xlo, xhi));
+                        block_product<E>(acc[n], va, vb, low.get(px[n] + a.pitch / 2 + at, lx[n] - at, xlo, xhi));
+                    } else {
+                        block_product<E>(acc[n], va, vb, x.get(px[n] + at, lx[n] - at, xlo, xhi));
+                    }
+                }
+            }
+        }
+    }
+    // the warps that share a strip: their sums in order
+    if (c.ways > 1) {
+        float* mine = s.part[warp] + lane * 4;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) *reinterpret_cast<float4*>(mine + n * 128) = make_float4(acc[n][0], acc[n][1], acc[n][2], acc[n][3]);
+        __syncthreads();
+        if (way == 0) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+                for (uint32_t w = 1; w < c.ways; ++w) {
+                    const float4 v = *reinterpret_cast<const float4*>(s.part[warp + w] + lane * 4 + n * 128);
+                    acc[n][0] += v.x; acc[n][1] += v.y; acc[n][2] += v.z; acc[n][3] += v.w;
+                }
+        }
+    }
+    if (way == 0) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const uint32_t col = n * 8 + t * 2 + q;
+                if (col >= columns) continue;
+                const uint32_t slot = s.slot[first + col];
+                if constexpr (kDown) {
+                    float* z = a.z + (uint64_t)slot * a.D;
+                    if (ja < rows) z[ja] = acc[n][q];
+                    if (jb < rows) z[jb] = acc[n][q + 2];
+                } else {
+                    const auto store = [&](uint32_t j, float v) {
+                        if (j >= rows) return;
+                        if constexpr (k32) {
+                            reinterpret_cast<float*>(a.h + slot * a.pitch)[j] = v;
+                        } else {
+                            // as the sum of two: a single one would be off by as much as the result's own rounding
+                            const E high = RowsElem<E>::down(v);
+                            const float rest = v - RowsElem<E>::up(high);
+                            reinterpret_cast<E*>(a.h + slot * a.pitch)[j] = high;
+                            reinterpret_cast<E*>(a.h + slot * a.pitch + a.pitch / 2)[j] = RowsElem<E>::down(isfinite(RowsElem<E>::up(high)) ? rest : 0.0f);
+                        }
+                    };
+                    if (gated) {
+                        store(ja, activated(acc[n][q], acc[n][q + 2]));
+                    } else {
+                        store(ja, acc[n][q] < 0.0f ? 0.0f : acc[n][q]);
+                        store(jb, acc[n][q + 2] < 0.0f ? 0.0f : acc[n][q + 2]);
+                    }
+                }
+            }
+    }
+}
+
+template <typename E, int kAlign, bool kDown>
+__device__ void product_of(const Args& a, Shared& s, const Cut& c, uint32_t i, uint32_t piece, uint32_t wait_for)
+{
+    const uint32_t end = s.first[i + 1];
+    for (uint32_t first = s.first[i]; first < end; first += 64) {
+        const uint32_t columns = end - first < 64 ? end - first : 64;
+        if (columns <= 8) product<E, kAlign, 1, kDown>(a, s, c, i, piece, first, columns, wait_for);
+        else if (columns <= 16) product<E, kAlign, 2, kDown>(a, s, c, i, piece, first, columns, wait_for);
+        else if (columns <= 32) product<E, kAlign, 4, kDown>(a, s, c, i, piece, first, columns, wait_for);
+        else product<E, kAlign, 8, kDown>(a, s, c, i, piece, first, columns, wait_for);
+        wait_for = 0;
+        __syncthreads();
+    }
+}
+
+// Pieces are taken in order, the first products' before the second ones'.  A CTA waits for an expert's first product only with
+// pieces of its own already taken, and each of those it waits for is with a CTA that runs: nobody waits for one that is yet to be launched.
+template <typename E, int kAlign>
+__global__ void __launch_bounds__(kThreads, 2) experts_kernel(Args a)
+{
+    extern __shared__ __align__(16) unsigned char memory[];
+    Shared& s = *reinterpret_cast<Shared*>(memory);
+    rows_begin();
+    plan(a, s);
+    const uint32_t asked = s.asked;
+    const bool gated = a.act == PEARL_ACT_SILU_GATED;
+    const Cut up = cut_of(gated ? a.H * 2 : a.H, a.D * (uint32_t)sizeof(E), asked), down = cut_of(a.D, a.H * (uint32_t)sizeof(E), asked);
+    const uint32_t ups = asked * up.pieces, all = ups + asked * down.pieces;
+    if (asked == 0)
+        for (uint64_t i = (uint64_t)blockIdx.x * kThreads + threadIdx.x; i < (uint64_t)a.T * a.D; i += (uint64_t)gridDim.x * kThreads)
+            reinterpret_cast<E*>(a.y + i / a.D * a.ld_y)[i % a.D] = RowsElem<E>::down(0.0f);
+    for (;;) {
+        if (threadIdx.x == 0) s.task = atomicAdd(&a.n->ticket, 1u);
+        __syncthreads();
+        const uint32_t task = s.task;
+        __syncthreads();
+        if (task >= all) break;
+        if (task < ups) {
+            const uint32_t i = task / up.pieces;
+            product_of<E, kAlign, false>(a, s, up, i, task - i * up.pieces, 0);
+            __threadfence();
+            __syncthreads();
+            if (threadIdx.x == 0) atomicAdd(&a.n->up[i], 1u);
+            continue;
+        }
+        const uint32_t i = (task - ups) / down.pieces, piece = task - ups - i * down.pieces;
+        product_of<E, kAlign, true>(a, s, down, i, piece, up.pieces);
+        __threadfence();
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            s.last = atomicAdd(&a.n->down[piece], 1u) + 1 == asked;
+            __threadfence();
+        }
+        __syncthreads();
+        if (!s.last) continue;
+        // every expert is through with these columns of y
+        const uint32_t d0 = piece * down.strips * 16, cols = min(down.strips * 16, a.D - d0);
+        for (uint32_t n = threadIdx.x; n < a.T * cols; n += kThreads) {
+            const uint32_t t = n / cols, d = d0 + n - t * cols;
+            float sum = 0.0f;
+            for (uint32_t j = 0; j < a.k; ++j) {
+                const uint32_t slot = t * a.k + j;
+                if ((uint32_t)a.ids[slot] < a.E) sum = __fmaf_rn(a.w[slot], a.z[(uint64_t)slot * a.D + d], sum);
+            }
+            reinterpret_cast<E*>(a.y + t * a.ld_y)[d] = RowsElem<E>::down(sum);
+        }
+    }
+    // the last one out leaves the counters as they were
+    if (threadIdx.x == 0) s.last = atomicAdd(&a.n->finished, 1u) + 1 == gridDim.x;
+    __syncthreads();
+    if (!s.last) return;
+    for (uint32_t i = threadIdx.x; i < asked; i += kThreads) a.n->up[i] = 0;
+    for (uint32_t i = threadIdx.x; i < down.pieces; i += kThreads) a.n->down[i] = 0;
+    if (threadIdx.x == 0) a.n->ticket = a.n->finished = 0;
+}
+
+template <typename T, int kAlign> int experts_launch(const Args& a, cudaStream_t s)
+{
+    static std::atomic<bool> ready[kRowsMaxDevices];
+    const int dev = rows_device();
+    if (dev < 0 || !ready[dev]) {
+        if (cudaFuncSetAttribute(experts_kernel<T, kAlign>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Shared)) != cudaSuccess) return -1;
+        if (dev >= 0) ready[dev] = true;
+    }
+    return rows_launch(experts_kernel<T, kAlign>, dim3(2 * rows_sm_count()), dim3(kThreads), sizeof(Shared), s, 0, a);
 }
 
 template <typename T> int experts_as(unsigned* status, const LayerExperts& a, cudaStream_t s)
 {
     const Layout l = layout_of(a.T, a.D, a.H, a.E, a.k);
-    float *logits = (float*)((char*)a.work + l.logits), *h = (float*)((char*)a.work + l.h);
+    float* logits = (float*)((char*)a.work + l.logits);
     int n = 0, m;
     if (a.router) {
-        if ((m = rows_launch(logits_kernel<T>, dim3((a.T * a.E + kWarps - 1) / kWarps), dim3(kWarps * 32), 0, s, 0, a.T, a.D, a.E, (const T*)a.x,
-                             a.ld_x, (const T*)a.router, logits)) < 0) return m;
+        if ((m = rows_launch(logits_kernel<T>, dim3((a.T * a.E + kWarps - 1) / kWarps), dim3(kThreads), 0, s, 0, a.T, a.D, a.E, (const T*)a.x, a.ld_x,
+                             (const T*)a.router, logits)) < 0) return m;
         n += m;
         if ((m = rows_launch_route(status, a.T, a.E, a.k, PEARL_F32, logits, a.E, a.over_chosen, a.w, a.ids, s)) < 0) return m;
         n += m;
     }
-    if ((m = rows_launch(up_kernel<T>, dim3((a.H + kWarps - 1) / kWarps, a.T * a.k), dim3(kWarps * 32), 0, s, 0, status, a.D, a.H, a.E, a.k, a.act,
-                         (const T*)a.x, a.ld_x, (const T*)a.up, (const int32_t*)a.ids, h)) < 0) return m;
-    n += m;
-    if ((m = rows_launch(down_kernel<T>, dim3((a.D + kWarps - 1) / kWarps, a.T), dim3(kWarps * 32), 0, s, 0, a.D, a.H, a.E, a.k, (const T*)a.down,
-                         (const float*)a.w, (const int32_t*)a.ids, (const float*)h, (T*)a.y, a.ld_y)) < 0) return m;
-    return n + m;
+    constexpr uint32_t S = sizeof(T);
+    unsigned char* work = (unsigned char*)a.work;
+    const unsigned char* x = (const unsigned char*)a.x;
+    const Args args = { a.T, a.D, a.H, a.E, a.k, a.act, x, (const unsigned char*)a.up, (const unsigned char*)a.down, work + l.z,
+                        x + ((uint64_t)(a.T - 1) * a.ld_x + a.D) * S, a.ld_x * S, a.ld_y * S, l.pitch, a.w, a.ids, (unsigned char*)a.y, work + l.h,
+                        (float*)(work + l.z), (Counters*)work, status };
+    const uint32_t granule = rows_granule((uintptr_t)a.x | (uintptr_t)a.up, (uintptr_t)a.down, a.ld_x * S, (uint64_t)a.D * S, (uint64_t)a.H * S);
+    m = granule >= 32 ? experts_launch<T, 32>(args, s) : granule >= 16 ? experts_launch<T, 16>(args, s) : experts_launch<T, 0>(args, s);
+    return m < 0 ? m : n + m;
 }
 
 }  // namespace
