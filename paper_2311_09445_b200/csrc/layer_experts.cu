@@ -52,36 +52,40 @@ __global__ void __launch_bounds__(kThreads) logits_kernel(uint32_t rows, uint32_
 }
 
 // ---- 32 bytes of a row ---------------------------------------------------------------------------------------------
-// A piece: 16 (or 8) elements of a row, of which the first n are there; the others are 0.  kAlign: what rows and their lengths are multiples
-// of, 32 or 16 bytes; 0: nothing, the piece comes out of the aligned words around it.
+// v = the `bytes` bytes from byte `off` of w on, zeros behind them.
+__device__ __forceinline__ void shifted(RowsRaw<32>& v, uint32_t (&w)[12], uint32_t off, int bytes)
+{
+#pragma unroll
+    for (int i = 0; i < 10; ++i) w[i] = off & 8u ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i < 9; ++i) w[i] = off & 4u ? w[i + 1] : w[i];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        v.r[i] = __funnelshift_r(w[i], w[i + 1], (off & 3u) * 8u);
+        if (4 * i >= bytes) v.r[i] = 0u;
+        else if (4 * i + 2 >= bytes) v.r[i] &= 0xFFFFu;
+    }
+}
+
+// A lane's piece of a row of x or h: 16 (or 8) elements, of which the first `bytes` bytes are there; the others are 0.  These rows are read
+// again and again, by all warps, and stay in the L1.  kAlign: what rows and their lengths are multiples of, 32 or 16 bytes; 0: nothing, the
+// piece comes out of the aligned words around it.
 template <int kAlign> struct Piece {
     RowsRaw<32> v;
-    __device__ __forceinline__ void clear()
+    __device__ __forceinline__ void fetch(const unsigned char* p, int bytes, const unsigned char*, const unsigned char*)
     {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v.r[i] = 0u;
-    }
-    template <bool kOnce> __device__ __forceinline__ void fetch(const unsigned char* p, int bytes, const unsigned char*, const unsigned char*)
-    {
-        clear();
         if constexpr (kAlign == 32) {
-            if constexpr (kOnce) {
-                rows_load_if<false>(bytes > 0, v, p);
-            } else {
-                asm volatile("{ .reg .pred q; setp.ne.u32 q, %9, 0; @q ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8]; }"
-                             : "+r"(v.r[0]), "+r"(v.r[1]), "+r"(v.r[2]), "+r"(v.r[3]), "+r"(v.r[4]), "+r"(v.r[5]), "+r"(v.r[6]), "+r"(v.r[7])
-                             : "l"(p), "r"((uint32_t)(bytes > 0)) : "memory");
-            }
+            asm volatile("{ .reg .pred q; setp.ne.u32 q, %9, 0; @q ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8]; }"
+                         : "+r"(v.r[0]), "+r"(v.r[1]), "+r"(v.r[2]), "+r"(v.r[3]), "+r"(v.r[4]), "+r"(v.r[5]), "+r"(v.r[6]), "+r"(v.r[7])
+                         : "l"(p), "r"((uint32_t)(bytes > 0)) : "memory");
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; i += 4) {
-                if constexpr (kOnce)
-                    asm volatile("{ .reg .pred q; setp.ne.u32 q, %5, 0; @q ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4]; }"
-                                 : "+r"(v.r[i]), "+r"(v.r[i + 1]), "+r"(v.r[i + 2]), "+r"(v.r[i + 3]) : "l"(p + i * 4), "r"((uint32_t)(bytes > i * 4)));
-                else
-                    asm volatile("{ .reg .pred q; setp.ne.u32 q, %5, 0; @q ld.global.v4.b32 {%0, %1, %2, %3}, [%4]; }"
-                                 : "+r"(v.r[i]), "+r"(v.r[i + 1]), "+r"(v.r[i + 2]), "+r"(v.r[i + 3]) : "l"(p + i * 4), "r"((uint32_t)(bytes > i * 4)) : "memory");
-            }
+            for (int i = 0; i < 8; i += 4)
+                asm volatile("{ .reg .pred q; setp.ne.u32 q, %5, 0; @q ld.global.v4.b32 {%0, %1, %2, %3}, [%4]; }"
+                             : "+r"(v.r[i]), "+r"(v.r[i + 1]), "+r"(v.r[i + 2]), "+r"(v.r[i + 3])
+                             : "l"(p + i * 4), "r"((uint32_t)(bytes > i * 4)) : "memory");
         }
     }
     __device__ __forceinline__ const RowsRaw<32>& get(const unsigned char*, int, const unsigned char*, const unsigned char*) { return v; }
@@ -95,40 +99,29 @@ template <> struct Piece<0> {
         const uint32_t off = (uint32_t)(uintptr_t)p & 15u;
         return (p - off >= lo) & (p - off + 48 <= hi);
     }
-    template <bool kOnce> __device__ __forceinline__ void fetch(const unsigned char* p, int bytes, const unsigned char* lo, const unsigned char* hi)
+    __device__ __forceinline__ void fetch(const unsigned char* p, int bytes, const unsigned char* lo, const unsigned char* hi)
     {
         const uint32_t off = (uint32_t)(uintptr_t)p & 15u;
         const bool words = bytes > 0 && whole(p, lo, hi);
-        const unsigned char* q = p - off;
 #pragma unroll
         for (int i = 0; i < 12; ++i) w[i] = 0u;
 #pragma unroll
         for (int i = 0; i < 12; i += 4)
             asm volatile("{ .reg .pred q; setp.ne.u32 q, %5, 0; @q ld.global.v4.b32 {%0, %1, %2, %3}, [%4]; }"
                          : "+r"(w[i]), "+r"(w[i + 1]), "+r"(w[i + 2]), "+r"(w[i + 3])
-                         : "l"(q + i * 4), "r"((uint32_t)(words & (i < 8 || off > 0) & ((int)off + bytes > i * 4))) : "memory");
+                         : "l"(p - off + i * 4), "r"((uint32_t)(words & (i < 8 || off > 0) & ((int)off + bytes > i * 4))) : "memory");
     }
     __device__ __forceinline__ const RowsRaw<32>& get(const unsigned char* p, int bytes, const unsigned char* lo, const unsigned char* hi)
     {
-        const uint32_t off = (uint32_t)(uintptr_t)p & 15u;
-        if (bytes > 0 && !whole(p, lo, hi)) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                v.r[i] = 0u;
-                if (4 * i < bytes) v.r[i] = *reinterpret_cast<const uint16_t*>(p + 4 * i);
-                if (4 * i + 2 < bytes) v.r[i] |= (uint32_t) * reinterpret_cast<const uint16_t*>(p + 4 * i + 2) << 16;
-            }
+        if (bytes <= 0 || whole(p, lo, hi)) {
+            shifted(v, w, (uint32_t)(uintptr_t)p & 15u, bytes);
             return v;
         }
 #pragma unroll
-        for (int i = 0; i < 10; ++i) w[i] = off & 8u ? w[i + 2] : w[i];
-#pragma unroll
-        for (int i = 0; i < 9; ++i) w[i] = off & 4u ? w[i + 1] : w[i];
-#pragma unroll
         for (int i = 0; i < 8; ++i) {
-            v.r[i] = __funnelshift_r(w[i], w[i + 1], (off & 3u) * 8u);
-            if (4 * i >= bytes) v.r[i] = 0u;
-            else if (4 * i + 2 >= bytes) v.r[i] &= 0xFFFFu;
+            v.r[i] = 0u;
+            if (4 * i < bytes) v.r[i] = *reinterpret_cast<const uint16_t*>(p + 4 * i);
+            if (4 * i + 2 < bytes) v.r[i] |= (uint32_t) * reinterpret_cast<const uint16_t*>(p + 4 * i + 2) << 16;
         }
         return v;
     }
@@ -172,7 +165,7 @@ __device__ __forceinline__ void split(RowsRaw<32>& high, RowsRaw<32>& low, const
 // ---- the experts' products --------------------------------------------------------------------------------------------
 struct Args {
     uint32_t T, D, H, E, k, act;
-    const unsigned char *x, *up, *down, *h_end, *x_end;
+    const unsigned char *x, *x_end, *up, *up_end, *down, *down_end, *h_end;
     uint64_t ld_x, ld_y, pitch;         // bytes
     const float* w;
     const int32_t* ids;
@@ -181,13 +174,17 @@ struct Args {
     Counters* n;
     unsigned* status;
 };
+// A warp's ring: stages of 16 rows of 128 bytes, 16 bytes more a row, which spreads the rows over the banks (and holds the rest of a row that
+// starts between two words).
+constexpr uint32_t kStages = 4, kPitch = kBlockBytes + 16, kStageBytes = 16 * kPitch;
 struct Shared {
-    float part[kWarps][16 * 64];                       // the warps' sums of one strip
+    unsigned char ring[kWarps][kStages][kStageBytes];
+    float part[kWarps][2 * 128];                       // the warps' sums of 16 columns of one strip
     uint32_t count[PEARL_ROWS_MAX_EXPERTS];            // slots of an expert; then where its next one goes
     uint16_t expert[PEARL_ROWS_MAX_EXPERTS], first[PEARL_ROWS_MAX_EXPERTS + 1];       // of the experts that are asked for
     uint16_t slot[kMaxSlots];                          // by expert
     uint32_t sums[2][kWarps];
-    uint32_t asked, task, last;
+    uint32_t asked, task[2], last;
 };
 
 // The experts that are asked for, and their slots.
@@ -270,39 +267,120 @@ __device__ __forceinline__ Cut cut_of(uint32_t rows, uint32_t row_bytes, uint32_
 
 __device__ __forceinline__ float activated(float gate, float value) { return gate / (1.0f + expf(-gate)) * value; }
 
-// One piece of a product of expert `i` (of those asked for) with `columns` of its slots from s.slot[first] on.
-template <typename E, int kAlign, int NT, bool kDown>
-__device__ void product(const Args& a, Shared& s, const Cut& c, uint32_t i, uint32_t piece, uint32_t first, uint32_t columns, uint32_t wait_for)
+// What a warp works on: a strip of 16 weight rows of one expert, with some of its slots.
+struct Item {
+    uint32_t i, piece, first, columns;          // the expert's place among those asked for; of its slots
+    bool down, any;
+};
+
+// The weight rows of an item's strip, as the lanes copy them: lane l has word l % 8 of rows l / 8 + 4 q of a block.
+template <typename E, int kAlign>
+struct Strip {
+    const unsigned char *low, *high;            // row 0's and row 8's first byte
+    uint32_t row_bytes, blocks, rows_low, rows_high;    // rows that there are, of the first and of the last 8
+    __device__ __forceinline__ Strip(const Args& a, const Shared& s, const Cut& c, const Item& it)
+    {
+        const bool gated = !it.down && a.act == PEARL_ACT_SILU_GATED;
+        const uint32_t rows = it.down ? a.D : a.H, strip = it.piece * c.strips + (threadIdx.x >> 5) / c.ways;
+        row_bytes = (it.down ? a.H : a.D) * (uint32_t)sizeof(E);
+        blocks = c.blocks;
+        const uint32_t j = strip * (gated ? 8u : 16u), k = gated ? j : j + 8;
+        const unsigned char* m = (it.down ? a.down : a.up) + (uint64_t)s.expert[it.i] * rows * (gated ? 2 : 1) * row_bytes;
+        low = m + (uint64_t)j * row_bytes;
+        high = m + (uint64_t)(gated ? rows + k : k) * row_bytes;
+        rows_low = j < rows ? min(rows - j, 8u) : 0u;
+        rows_high = k < rows ? min(rows - k, 8u) : 0u;
+    }
+    // Starts the copy of a block of the strip to a stage; what is not there becomes 0.
+    __device__ __forceinline__ void copy(const Args& a, const Item& it, uint32_t block, unsigned char* stage) const
+    {
+        const uint32_t lane = threadIdx.x & 31u;
+        constexpr uint32_t kWords = kPitch / 16;
+        if (block >= blocks) {
+        } else if constexpr (kAlign != 0) {
+            const uint32_t r = lane >> 3, at = block * kBlockBytes + (lane & 7u) * 16;
+            unsigned char* to = stage + r * kPitch + (lane & 7u) * 16;
+#pragma unroll
+            for (uint32_t q = 0; q < 4; ++q) {
+                const uint32_t row = r + q % 2 * 4;
+                const bool there = at < row_bytes && row < (q < 2 ? rows_low : rows_high);
+                word(a.status, to + q * 4 * kPitch, (q < 2 ? low : high) + (uint64_t)row * row_bytes + at, there ? 16u : 0u, it.down ? a.down : a.up,
+                     it.down ? a.down_end : a.up_end);
+            }
+        } else {
+            const unsigned char *lo = it.down ? a.down : a.up, *hi = it.down ? a.down_end : a.up_end;
+#pragma unroll
+            for (uint32_t q = 0; q < (16 * kWords + 31) / 32; ++q) {
+                const uint32_t n = lane + q * 32, row = n / kWords, w = n - row * kWords;
+                if (row >= 16) break;
+                const unsigned char* from = (row < 8 ? low : high) + (uint64_t)(row & 7u) * row_bytes;
+                const unsigned char* p = from - ((uintptr_t)from & 15u) + block * kBlockBytes + w * 16;
+                const bool there = (row & 7u) < (row < 8 ? rows_low : rows_high) && p < from + row_bytes;
+                unsigned char* to = stage + row * kPitch + w * 16;
+                if (there && p < lo) {                       // the array's first word, of which a part is not its own
+                    for (int b = 0; b < 16; b += 2)
+                        *reinterpret_cast<uint16_t*>(to + b) = p + b >= lo && p + b < hi ? *reinterpret_cast<const uint16_t*>(p + b) : (uint16_t)0;
+                    continue;
+                }
+                word(a.status, to, p, !there ? 0u : hi - p < 16 ? (uint32_t)(hi - p) : 16u, lo, hi);
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    // `bytes` bytes (1 .. 16) of the array [lo, hi) and zeros behind them, or 16 zeros.
+    __device__ __forceinline__ static void word(unsigned* status, unsigned char* to, const unsigned char* from, uint32_t bytes, const unsigned char* lo,
+                                                const unsigned char* hi)
+    {
+        if (bytes && ROWS_IN_ARRAY(status, from, bytes, lo, hi))
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "r"(bytes) : "memory");
+        else
+            *reinterpret_cast<uint4*>(to) = make_uint4(0, 0, 0, 0);
+    }
+    // The lane's piece of row g of the stage (g + 8 with `upper`), of which `bytes` are there.
+    __device__ __forceinline__ RowsRaw<32> piece(const unsigned char* stage, bool upper, int bytes) const
+    {
+        const uint32_t lane = threadIdx.x & 31u, g = lane >> 2, t = lane & 3u;
+        const uint4* p = reinterpret_cast<const uint4*>(stage + (g + (upper ? 8 : 0)) * kPitch + t * 32);
+        RowsRaw<32> v;
+        if constexpr (kAlign != 0) {
+            const uint4 x = p[0], y = p[1];
+            v.r[0] = x.x; v.r[1] = x.y; v.r[2] = x.z; v.r[3] = x.w; v.r[4] = y.x; v.r[5] = y.y; v.r[6] = y.z; v.r[7] = y.w;
+        } else {
+            const uint32_t off = (uint32_t)(uintptr_t)((upper ? high : low) + (uint64_t)g * row_bytes) & 15u;
+            const uint4 x = p[0], y = p[1], z = p[2];
+            uint32_t w[12] = { x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w, z.x, z.y, z.z, z.w };
+            shifted(v, w, off, bytes);
+        }
+        return v;
+    }
+};
+
+// Starts an item's first blocks.
+template <typename E, int kAlign> __device__ __forceinline__ void start(const Args& a, Shared& s, const Cut& c, const Item& it)
 {
-    constexpr int U = kAlign == 0 ? (NT > 2 ? 1 : 2) : NT == 8 ? 2 : NT == 4 ? 3 : 4;         // blocks on their way
+    const uint32_t warp = threadIdx.x >> 5, way = warp % c.ways;
+    const Strip<E, kAlign> strip(a, s, c, it);
+#pragma unroll
+    for (uint32_t u = 0; u + 1 < kStages; ++u) strip.copy(a, it, way + u * c.ways, s.ring[warp][u]);
+}
+
+// One item's product; its first blocks are on their way.  next() names the item to start as soon as the ring is free.
+template <typename E, int kAlign, int NT, bool kDown, typename Next>
+__device__ void product(const Args& a, Shared& s, const Cut& c, const Item& it, uint32_t wait_for, Next next)
+{
     constexpr bool k32 = sizeof(E) == 4;
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3u;
-    const uint32_t way = warp % c.ways, strip = piece * c.strips + warp / c.ways;
-    const uint32_t e = s.expert[i];
+    const uint32_t way = warp % c.ways;
     const bool gated = !kDown && a.act == PEARL_ACT_SILU_GATED;
-    const uint32_t length = kDown ? a.H : a.D, rows = kDown ? a.D : a.H;
-    const uint32_t row_bytes = length * (uint32_t)sizeof(E);
-    const uint32_t j0 = strip * (gated ? 8u : 16u), ja = j0 + g, jb = gated ? ja : j0 + 8 + g;
-    const unsigned char* m = kDown ? a.down : a.up;
-    const uint64_t matrix = (uint64_t)rows * (gated ? 2 : 1) * row_bytes;
-    const unsigned char *lo = m, *hi = m + matrix * a.E;
-    const unsigned char* row = m + matrix * e;
-    const unsigned char* pa = row + (uint64_t)ja * row_bytes + t * 32;
-    const unsigned char* pb = row + (uint64_t)(gated ? rows + jb : jb) * row_bytes + t * 32;
-    const int here = (int)row_bytes - (int)(t * 32);
-    const int la = ja < rows ? here : 0, lb = jb < rows ? here : 0;          // bytes from a lane's first piece on
-    Piece<kAlign> wa[U], wb[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int at = (int)((way + u * c.ways) * kBlockBytes);
-        wa[u].template fetch<true>(pa + at, la - at, lo, hi);
-        wb[u].template fetch<true>(pb + at, lb - at, lo, hi);
-    }
+    const uint32_t rows = kDown ? a.D : a.H;
+    const uint32_t j0 = (it.piece * c.strips + warp / c.ways) * (gated ? 8u : 16u), ja = j0 + g, jb = gated ? ja : j0 + 8 + g;
+    const Strip<E, kAlign> strip(a, s, c, it);
+    const int here = (int)strip.row_bytes - (int)(t * 32);       // bytes from a lane's first piece on
     if constexpr (kDown) {
         // h: wait for the expert's first product
         if (wait_for && threadIdx.x == 0) {
             uint32_t spins = 0;
-            while (read_acquired(&a.n->up[i]) < wait_for)
+            while (read_acquired(&a.n->up[it.i]) < wait_for)
                 if (++spins > kSpins) { atomicOr(a.status, PEARL_ST_INTERNAL); break; }
             __threadfence();
         }
@@ -313,9 +391,9 @@ __device__ void product(const Args& a, Shared& s, const Cut& c, uint32_t i, uint
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const uint32_t col = n * 8 + g;
-        const uint32_t slot = col < columns ? s.slot[first + col] : 0u;
+        const uint32_t slot = col < it.columns ? s.slot[it.first + col] : 0u;
         px[n] = (kDown ? a.h + slot * a.pitch : a.x + (uint64_t)(slot / a.k) * a.ld_x) + t * 32;
-        lx[n] = col < columns ? here : 0;
+        lx[n] = col < it.columns ? here : 0;
     }
     const unsigned char *xlo = kDown ? a.h : a.x, *xhi = kDown ? a.h_end : a.x_end;
     float acc[NT][4];
@@ -323,67 +401,67 @@ __device__ void product(const Args& a, Shared& s, const Cut& c, uint32_t i, uint
     for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int q = 0; q < 4; ++q) acc[n][q] = 0.0f;
-    for (uint32_t b0 = way; b0 < c.blocks; b0 += U * c.ways) {
+    uint32_t stage = 0;
+    for (uint32_t block = way; block < c.blocks; block += c.ways) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+        __syncwarp();
+        const int at = (int)(block * kBlockBytes);
+        strip.copy(a, it, block + (kStages - 1) * c.ways, s.ring[warp][(stage + kStages - 1) % kStages]);
+        const RowsRaw<32> va = strip.piece(s.ring[warp][stage], false, here - at), vb = strip.piece(s.ring[warp][stage], true, here - at);
+        stage = (stage + 1) % kStages;
+        if constexpr (k32) {
+            RowsRaw<32> ah, al, bh, bl;
+            split(ah, al, va);
+            split(bh, bl, vb);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const uint32_t block = b0 + u * c.ways;
-            if (block >= c.blocks) break;
-            const int at = (int)(block * kBlockBytes), next = at + (int)(U * c.ways * kBlockBytes);
-            const RowsRaw<32> va = wa[u].get(pa + at, la - at, lo, hi), vb = wb[u].get(pb + at, lb - at, lo, hi);
-            if (block + U * c.ways < c.blocks) {
-                wa[u].template fetch<true>(pa + next, la - next, lo, hi);
-                wb[u].template fetch<true>(pb + next, lb - next, lo, hi);
-            }
-            if constexpr (k32) {
-                RowsRaw<32> ah, al, bh, bl;
-                split(ah, al, va);
-                split(bh, bl, vb);
+            for (int n = 0; n < NT; ++n) {
+                if (n > 0 && n * 8 >= (int)it.columns) break;
+                Piece<kAlign> x;
+                x.fetch(px[n] + at, lx[n] - at, xlo, xhi);
+                RowsRaw<32> xh, xl;
+                split(xh, xl, x.get(px[n] + at, lx[n] - at, xlo, xhi));
+                float part[4] = { 0.0f, 0.0f, 0.0f, 0.0f };     // (the instruction cuts off where an addition rounds: sums of a block only)
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    if (n > 0 && n * 8 >= (int)columns) break;
-                    Piece<kAlign> x;
-                    x.template fetch<false>(px[n] + at, lx[n] - at, xlo, xhi);
-                    RowsRaw<32> xh, xl;
-                    split(xh, xl, x.get(px[n] + at, lx[n] - at, xlo, xhi));
-                    float part[4] = { 0.0f, 0.0f, 0.0f, 0.0f };     // (the instruction cuts off where an addition rounds: sums of a block only)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        mma8(part, al.r[2 * q], bl.r[2 * q], al.r[2 * q + 1], bl.r[2 * q + 1], xh.r[2 * q], xh.r[2 * q + 1]);
-                        mma8(part, ah.r[2 * q], bh.r[2 * q], ah.r[2 * q + 1], bh.r[2 * q + 1], xl.r[2 * q], xl.r[2 * q + 1]);
-                        mma8(part, ah.r[2 * q], bh.r[2 * q], ah.r[2 * q + 1], bh.r[2 * q + 1], xh.r[2 * q], xh.r[2 * q + 1]);
-                    }
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) acc[n][q] += part[q];
+                for (int q = 0; q < 4; ++q) {
+                    mma8(part, al.r[2 * q], bl.r[2 * q], al.r[2 * q + 1], bl.r[2 * q + 1], xh.r[2 * q], xh.r[2 * q + 1]);
+                    mma8(part, ah.r[2 * q], bh.r[2 * q], ah.r[2 * q + 1], bh.r[2 * q + 1], xl.r[2 * q], xl.r[2 * q + 1]);
+                    mma8(part, ah.r[2 * q], bh.r[2 * q], ah.r[2 * q + 1], bh.r[2 * q + 1], xh.r[2 * q], xh.r[2 * q + 1]);
                 }
-            } else {
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    if (n > 0 && n * 8 >= (int)columns) break;
-                    Piece<kAlign> x;
-                    x.template fetch<false>(px[n] + at, lx[n] - at, xlo, xhi);
-                    if constexpr (kDown) {
-                        Piece<kAlign> low;
-                        low.template fetch<false>(px[n] + a.pitch / 2 + at, lx[n] - at, xlo, xhi);
-                        block_product<E>(acc[n], va, vb, x.get(px[n] + at, lx[n] - at, xlo, xhi));
-                        block_product<E>(acc[n], va, vb, low.get(px[n] + a.pitch / 2 + at, lx[n] - at, xlo, xhi));
-                    } else {
-                        block_product<E>(acc[n], va, vb, x.get(px[n] + at, lx[n] - at, xlo, xhi));
-                    }
+                for (int q = 0; q < 4; ++q) acc[n][q] += part[q];
+            }
+        } else {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                if (n > 0 && n * 8 >= (int)it.columns) break;
+                Piece<kAlign> x;
+                x.fetch(px[n] + at, lx[n] - at, xlo, xhi);
+                if constexpr (kDown) {
+                    Piece<kAlign> low;
+                    low.fetch(px[n] + a.pitch / 2 + at, lx[n] - at, xlo, xhi);
+                    block_product<E>(acc[n], va, vb, x.get(px[n] + at, lx[n] - at, xlo, xhi));
+                    block_product<E>(acc[n], va, vb, low.get(px[n] + a.pitch / 2 + at, lx[n] - at, xlo, xhi));
+                } else {
+                    block_product<E>(acc[n], va, vb, x.get(px[n] + at, lx[n] - at, xlo, xhi));
                 }
             }
         }
     }
-    // the warps that share a strip: their sums in order
+    next();
+    // the warps that share a strip: their sums in order, 16 columns at a time
     if (c.ways > 1) {
-        float* mine = s.part[warp] + lane * 4;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) *reinterpret_cast<float4*>(mine + n * 128) = make_float4(acc[n][0], acc[n][1], acc[n][2], acc[n][3]);
-        __syncthreads();
-        if (way == 0) {
+        for (int n0 = 0; n0 < NT; n0 += 2) {
+            if (n0 > 0) __syncthreads();
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+            for (int n = n0; n < NT && n < n0 + 2; ++n)
+                *reinterpret_cast<float4*>(s.part[warp] + (n - n0) * 128 + lane * 4) = make_float4(acc[n][0], acc[n][1], acc[n][2], acc[n][3]);
+            __syncthreads();
+            if (way != 0) continue;
+#pragma unroll
+            for (int n = n0; n < NT && n < n0 + 2; ++n)
                 for (uint32_t w = 1; w < c.ways; ++w) {
-                    const float4 v = *reinterpret_cast<const float4*>(s.part[warp + w] + lane * 4 + n * 128);
+                    const float4 v = *reinterpret_cast<const float4*>(s.part[warp + w] + (n - n0) * 128 + lane * 4);
                     acc[n][0] += v.x; acc[n][1] += v.y; acc[n][2] += v.z; acc[n][3] += v.w;
                 }
         }
@@ -394,8 +472,8 @@ __device__ void product(const Args& a, Shared& s, const Cut& c, uint32_t i, uint
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
                 const uint32_t col = n * 8 + t * 2 + q;
-                if (col >= columns) continue;
-                const uint32_t slot = s.slot[first + col];
+                if (col >= it.columns) continue;
+                const uint32_t slot = s.slot[it.first + col];
                 if constexpr (kDown) {
                     float* z = a.z + (uint64_t)slot * a.D;
                     if (ja < rows) z[ja] = acc[n][q];
@@ -424,19 +502,13 @@ __device__ void product(const Args& a, Shared& s, const Cut& c, uint32_t i, uint
     }
 }
 
-template <typename E, int kAlign, bool kDown>
-__device__ void product_of(const Args& a, Shared& s, const Cut& c, uint32_t i, uint32_t piece, uint32_t wait_for)
+template <typename E, int kAlign, bool kDown, typename Next>
+__device__ __forceinline__ void product_of(const Args& a, Shared& s, const Cut& c, const Item& it, uint32_t wait_for, Next next)
 {
-    const uint32_t end = s.first[i + 1];
-    for (uint32_t first = s.first[i]; first < end; first += 64) {
-        const uint32_t columns = end - first < 64 ? end - first : 64;
-        if (columns <= 8) product<E, kAlign, 1, kDown>(a, s, c, i, piece, first, columns, wait_for);
-        else if (columns <= 16) product<E, kAlign, 2, kDown>(a, s, c, i, piece, first, columns, wait_for);
-        else if (columns <= 32) product<E, kAlign, 4, kDown>(a, s, c, i, piece, first, columns, wait_for);
-        else product<E, kAlign, 8, kDown>(a, s, c, i, piece, first, columns, wait_for);
-        wait_for = 0;
-        __syncthreads();
-    }
+    if (it.columns <= 8) product<E, kAlign, 1, kDown>(a, s, c, it, wait_for, next);
+    else if (it.columns <= 16) product<E, kAlign, 2, kDown>(a, s, c, it, wait_for, next);
+    else if (it.columns <= 32) product<E, kAlign, 4, kDown>(a, s, c, it, wait_for, next);
+    else product<E, kAlign, 8, kDown>(a, s, c, it, wait_for, next);
 }
 
 // Pieces are taken in order, the first products' before the second ones'.  A CTA waits for an expert's first product only with
@@ -455,32 +527,60 @@ __global__ void __launch_bounds__(kThreads, 2) experts_kernel(Args a)
     if (asked == 0)
         for (uint64_t i = (uint64_t)blockIdx.x * kThreads + threadIdx.x; i < (uint64_t)a.T * a.D; i += (uint64_t)gridDim.x * kThreads)
             reinterpret_cast<E*>(a.y + i / a.D * a.ld_y)[i % a.D] = RowsElem<E>::down(0.0f);
-    for (;;) {
-        if (threadIdx.x == 0) s.task = atomicAdd(&a.n->ticket, 1u);
-        __syncthreads();
-        const uint32_t task = s.task;
-        __syncthreads();
-        if (task >= all) break;
-        if (task < ups) {
-            const uint32_t i = task / up.pieces;
-            product_of<E, kAlign, false>(a, s, up, i, task - i * up.pieces, 0);
-            __threadfence();
+    const auto item = [&](uint32_t task) {
+        Item it;
+        it.any = task < all;
+        it.down = task >= ups;
+        const uint32_t n = it.down ? task - ups : task, pieces = it.down ? down.pieces : up.pieces;
+        it.i = it.any ? n / pieces : 0u;
+        it.piece = n - it.i * pieces;
+        it.first = s.first[it.i];
+        it.columns = min(s.first[it.i + 1] - it.first, 64u);
+        return it;
+    };
+    const auto begin = [&](const Item& it) {
+        if (it.any) start<E, kAlign>(a, s, it.down ? down : up, it);
+    };
+    if (threadIdx.x == 0) s.task[0] = asked ? atomicAdd(&a.n->ticket, 1u) : 0u;
+    __syncthreads();
+    Item it = item(s.task[0]);
+    begin(it);
+    for (uint32_t turn = 1; it.any; turn ^= 1u) {
+        const bool more = it.first + it.columns < s.first[it.i + 1];       // (an expert of more than 64 slots is gone over once for each 64)
+        uint32_t ticket = 0;
+        if (threadIdx.x == 0 && !more) ticket = atomicAdd(&a.n->ticket, 1u);
+        Item then;
+        const auto next = [&]() {
+            if (threadIdx.x == 0) s.task[turn] = ticket;
             __syncthreads();
-            if (threadIdx.x == 0) atomicAdd(&a.n->up[i], 1u);
-            continue;
-        }
-        const uint32_t i = (task - ups) / down.pieces, piece = task - ups - i * down.pieces;
-        product_of<E, kAlign, true>(a, s, down, i, piece, up.pieces);
+            if (more) {
+                then = it;
+                then.first = it.first + it.columns;
+                then.columns = min(s.first[it.i + 1] - then.first, 64u);
+            } else {
+                then = item(s.task[turn]);
+            }
+            begin(then);
+        };
+        if (it.down) product_of<E, kAlign, true>(a, s, down, it, up.pieces, next);
+        else product_of<E, kAlign, false>(a, s, up, it, 0, next);
+        const Item done = it;
+        it = then;
+        if (more) { __syncthreads(); continue; }
         __threadfence();
         __syncthreads();
+        if (!done.down) {
+            if (threadIdx.x == 0) atomicAdd(&a.n->up[done.i], 1u);
+            continue;
+        }
         if (threadIdx.x == 0) {
-            s.last = atomicAdd(&a.n->down[piece], 1u) + 1 == asked;
+            s.last = atomicAdd(&a.n->down[done.piece], 1u) + 1 == asked;
             __threadfence();
         }
         __syncthreads();
         if (!s.last) continue;
         // every expert is through with these columns of y
-        const uint32_t d0 = piece * down.strips * 16, cols = min(down.strips * 16, a.D - d0);
+        const uint32_t d0 = done.piece * down.strips * 16, cols = min(down.strips * 16, a.D - d0);
         for (uint32_t n = threadIdx.x; n < a.T * cols; n += kThreads) {
             const uint32_t t = n / cols, d = d0 + n - t * cols;
             float sum = 0.0f;
@@ -526,9 +626,11 @@ template <typename T> int experts_as(unsigned* status, const LayerExperts& a, cu
     constexpr uint32_t S = sizeof(T);
     unsigned char* work = (unsigned char*)a.work;
     const unsigned char* x = (const unsigned char*)a.x;
-    const Args args = { a.T, a.D, a.H, a.E, a.k, a.act, x, (const unsigned char*)a.up, (const unsigned char*)a.down, work + l.z,
-                        x + ((uint64_t)(a.T - 1) * a.ld_x + a.D) * S, a.ld_x * S, a.ld_y * S, l.pitch, a.w, a.ids, (unsigned char*)a.y, work + l.h,
-                        (float*)(work + l.z), (Counters*)work, status };
+    const unsigned char *up = (const unsigned char*)a.up, *down = (const unsigned char*)a.down;
+    const uint64_t matrix = (uint64_t)a.E * a.D * a.H * S;
+    const Args args = { a.T, a.D, a.H, a.E, a.k, a.act, x, x + ((uint64_t)(a.T - 1) * a.ld_x + a.D) * S, up,
+                        up + matrix * (a.act == PEARL_ACT_SILU_GATED ? 2 : 1), down, down + matrix, work + l.z, a.ld_x * S, a.ld_y * S, l.pitch, a.w, a.ids,
+                        (unsigned char*)a.y, work + l.h, (float*)(work + l.z), (Counters*)work, status };
     const uint32_t granule = rows_granule((uintptr_t)a.x | (uintptr_t)a.up, (uintptr_t)a.down, a.ld_x * S, (uint64_t)a.D * S, (uint64_t)a.H * S);
     m = granule >= 32 ? experts_launch<T, 32>(args, s) : granule >= 16 ? experts_launch<T, 16>(args, s) : experts_launch<T, 0>(args, s);
     return m < 0 ? m : n + m;
