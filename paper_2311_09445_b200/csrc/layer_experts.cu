@@ -8,7 +8,7 @@
 
 namespace {
 
-constexpr uint32_t kWarps = 8, kThreads = kWarps * 32;
+constexpr uint32_t kWarps = 8, kThreads = kWarps * 32;        // (of the experts' kernel: those that multiply; one more warp keeps the books)
 constexpr uint32_t kBlockBytes = 128;         // of a weight row: what a warp takes of 16 rows in one step, 32 bytes a lane of each of two rows
 constexpr uint32_t kMaxSlots = PEARL_LAYER_MAX_FEW * PEARL_ROWS_MAX_CHOICES;
 constexpr uint32_t kSpins = 1u << 21;
@@ -16,8 +16,8 @@ constexpr uint32_t kSpins = 1u << 21;
 // The parts of the scratch, in bytes from its start.  The counters are zero between calls.
 struct Counters {
     uint32_t ticket, finished;
-    uint32_t up[PEARL_ROWS_MAX_EXPERTS];               // finished pieces of an expert's first product
-    uint32_t down[PEARL_LAYER_MAX_INNER / 16];         // experts that are through with a piece of y
+    uint32_t down;                                     // finished pieces of all second products
+    uint32_t up[PEARL_ROWS_MAX_EXPERTS];               // of an expert's first product
 };
 struct Layout {
     uint64_t logits, h, z, bytes, pitch;
@@ -174,6 +174,12 @@ struct Args {
     Counters* n;
     unsigned* status;
 };
+// What a CTA works on: some strips of 16 weight rows of one expert, with some of its slots; or a part of y.
+enum Kind : uint32_t { kUp, kDown, kSum, kEnd };
+struct Item {
+    uint32_t kind;
+    uint32_t i, piece, first, columns;          // the expert's place among those asked for; of its slots
+};
 // A warp's ring: stages of 16 rows of 128 bytes, 16 bytes more a row, which spreads the rows over the banks (and holds the rest of a row that
 // starts between two words).
 constexpr uint32_t kStages = 4, kPitch = kBlockBytes + 16, kStageBytes = 16 * kPitch;
@@ -184,16 +190,17 @@ struct Shared {
     uint16_t expert[PEARL_ROWS_MAX_EXPERTS], first[PEARL_ROWS_MAX_EXPERTS + 1];       // of the experts that are asked for
     uint16_t slot[kMaxSlots];                          // by expert
     uint32_t sums[2][kWarps];
-    uint32_t asked, task[2], last;
+    Item item[2];                                      // what the warps work on, and what comes next
+    uint32_t asked, last;
 };
 
 // The experts that are asked for, and their slots.
 __device__ void plan(const Args& a, Shared& s)
 {
     const uint32_t slots = a.T * a.k, tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5;
-    for (uint32_t e = tid; e < a.E; e += kThreads) s.count[e] = 0;
+    for (uint32_t e = tid; e < a.E; e += kThreads + 32) s.count[e] = 0;
     __syncthreads();
-    for (uint32_t i = tid; i < slots; i += kThreads) {
+    for (uint32_t i = tid; i < slots; i += kThreads + 32) {
         const int32_t e = a.ids[i];
         if ((uint32_t)e < a.E) atomicAdd(&s.count[e], 1u);
         else if (e != -1 && blockIdx.x == 0) atomicOr(a.status, PEARL_ST_BAD_INDEX);
@@ -204,7 +211,7 @@ __device__ void plan(const Args& a, Shared& s)
 #pragma unroll
     for (uint32_t i = 0; i < kEach; ++i) {
         const uint32_t e = tid * kEach + i;
-        mine[i] = e < a.E ? s.count[e] : 0u;
+        mine[i] = e < a.E ? s.count[e] : 0u;               // (the last warp has none)
         slots_here += mine[i];
         asked_here += mine[i] != 0;
     }
@@ -214,10 +221,10 @@ __device__ void plan(const Args& a, Shared& s)
         const uint32_t p = __shfl_up_sync(0xFFFFFFFFu, slots_to, o), q = __shfl_up_sync(0xFFFFFFFFu, asked_to, o);
         if (lane >= (uint32_t)o) { slots_to += p; asked_to += q; }
     }
-    if (lane == 31) { s.sums[0][warp] = slots_to; s.sums[1][warp] = asked_to; }
+    if (lane == 31 && warp < kWarps) { s.sums[0][warp] = slots_to; s.sums[1][warp] = asked_to; }
     __syncthreads();
     uint32_t at = slots_to - slots_here, i_asked = asked_to - asked_here;
-    for (uint32_t w = 0; w < warp; ++w) { at += s.sums[0][w]; i_asked += s.sums[1][w]; }
+    for (uint32_t w = 0; w < min(warp, kWarps); ++w) { at += s.sums[0][w]; i_asked += s.sums[1][w]; }
 #pragma unroll
     for (uint32_t i = 0; i < kEach; ++i) {
         const uint32_t e = tid * kEach + i;
@@ -232,12 +239,21 @@ __device__ void plan(const Args& a, Shared& s)
     }
     if (tid == kThreads - 1) { s.asked = i_asked; s.first[i_asked] = (uint16_t)at; }
     __syncthreads();
-    for (uint32_t i = tid; i < slots; i += kThreads) {
+    for (uint32_t i = tid; i < slots; i += kThreads + 32) {
         const int32_t e = a.ids[i];
         if ((uint32_t)e < a.E) s.slot[atomicAdd(&s.count[e], 1u)] = (uint16_t)i;      // (in any order: no sum runs over an expert's slots)
     }
     __syncthreads();
 }
+
+// Barriers between the warps that multiply and the one that keeps the books: items handed over, what they need there, items finished; two of
+// each, for every other item.
+constexpr uint32_t kFull = 1, kReady = 3, kDone = 5, kMeet = 7;
+__device__ __forceinline__ void worker_waits(uint32_t id) { asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(kThreads + 32) : "memory"); }
+__device__ __forceinline__ void worker_arrives(uint32_t id) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "n"(kThreads + 32) : "memory"); }
+__device__ __forceinline__ void books_arrive(uint32_t id) { worker_arrives(id); }
+__device__ __forceinline__ void books_wait(uint32_t id) { worker_waits(id); }
+__device__ __forceinline__ void workers_meet() { asm volatile("bar.sync %0, %1;" ::"n"(kMeet), "n"(kThreads) : "memory"); }
 
 __device__ __forceinline__ uint32_t read_acquired(const uint32_t* p)
 {
@@ -267,12 +283,6 @@ __device__ __forceinline__ Cut cut_of(uint32_t rows, uint32_t row_bytes, uint32_
 
 __device__ __forceinline__ float activated(float gate, float value) { return gate / (1.0f + expf(-gate)) * value; }
 
-// What a warp works on: a strip of 16 weight rows of one expert, with some of its slots.
-struct Item {
-    uint32_t i, piece, first, columns;          // the expert's place among those asked for; of its slots
-    bool down, any;
-};
-
 // The weight rows of an item's strip, as the lanes copy them: lane l has word l % 8 of rows l / 8 + 4 q of a block.
 template <typename E, int kAlign>
 struct Strip {
@@ -280,12 +290,12 @@ struct Strip {
     uint32_t row_bytes, blocks, rows_low, rows_high;    // rows that there are, of the first and of the last 8
     __device__ __forceinline__ Strip(const Args& a, const Shared& s, const Cut& c, const Item& it)
     {
-        const bool gated = !it.down && a.act == PEARL_ACT_SILU_GATED;
-        const uint32_t rows = it.down ? a.D : a.H, strip = it.piece * c.strips + (threadIdx.x >> 5) / c.ways;
-        row_bytes = (it.down ? a.H : a.D) * (uint32_t)sizeof(E);
+        const bool gated = it.kind == kUp && a.act == PEARL_ACT_SILU_GATED;
+        const uint32_t rows = it.kind == kDown ? a.D : a.H, strip = it.piece * c.strips + (threadIdx.x >> 5) / c.ways;
+        row_bytes = (it.kind == kDown ? a.H : a.D) * (uint32_t)sizeof(E);
         blocks = c.blocks;
         const uint32_t j = strip * (gated ? 8u : 16u), k = gated ? j : j + 8;
-        const unsigned char* m = (it.down ? a.down : a.up) + (uint64_t)s.expert[it.i] * rows * (gated ? 2 : 1) * row_bytes;
+        const unsigned char* m = (it.kind == kDown ? a.down : a.up) + (uint64_t)s.expert[it.i] * rows * (gated ? 2 : 1) * row_bytes;
         low = m + (uint64_t)j * row_bytes;
         high = m + (uint64_t)(gated ? rows + k : k) * row_bytes;
         rows_low = j < rows ? min(rows - j, 8u) : 0u;
@@ -304,11 +314,11 @@ struct Strip {
             for (uint32_t q = 0; q < 4; ++q) {
                 const uint32_t row = r + q % 2 * 4;
                 const bool there = at < row_bytes && row < (q < 2 ? rows_low : rows_high);
-                word(a.status, to + q * 4 * kPitch, (q < 2 ? low : high) + (uint64_t)row * row_bytes + at, there ? 16u : 0u, it.down ? a.down : a.up,
-                     it.down ? a.down_end : a.up_end);
+                word(a.status, to + q * 4 * kPitch, (q < 2 ? low : high) + (uint64_t)row * row_bytes + at, there ? 16u : 0u, it.kind == kDown ? a.down : a.up,
+                     it.kind == kDown ? a.down_end : a.up_end);
             }
         } else {
-            const unsigned char *lo = it.down ? a.down : a.up, *hi = it.down ? a.down_end : a.up_end;
+            const unsigned char *lo = it.kind == kDown ? a.down : a.up, *hi = it.kind == kDown ? a.down_end : a.up_end;
 #pragma unroll
             for (uint32_t q = 0; q < (16 * kWords + 31) / 32; ++q) {
                 const uint32_t n = lane + q * 32, row = n / kWords, w = n - row * kWords;
@@ -365,42 +375,33 @@ template <typename E, int kAlign> __device__ __forceinline__ void start(const Ar
 }
 
 // One item's product; its first blocks are on their way.  next() names the item to start as soon as the ring is free.
-template <typename E, int kAlign, int NT, bool kDown, typename Next>
-__device__ void product(const Args& a, Shared& s, const Cut& c, const Item& it, uint32_t wait_for, Next next)
+template <typename E, int kAlign, int NT, uint32_t kKind, typename Next>
+__device__ void product(const Args& a, Shared& s, const Cut& c, const Item& it, uint32_t turn, Next next)
 {
-    constexpr bool k32 = sizeof(E) == 4;
+    constexpr bool k32 = sizeof(E) == 4, kSecond = kKind == kDown;
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3u;
     const uint32_t way = warp % c.ways;
-    const bool gated = !kDown && a.act == PEARL_ACT_SILU_GATED;
-    const uint32_t rows = kDown ? a.D : a.H;
+    const bool gated = kKind == kUp && a.act == PEARL_ACT_SILU_GATED;
+    const uint32_t rows = kSecond ? a.D : a.H;
     const uint32_t j0 = (it.piece * c.strips + warp / c.ways) * (gated ? 8u : 16u), ja = j0 + g, jb = gated ? ja : j0 + 8 + g;
     const Strip<E, kAlign> strip(a, s, c, it);
     const int here = (int)strip.row_bytes - (int)(t * 32);       // bytes from a lane's first piece on
-    if constexpr (kDown) {
-        // h: wait for the expert's first product
-        if (wait_for && threadIdx.x == 0) {
-            uint32_t spins = 0;
-            while (read_acquired(&a.n->up[it.i]) < wait_for)
-                if (++spins > kSpins) { atomicOr(a.status, PEARL_ST_INTERNAL); break; }
-            __threadfence();
-        }
-        __syncthreads();
-    }
     const unsigned char* px[NT];
     int lx[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const uint32_t col = n * 8 + g;
         const uint32_t slot = col < it.columns ? s.slot[it.first + col] : 0u;
-        px[n] = (kDown ? a.h + slot * a.pitch : a.x + (uint64_t)(slot / a.k) * a.ld_x) + t * 32;
+        px[n] = (kSecond ? a.h + slot * a.pitch : a.x + (uint64_t)(slot / a.k) * a.ld_x) + t * 32;
         lx[n] = col < it.columns ? here : 0;
     }
-    const unsigned char *xlo = kDown ? a.h : a.x, *xhi = kDown ? a.h_end : a.x_end;
+    const unsigned char *xlo = kSecond ? a.h : a.x, *xhi = kSecond ? a.h_end : a.x_end;
     float acc[NT][4];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int q = 0; q < 4; ++q) acc[n][q] = 0.0f;
+    worker_waits(kReady + turn);
     uint32_t stage = 0;
     for (uint32_t block = way; block < c.blocks; block += c.ways) {
         asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
@@ -436,7 +437,7 @@ __device__ void product(const Args& a, Shared& s, const Cut& c, const Item& it, 
                 if (n > 0 && n * 8 >= (int)it.columns) break;
                 Piece<kAlign> x;
                 x.fetch(px[n] + at, lx[n] - at, xlo, xhi);
-                if constexpr (kDown) {
+                if constexpr (kSecond) {
                     Piece<kAlign> low;
                     low.fetch(px[n] + a.pitch / 2 + at, lx[n] - at, xlo, xhi);
                     block_product<E>(acc[n], va, vb, x.get(px[n] + at, lx[n] - at, xlo, xhi));
@@ -452,11 +453,11 @@ __device__ void product(const Args& a, Shared& s, const Cut& c, const Item& it, 
     if (c.ways > 1) {
 #pragma unroll
         for (int n0 = 0; n0 < NT; n0 += 2) {
-            if (n0 > 0) __syncthreads();
+            if (n0 > 0) workers_meet();
 #pragma unroll
             for (int n = n0; n < NT && n < n0 + 2; ++n)
                 *reinterpret_cast<float4*>(s.part[warp] + (n - n0) * 128 + lane * 4) = make_float4(acc[n][0], acc[n][1], acc[n][2], acc[n][3]);
-            __syncthreads();
+            workers_meet();
             if (way != 0) continue;
 #pragma unroll
             for (int n = n0; n < NT && n < n0 + 2; ++n)
@@ -474,7 +475,7 @@ __device__ void product(const Args& a, Shared& s, const Cut& c, const Item& it, 
                 const uint32_t col = n * 8 + t * 2 + q;
                 if (col >= it.columns) continue;
                 const uint32_t slot = s.slot[it.first + col];
-                if constexpr (kDown) {
+                if constexpr (kSecond) {
                     float* z = a.z + (uint64_t)slot * a.D;
                     if (ja < rows) z[ja] = acc[n][q];
                     if (jb < rows) z[jb] = acc[n][q + 2];
@@ -502,19 +503,110 @@ __device__ void product(const Args& a, Shared& s, const Cut& c, const Item& it, 
     }
 }
 
-template <typename E, int kAlign, bool kDown, typename Next>
-__device__ __forceinline__ void product_of(const Args& a, Shared& s, const Cut& c, const Item& it, uint32_t wait_for, Next next)
+template <typename E, int kAlign, uint32_t kKind, typename Next>
+__device__ __forceinline__ void product_of(const Args& a, Shared& s, const Cut& c, const Item& it, uint32_t turn, Next next)
 {
-    if (it.columns <= 8) product<E, kAlign, 1, kDown>(a, s, c, it, wait_for, next);
-    else if (it.columns <= 16) product<E, kAlign, 2, kDown>(a, s, c, it, wait_for, next);
-    else if (it.columns <= 32) product<E, kAlign, 4, kDown>(a, s, c, it, wait_for, next);
-    else product<E, kAlign, 8, kDown>(a, s, c, it, wait_for, next);
+    if (it.columns <= 8) product<E, kAlign, 1, kKind>(a, s, c, it, turn, next);
+    else if (it.columns <= 16) product<E, kAlign, 2, kKind>(a, s, c, it, turn, next);
+    else if (it.columns <= 32) product<E, kAlign, 4, kKind>(a, s, c, it, turn, next);
+    else product<E, kAlign, 8, kKind>(a, s, c, it, turn, next);
 }
 
-// Pieces are taken in order, the first products' before the second ones'.  A CTA waits for an expert's first product only with
-// pieces of its own already taken, and each of those it waits for is with a CTA that runs: nobody waits for one that is yet to be launched.
+// A part of y, of `parts`: the slots' sums in the order of the choices.
+template <typename E> __device__ void weighted_sums(const Args& a, uint32_t part, uint32_t parts)
+{
+    const uint64_t all = (uint64_t)a.T * a.D, each = (all + parts - 1) / parts, end = min(all, (part + 1) * each);
+    for (uint64_t n = part * each + threadIdx.x; n < end; n += kThreads) {
+        const uint32_t t = (uint32_t)(n / a.D), d = (uint32_t)(n - (uint64_t)t * a.D);
+        float sum = 0.0f;
+#pragma unroll 4
+        for (uint32_t j = 0; j < a.k; ++j) {
+            const uint32_t slot = t * a.k + j;
+            if ((uint32_t)a.ids[slot] < a.E) sum = __fmaf_rn(a.w[slot], a.z[(uint64_t)slot * a.D + d], sum);
+        }
+        reinterpret_cast<E*>(a.y + t * a.ld_y)[d] = RowsElem<E>::down(sum);
+    }
+}
+
+// The warp that keeps the books.  It takes pieces in order -- all first products' before the second ones', these before the parts of y --,
+// hands them to the others, waits for what a piece needs and tells what is finished.  It alone fences, and it has no copies on their way, for
+// which a fence would wait.  A CTA waits only with an earlier piece told, and each piece that it waits for is with a CTA that runs: nobody waits
+// for one that is yet to be launched.
+__device__ void keep_books(const Args& a, Shared& s, const Cut& up, const Cut& down, uint32_t parts)
+{
+    const uint32_t lane = threadIdx.x & 31u;
+    const uint32_t asked = s.asked, ups = asked * up.pieces, downs = asked * down.pieces;
+    uint32_t known = 0;                             // experts (in order) whose first product is known to be there
+    const auto ticket = [&] { return lane == 0 ? atomicAdd(&a.n->ticket, 1u) : 0u; };
+    uint32_t ahead = ticket();
+    const auto item = [&] {
+        Item it = { kEnd, 0, 0, 0, 0 };
+        const uint32_t task = __shfl_sync(0xFFFFFFFFu, ahead, 0);
+        if (task >= ups + downs + parts) return it;
+        ahead = ticket();
+        if (task >= ups + downs) {
+            it.kind = kSum;
+            it.piece = task - ups - downs;
+            return it;
+        }
+        it.kind = task < ups ? kUp : kDown;
+        const uint32_t n = task < ups ? task : task - ups, pieces = task < ups ? up.pieces : down.pieces;
+        it.i = n / pieces;
+        it.piece = n - it.i * pieces;
+        it.first = s.first[it.i];
+        it.columns = min(s.first[it.i + 1] - it.first, 64u);
+        return it;
+    };
+    // whether what the item needs is there; `wait` for it (with a limit, and a status bit behind that)
+    const auto needs = [&](const Item& it, bool wait) {
+        if (it.kind == kUp || it.kind == kEnd || (it.kind == kDown && it.i < known)) return true;
+        uint32_t there = 0;
+        if (lane == 0) {
+            const uint32_t* p = it.kind == kDown ? &a.n->up[it.i] : &a.n->down;
+            const uint32_t count = it.kind == kDown ? up.pieces : downs;
+            uint32_t spins = 0;
+            while (!(there = read_acquired(p) >= count) && wait)
+                if (++spins > kSpins) { atomicOr(a.status, PEARL_ST_INTERNAL); break; }
+        }
+        there = __shfl_sync(0xFFFFFFFFu, there, 0);
+        if (there && it.kind == kDown) known = it.i + 1;
+        return there != 0;
+    };
+    const auto give = [&](const Item& it, uint32_t turn) {
+        if (lane == 0) s.item[turn] = it;
+        __syncwarp();
+        books_arrive(kFull + turn);
+    };
+    Item it = item();
+    give(it, 0);
+    bool told = false;
+    for (uint32_t turn = 0;; turn ^= 1u) {
+        if (!told) { needs(it, true); books_arrive(kReady + turn); }
+        if (it.kind == kEnd) break;
+        Item then;
+        // an expert of more than 64 slots is gone over once for each 64
+        const bool more = (it.kind == kUp || it.kind == kDown) && it.first + it.columns < s.first[it.i + 1];
+        if (more) {
+            then = it;
+            then.first = it.first + it.columns;
+            then.columns = min(s.first[it.i + 1] - then.first, 64u);
+        } else {
+            then = item();
+        }
+        give(then, turn ^ 1u);
+        told = needs(then, false);
+        if (told) books_arrive(kReady + (turn ^ 1u));
+        books_wait(kDone + turn);
+        if (!more && it.kind != kSum && lane == 0) {
+            __threadfence();
+            atomicAdd(it.kind == kUp ? &a.n->up[it.i] : &a.n->down, 1u);
+        }
+        it = then;
+    }
+}
+
 template <typename E, int kAlign>
-__global__ void __launch_bounds__(kThreads, 2) experts_kernel(Args a)
+__global__ void __launch_bounds__(kThreads + 32, 2) experts_kernel(Args a)
 {
     extern __shared__ __align__(16) unsigned char memory[];
     Shared& s = *reinterpret_cast<Shared*>(memory);
@@ -523,81 +615,43 @@ __global__ void __launch_bounds__(kThreads, 2) experts_kernel(Args a)
     const uint32_t asked = s.asked;
     const bool gated = a.act == PEARL_ACT_SILU_GATED;
     const Cut up = cut_of(gated ? a.H * 2 : a.H, a.D * (uint32_t)sizeof(E), asked), down = cut_of(a.D, a.H * (uint32_t)sizeof(E), asked);
-    const uint32_t ups = asked * up.pieces, all = ups + asked * down.pieces;
-    if (asked == 0)
-        for (uint64_t i = (uint64_t)blockIdx.x * kThreads + threadIdx.x; i < (uint64_t)a.T * a.D; i += (uint64_t)gridDim.x * kThreads)
-            reinterpret_cast<E*>(a.y + i / a.D * a.ld_y)[i % a.D] = RowsElem<E>::down(0.0f);
-    const auto item = [&](uint32_t task) {
-        Item it;
-        it.any = task < all;
-        it.down = task >= ups;
-        const uint32_t n = it.down ? task - ups : task, pieces = it.down ? down.pieces : up.pieces;
-        it.i = it.any ? n / pieces : 0u;
-        it.piece = n - it.i * pieces;
-        it.first = s.first[it.i];
-        it.columns = min(s.first[it.i + 1] - it.first, 64u);
-        return it;
-    };
-    const auto begin = [&](const Item& it) {
-        if (it.any) start<E, kAlign>(a, s, it.down ? down : up, it);
-    };
-    if (threadIdx.x == 0) s.task[0] = asked ? atomicAdd(&a.n->ticket, 1u) : 0u;
-    __syncthreads();
-    Item it = item(s.task[0]);
-    begin(it);
-    for (uint32_t turn = 1; it.any; turn ^= 1u) {
-        const bool more = it.first + it.columns < s.first[it.i + 1];       // (an expert of more than 64 slots is gone over once for each 64)
-        uint32_t ticket = 0;
-        if (threadIdx.x == 0 && !more) ticket = atomicAdd(&a.n->ticket, 1u);
-        Item then;
-        const auto next = [&]() {
-            if (threadIdx.x == 0) s.task[turn] = ticket;
-            __syncthreads();
-            if (more) {
-                then = it;
-                then.first = it.first + it.columns;
-                then.columns = min(s.first[it.i + 1] - then.first, 64u);
-            } else {
-                then = item(s.task[turn]);
-            }
-            begin(then);
+    const uint32_t parts = min(gridDim.x, (uint32_t)(((uint64_t)a.T * a.D + kThreads - 1) / kThreads));
+    if (threadIdx.x >= kThreads) {
+        keep_books(a, s, up, down, parts);
+    } else {
+        const auto begin = [&](const Item& it) {
+            if (it.kind == kUp || it.kind == kDown) start<E, kAlign>(a, s, it.kind == kDown ? down : up, it);
         };
-        if (it.down) product_of<E, kAlign, true>(a, s, down, it, up.pieces, next);
-        else product_of<E, kAlign, false>(a, s, up, it, 0, next);
-        const Item done = it;
-        it = then;
-        if (more) { __syncthreads(); continue; }
-        __threadfence();
-        __syncthreads();
-        if (!done.down) {
-            if (threadIdx.x == 0) atomicAdd(&a.n->up[done.i], 1u);
-            continue;
-        }
-        if (threadIdx.x == 0) {
-            s.last = atomicAdd(&a.n->down[done.piece], 1u) + 1 == asked;
-            __threadfence();
-        }
-        __syncthreads();
-        if (!s.last) continue;
-        // every expert is through with these columns of y
-        const uint32_t d0 = done.piece * down.strips * 16, cols = min(down.strips * 16, a.D - d0);
-        for (uint32_t n = threadIdx.x; n < a.T * cols; n += kThreads) {
-            const uint32_t t = n / cols, d = d0 + n - t * cols;
-            float sum = 0.0f;
-            for (uint32_t j = 0; j < a.k; ++j) {
-                const uint32_t slot = t * a.k + j;
-                if ((uint32_t)a.ids[slot] < a.E) sum = __fmaf_rn(a.w[slot], a.z[(uint64_t)slot * a.D + d], sum);
+        worker_waits(kFull);
+        Item it = s.item[0];
+        begin(it);
+        for (uint32_t turn = 0; it.kind != kEnd; turn ^= 1u) {
+            Item then;
+            const auto next = [&]() {
+                worker_waits(kFull + (turn ^ 1u));
+                then = s.item[turn ^ 1u];
+                begin(then);
+            };
+            if (it.kind == kUp) {
+                product_of<E, kAlign, kUp>(a, s, up, it, turn, next);
+            } else if (it.kind == kDown) {
+                product_of<E, kAlign, kDown>(a, s, down, it, turn, next);
+            } else {
+                next();
+                worker_waits(kReady + turn);
+                weighted_sums<E>(a, it.piece, parts);
             }
-            reinterpret_cast<E*>(a.y + t * a.ld_y)[d] = RowsElem<E>::down(sum);
+            worker_arrives(kDone + turn);
+            it = then;
         }
     }
     // the last one out leaves the counters as they were
+    __syncthreads();
     if (threadIdx.x == 0) s.last = atomicAdd(&a.n->finished, 1u) + 1 == gridDim.x;
     __syncthreads();
     if (!s.last) return;
-    for (uint32_t i = threadIdx.x; i < asked; i += kThreads) a.n->up[i] = 0;
-    for (uint32_t i = threadIdx.x; i < down.pieces; i += kThreads) a.n->down[i] = 0;
-    if (threadIdx.x == 0) a.n->ticket = a.n->finished = 0;
+    for (uint32_t i = threadIdx.x; i < asked; i += kThreads + 32) a.n->up[i] = 0;
+    if (threadIdx.x == 0) a.n->ticket = a.n->finished = a.n->down = 0;
 }
 
 template <typename T, int kAlign> int experts_launch(const Args& a, cudaStream_t s)
@@ -608,7 +662,7 @@ template <typename T, int kAlign> int experts_launch(const Args& a, cudaStream_t
         if (cudaFuncSetAttribute(experts_kernel<T, kAlign>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Shared)) != cudaSuccess) return -1;
         if (dev >= 0) ready[dev] = true;
     }
-    return rows_launch(experts_kernel<T, kAlign>, dim3(2 * rows_sm_count()), dim3(kThreads), sizeof(Shared), s, 0, a);
+    return rows_launch(experts_kernel<T, kAlign>, dim3(2 * rows_sm_count()), dim3(kThreads + 32), sizeof(Shared), s, 0, a);
 }
 
 template <typename T> int experts_as(unsigned* status, const LayerExperts& a, cudaStream_t s)
