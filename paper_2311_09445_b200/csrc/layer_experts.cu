@@ -36,21 +36,79 @@ Layout layout_of(uint32_t T, uint32_t D, uint32_t H, uint32_t E, uint32_t k)
     return l;
 }
 
-template <typename E> __device__ __forceinline__ float element(const E* p) { return RowsElem<E>::up(*p); }
-
 // ---- the router's product --------------------------------------------------------------------------------------------
-// logits[t, e]: a warp each, in binary64.
-template <typename T>
-__global__ void __launch_bounds__(kWorkers * 32) logits_kernel(uint32_t rows, uint32_t D, uint32_t E, const T* x, uint64_t ld_x, const T* router, float* logits)
+// Logits of X experts for 4 rows, in binary64, so that the choice does not hang on the order of a sum: 8 warps share the width.  A
+// conversion takes four times a multiply-add's time, and 4 x 4 numbers need 8 for 16 products.
+constexpr uint32_t kRowsAtOnce = 4;
+template <typename E, int V, int X>
+__global__ void __launch_bounds__(kWorkers * 32) logits_kernel(unsigned* status, uint32_t T, uint32_t D, uint32_t experts, const E* x, uint64_t ld_x,
+                                                               const E* router, float* logits)
 {
+    __shared__ double sums[kWorkers][X * kRowsAtOnce];
     rows_begin();
-    const uint32_t i = blockIdx.x * kWorkers + (threadIdx.x >> 5), lane = threadIdx.x & 31u;
-    if (i >= rows * E) return;
-    const T *a = x + (uint64_t)(i / E) * ld_x, *b = router + (uint64_t)(i % E) * D;
-    double s = 0.0;
-    for (uint32_t d = lane; d < D; d += 32) s = __fma_rn((double)element(a + d), (double)element(b + d), s);
-    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-    if (lane == 0) logits[i] = (float)s;
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, e0 = blockIdx.x * X, t0 = blockIdx.y * kRowsAtOnce;
+    double s[X * kRowsAtOnce];
+#pragma unroll
+    for (int i = 0; i < X * (int)kRowsAtOnce; ++i) s[i] = 0.0;
+    for (uint32_t d = threadIdx.x * V; d < D; d += kWorkers * 32 * V) {
+        RowsVec<E, V> w[X], r[kRowsAtOnce];
+        // (rows and widths are multiples of an access here; rows that there are none of repeat the last one)
+#pragma unroll
+        for (int i = 0; i < X; ++i) w[i] = rows_load_vec<E, V>(router + (uint64_t)min(e0 + i, experts - 1) * D + d);
+#pragma unroll
+        for (int i = 0; i < (int)kRowsAtOnce; ++i) r[i] = rows_load_vec<E, V>(x + (uint64_t)min(t0 + i, T - 1) * ld_x + d);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            double a[X];
+#pragma unroll
+            for (int i = 0; i < X; ++i) a[i] = (double)w[i].get(v);
+#pragma unroll
+            for (int j = 0; j < (int)kRowsAtOnce; ++j) {
+                const double b = (double)r[j].get(v);
+#pragma unroll
+                for (int i = 0; i < X; ++i) s[i * kRowsAtOnce + j] = __fma_rn(a[i], b, s[i * kRowsAtOnce + j]);
+            }
+        }
+    }
+    // each step a lane hands half of its sums to another and adds the other half; what is left is one sum a lane, or a part of it
+    int n = X * (int)kRowsAtOnce, which = 0;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        if (n > 1) {
+            n /= 2;
+            const bool upper = lane & o;
+            which += upper ? n : 0;
+#pragma unroll
+            for (int i = 0; i < X * (int)kRowsAtOnce / 2; ++i) {
+                if (i >= n) break;
+                const double mine = upper ? s[i + n] : s[i], other = upper ? s[i] : s[i + n];
+                s[i] = mine + __shfl_xor_sync(0xFFFFFFFFu, other, o);
+            }
+        } else {
+            s[0] += __shfl_xor_sync(0xFFFFFFFFu, s[0], o);
+        }
+    }
+    sums[warp][which] = s[0];                          // (lanes that share a sum have the same)
+    __syncthreads();
+    if (threadIdx.x >= X * kRowsAtOnce) return;
+    const uint32_t e = e0 + threadIdx.x / kRowsAtOnce, t = t0 + threadIdx.x % kRowsAtOnce;
+    if (e >= experts || t >= T) return;
+    double all = 0.0;
+#pragma unroll
+    for (int w = 0; w < (int)kWorkers; ++w) all += sums[w][threadIdx.x];
+    float* to = logits + (uint64_t)t * experts + e;
+    if (ROWS_IN_ARRAY(status, to, 4, logits, logits + (uint64_t)T * experts)) *to = (float)all;
+}
+
+template <typename E, int V> int logits_launch(unsigned* status, const LayerExperts& a, float* logits, cudaStream_t s)
+{
+    const uint32_t fours = (a.T + kRowsAtOnce - 1) / kRowsAtOnce;
+#define LOGITS(X)                                                                                                                             \
+    rows_launch(logits_kernel<E, V, X>, dim3((a.E + X - 1) / X, fours), dim3(kWorkers * 32), 0, s, 0, status, a.T, a.D, a.E, (const E*)a.x, a.ld_x, \
+                (const E*)a.router, logits)
+    // (four experts a block where there are more than two blocks an SM without that)
+    return a.E * fours > 2 * rows_sm_count() ? LOGITS(4) : LOGITS(1);
+#undef LOGITS
 }
 
 // ---- matrix instructions ----------------------------------------------------------------------------------------------
@@ -812,8 +870,9 @@ template <typename T> int experts_as(unsigned* status, const LayerExperts& a, cu
     float* logits = (float*)((char*)a.work + l.logits);
     int n = 0, m;
     if (a.router) {
-        if ((m = rows_launch(logits_kernel<T>, dim3((a.T * a.E + kWorkers - 1) / kWorkers), dim3(kWorkers * 32), 0, s, 0, a.T, a.D, a.E, (const T*)a.x, a.ld_x,
-                             (const T*)a.router, logits)) < 0) return m;
+        constexpr int V = 16 / (int)sizeof(T);
+        const uint32_t granule = rows_granule((uintptr_t)a.x, (uintptr_t)a.router, a.ld_x * sizeof(T), (uint64_t)a.D * sizeof(T));
+        if ((m = granule >= 16 ? logits_launch<T, V>(status, a, logits, s) : logits_launch<T, 1>(status, a, logits, s)) < 0) return m;
         n += m;
         if ((m = rows_launch_route(status, a.T, a.E, a.k, PEARL_F32, logits, a.E, a.over_chosen, a.w, a.ids, s)) < 0) return m;
         n += m;
