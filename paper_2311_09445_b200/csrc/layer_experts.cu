@@ -13,7 +13,7 @@ constexpr uint32_t kWorkers = 8;              // warps that multiply
 constexpr uint32_t kBlockBytes = 128;         // of a row: what a warp takes of 16 weight rows in one step, 32 bytes a lane of each of two rows
 constexpr uint32_t kMaxSlots = PEARL_LAYER_MAX_FEW * PEARL_ROWS_MAX_CHOICES;
 constexpr uint32_t kMaxColumns = 64;          // slots of an expert that are multiplied at once
-constexpr uint32_t kSpins = 1u << 21;
+constexpr uint32_t kSpins = kLayerSpins;
 
 // The parts of the scratch, in bytes from its start.  The counters are zero between calls.
 struct Counters {
@@ -268,26 +268,6 @@ __device__ void plan(const Args& a, Shared& s)
 }
 
 // ---- barriers ---------------------------------------------------------------------------------------------------------
-__device__ __forceinline__ uint32_t address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void set_up(uint64_t* barrier, uint32_t arrivals)
-{
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(address(barrier)), "r"(arrivals) : "memory");
-}
-__device__ __forceinline__ void arrive(uint64_t* barrier) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(address(barrier)) : "memory"); }
-__device__ __forceinline__ void arrive_with(uint64_t* barrier, uint32_t bytes)
-{
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(address(barrier)), "r"(bytes) : "memory");
-}
-// Waits for the end of a barrier's phase of this parity; with a limit, and a status bit behind it.
-__device__ __forceinline__ void wait_for(unsigned* status, uint64_t* barrier, uint32_t parity)
-{
-    uint32_t there = 0;
-    for (uint32_t spins = 0; !there; ++spins) {
-        asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
-                     : "=r"(there) : "r"(address(barrier)), "r"(parity & 1u) : "memory");
-        if (spins > 4 * kSpins) { atomicOr(status, PEARL_ST_INTERNAL); break; }
-    }
-}
 __device__ __forceinline__ void workers_meet() { asm volatile("bar.sync 1, %0;" ::"n"(kWorkers * 32) : "memory"); }
 __device__ __forceinline__ uint32_t read_acquired(const uint32_t* p)
 {
@@ -332,12 +312,12 @@ struct Place {
 __device__ __forceinline__ void copy_blocks(uint64_t* barrier, unsigned char* to, const CUtensorMap* map, uint32_t row, uint32_t group, uint32_t block)
 {
     asm volatile("cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
-                 ::"r"(address(to)), "l"(map), "r"(0), "r"(row), "r"(group), "r"(block), "r"(address(barrier)) : "memory");
+                 ::"r"(layer_address(to)), "l"(map), "r"(0), "r"(row), "r"(group), "r"(block), "r"(layer_address(barrier)) : "memory");
 }
 __device__ __forceinline__ void copy_block(uint64_t* barrier, unsigned char* to, const CUtensorMap* map, uint32_t column, uint32_t row, uint32_t group)
 {
     asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-                 ::"r"(address(to)), "l"(map), "r"(column), "r"(row), "r"(group), "r"(address(barrier)) : "memory");
+                 ::"r"(layer_address(to)), "l"(map), "r"(column), "r"(row), "r"(group), "r"(layer_address(barrier)) : "memory");
 }
 // The 16-byte word at `from`, of which `bytes` are read, zeros for the rest.  (A word that an array begins in is read whole.)
 __device__ __forceinline__ void copy_word(uint32_t to, const unsigned char* from, uint32_t bytes, const unsigned char* lo, const unsigned char* hi,
@@ -349,7 +329,7 @@ __device__ __forceinline__ void copy_word(uint32_t to, const unsigned char* from
 // An arrival when this thread's words are there.
 __device__ __forceinline__ void arrive_with_words(uint64_t* barrier)
 {
-    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(address(barrier)) : "memory");
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(layer_address(barrier)) : "memory");
 }
 
 // The warps that bring weights: one thread of one; eight warps where words have to be cut out of rows.
@@ -378,7 +358,7 @@ __device__ void bring_weights(const Args& a, Shared& s, const Ring& r, uint32_t 
     const uint32_t lane = threadIdx.x & 31u;
     Place at = { 0, 0 };
     for (uint32_t n = 0;; ++n) {
-        wait_for(a.status, s.queued + n % kQueue, n / kQueue);
+        layer_wait(a.status, s.queued + n % kQueue, n / kQueue);
         const Item it = s.item[n % kQueue];
         if (it.kind == kEnd) break;
         if (it.kind == kUp || it.kind == kDown) {
@@ -389,10 +369,10 @@ __device__ void bring_weights(const Args& a, Shared& s, const Ring& r, uint32_t 
                 const bool whole = c.row_bytes % kBlockBytes == 0;
                 const CUtensorMap* map = it.kind == kDown ? down_map : up_map;
                 for (uint32_t k = 0; k < c.chunks; ++k, at.step(r)) {
-                    wait_for(a.status, s.empty + at.stage, at.round + 1);
+                    layer_wait(a.status, s.empty + at.stage, at.round + 1);
                     if (lane != 0) continue;
                     unsigned char* to = r.base + at.stage * r.bytes;
-                    arrive_with(s.full + at.stage, c.strips * 16 * c.chunk);
+                    layer_arrive_with(s.full + at.stage, c.strips * 16 * c.chunk);
                     if (whole) {
                         copy_blocks(s.full + at.stage, to, map, row, group, k * c.across);
                     } else {
@@ -415,8 +395,8 @@ __device__ void bring_weights(const Args& a, Shared& s, const Ring& r, uint32_t 
                     left[i] = p ? (int)min((long long)(hi - from[i]), (long long)1 << 30) : 0;
                 }
                 for (uint32_t k = 0; k < c.chunks; ++k, at.step(r)) {
-                    wait_for(a.status, s.empty + at.stage, at.round + 1);
-                    const uint32_t to = address(r.base) + at.stage * r.bytes + first * c.pitch + w * 16;
+                    layer_wait(a.status, s.empty + at.stage, at.round + 1);
+                    const uint32_t to = layer_address(r.base) + at.stage * r.bytes + first * c.pitch + w * 16;
 #pragma unroll
                     for (uint32_t i = 0; i < 4; ++i)
                         for (uint32_t b = 0; b < c.across + (w == 0); ++b) {
@@ -428,7 +408,7 @@ __device__ void bring_weights(const Args& a, Shared& s, const Ring& r, uint32_t 
             }
         }
         __syncwarp();
-        if (lane == 0) arrive(s.done + n % kQueue);
+        if (lane == 0) layer_arrive(s.done + n % kQueue);
     }
 }
 
@@ -440,17 +420,17 @@ template <typename E, int kAlign> __device__ void bring_rows(const Args& a, Shar
     uint32_t known = 0;                             // experts (in order) whose first product is there
     bool summed = false;
     for (uint32_t n = 0;; ++n) {
-        wait_for(a.status, s.queued + n % kQueue, n / kQueue);
+        layer_wait(a.status, s.queued + n % kQueue, n / kQueue);
         const Item it = s.item[n % kQueue];
         if (it.kind == kEnd) break;
         if (it.kind == kSum) {
             if (warp == 0 && lane == 0) {
                 if (!summed) poll(a.status, &a.n->down, s.asked * a.down_cut.pieces);
-                arrive(s.ready + n % kQueue);
+                layer_arrive(s.ready + n % kQueue);
             }
             summed = true;
         } else {
-            if (warp == 0 && lane == 0) arrive(s.ready + n % kQueue);
+            if (warp == 0 && lane == 0) layer_arrive(s.ready + n % kQueue);
             if (it.kind == kDown && it.i >= known) {
                 if (lane == 0) poll(a.status, &a.n->up[it.i], a.up_cut.pieces);
                 __syncwarp();
@@ -470,9 +450,9 @@ template <typename E, int kAlign> __device__ void bring_rows(const Args& a, Shar
                 const uint32_t w = lane & 7u, first = warp * 4 + (lane >> 3), from_block = r.columns * parts * kBlockBytes;
                 const unsigned char* from = first < rows ? row_at(first) + w * 16 : nullptr;
                 const uint32_t place = first + (first >= it.columns ? gap : 0u);
-                const uint32_t to = address(r.base) + r.x_at + place * kBlockBytes + ((w ^ (place & 7u)) * 16);
+                const uint32_t to = layer_address(r.base) + r.x_at + place * kBlockBytes + ((w ^ (place & 7u)) * 16);
                 for (uint32_t k = 0; k < c.chunks; ++k, at.step(r)) {
-                    wait_for(a.status, s.empty + at.stage, at.round + 1);
+                    layer_wait(a.status, s.empty + at.stage, at.round + 1);
                     if (from) {
                         const int left = (int)(c.row_bytes - k * c.chunk - w * 16);
                         const unsigned char* p = from + k * c.chunk;
@@ -482,7 +462,7 @@ template <typename E, int kAlign> __device__ void bring_rows(const Args& a, Shar
                         for (uint32_t row = first + 16; row < rows; row += 16) {
                             const uint32_t there = row + (row >= it.columns ? gap : 0u);
                             p = row_at(row) + w * 16 + k * c.chunk;
-                            q = address(r.base) + at.stage * r.bytes + r.x_at + there * kBlockBytes + ((w ^ (there & 7u)) * 16);
+                            q = layer_address(r.base) + at.stage * r.bytes + r.x_at + there * kBlockBytes + ((w ^ (there & 7u)) * 16);
                             for (uint32_t b = 0; b < c.across; ++b, p += kBlockBytes, q += from_block) copy_word(q, p, left > (int)(b * kBlockBytes) ? 16u : 0u, lo, hi, a);
                         }
                     }
@@ -492,8 +472,8 @@ template <typename E, int kAlign> __device__ void bring_rows(const Args& a, Shar
                 const uint32_t w = lane & 7u, first = warp * 4 + (lane >> 3);
                 const unsigned char* at_first = first < rows ? row_at(first) : nullptr;
                 for (uint32_t k = 0; k < c.chunks; ++k, at.step(r)) {
-                    wait_for(a.status, s.empty + at.stage, at.round + 1);
-                    const uint32_t to = address(r.base) + at.stage * r.bytes + r.x_at + w * 16;
+                    layer_wait(a.status, s.empty + at.stage, at.round + 1);
+                    const uint32_t to = layer_address(r.base) + at.stage * r.bytes + r.x_at + w * 16;
                     for (uint32_t row = first; row < rows; row += 16) {
                         const unsigned char* from = row == first ? at_first : row_at(row);
                         const unsigned char *end = from + c.row_bytes, *p = from - ((uintptr_t)from & 15u) + k * c.chunk + w * 16;
@@ -506,7 +486,7 @@ template <typename E, int kAlign> __device__ void bring_rows(const Args& a, Shar
             }
         }
         __syncwarp();
-        if (lane == 0) arrive(s.done + n % kQueue);
+        if (lane == 0) layer_arrive(s.done + n % kQueue);
     }
 }
 
@@ -593,7 +573,7 @@ __device__ __forceinline__ void product(const Args& a, Shared& s, const Ring& r,
 #pragma unroll
         for (int q = 0; q < 4; ++q) acc[n][q] = pair[n][0][q] = pair[n][1][q] = 0.0f;
     for (uint32_t k = 0; k < c.chunks; ++k, at.step(r)) {
-        wait_for(a.status, s.full + at.stage, at.round);
+        layer_wait(a.status, s.full + at.stage, at.round);
         for (uint32_t block = way; block < c.across; block += c.ways) {
             const unsigned char* stage = r.base + at.stage * r.bytes;
             const int left = (int)c.row_bytes - (int)(k * c.chunk + block * kBlockBytes);         // of the row from the block on
@@ -630,7 +610,7 @@ __device__ __forceinline__ void product(const Args& a, Shared& s, const Ring& r,
             }
         }
         __syncwarp();
-        if (lane == 0) arrive(s.empty + at.stage);
+        if (lane == 0) layer_arrive(s.empty + at.stage);
     }
     if constexpr (!k32) {
 #pragma unroll
@@ -711,7 +691,7 @@ __device__ void multiply(const Args& a, Shared& s, const Ring& r, uint32_t parts
     Place at = { 0, 0 };
     uint32_t swaps = 0;
     for (uint32_t n = 0;; ++n) {
-        wait_for(a.status, s.queued + n % kQueue, n / kQueue);
+        layer_wait(a.status, s.queued + n % kQueue, n / kQueue);
         const Item it = s.item[n % kQueue];
         if (it.kind == kEnd) break;
         if (it.kind == kUp) {
@@ -719,11 +699,11 @@ __device__ void multiply(const Args& a, Shared& s, const Ring& r, uint32_t parts
         } else if (it.kind == kDown) {
             product_of<E, kAlign, kDown>(a, s, r, it, n, at, swaps);
         } else {
-            wait_for(a.status, s.ready + n % kQueue, n / kQueue);
+            layer_wait(a.status, s.ready + n % kQueue, n / kQueue);
             weighted_sums<E>(a, it.piece, parts);
         }
         __syncwarp();
-        if ((threadIdx.x & 31u) == 0) arrive(s.done + n % kQueue);
+        if ((threadIdx.x & 31u) == 0) layer_arrive(s.done + n % kQueue);
     }
 }
 
@@ -768,13 +748,13 @@ __device__ void keep_books(const Args& a, Shared& s, const Ring& r, uint32_t par
         while (!ended && given - told < kQueue && (given == told || ahead < r.stages)) {
             last = take();
             s.item[given % kQueue] = last;
-            arrive(s.queued + given % kQueue);
+            layer_arrive(s.queued + given % kQueue);
             ++given;
             ahead += stages(last);
             ended = last.kind == kEnd;
         }
         if (ended && told + 1 == given) break;
-        wait_for(a.status, s.done + told % kQueue, told / kQueue);
+        layer_wait(a.status, s.done + told % kQueue, told / kQueue);
         const Item it = s.item[told % kQueue];
         if (it.kind != kSum && !more(it)) {
             __threadfence();
@@ -794,13 +774,13 @@ __global__ void __launch_bounds__(kThreads<kAlign>, 1) experts_kernel(const __gr
     const uint32_t warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) {
         for (uint32_t i = 0; i < kMaxStages; ++i) {
-            set_up(s.full + i, 32 * kRowWarps + (kAlign ? 1 : 32 * kWeightWarps<kAlign>));
-            set_up(s.empty + i, kWorkers);
+            layer_barrier(s.full + i, 32 * kRowWarps + (kAlign ? 1 : 32 * kWeightWarps<kAlign>));
+            layer_barrier(s.empty + i, kWorkers);
         }
         for (uint32_t i = 0; i < kQueue; ++i) {
-            set_up(s.queued + i, 1);
-            set_up(s.ready + i, 1);
-            set_up(s.done + i, kWorkers + kRowWarps + kWeightWarps<kAlign>);
+            layer_barrier(s.queued + i, 1);
+            layer_barrier(s.ready + i, 1);
+            layer_barrier(s.done + i, kWorkers + kRowWarps + kWeightWarps<kAlign>);
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }

@@ -47,8 +47,9 @@ def norm_grad(dy, x, mean, rstd, gamma, lines):
     dx = r * (w - a - n * b)
     inner = 2 * U * np.abs(w) + off_a + U * np.abs(a) + np.abs(n) * off_b + 4 * U * np.abs(n * b)
     off_dx = np.abs(r) * (inner + 2 * U * (np.abs(w) + np.abs(a) + np.abs(n * b)))
-    # rows a block adds up one after the other, its 8 warps, the lines (32 sums of them, then 5 steps); two roundings of n
-    chain = math.ceil(T / max(1, min(T, lines))) + 8 + math.ceil(lines / 32) + 5
+    # rows a thread adds up one after the other (there are 148 blocks at least where there are as many rows), the teams of a block (15 at
+    # most), the lines (32 sums of them, then 5 steps); two roundings of n
+    chain = math.ceil(T / max(1, min(T, 148))) + 15 + math.ceil(lines / 32) + 5
     return (dx, (dy * n).sum(0), dy.sum(0)), (off_dx, (chain + 3) * U * np.abs(dy * n).sum(0), chain * U * np.abs(dy).sum(0))
 
 

@@ -71,8 +71,11 @@ NORM_SIZES = [(1, 1), (2, 2), (3, 7), (5, 17), (257, 33), (70, 128), (9, 129), (
               (3, 5000), (2, 12289), (3, 16384), (2, 33000), (1, 65536)]
 
 
+MANY_ROWS = [(1000, 40), (700, 600), (301, 2048), (20011, 512), (40001, 256), (3001, 1000)]
+
+
 @pytest.mark.parametrize("kind", KINDS)
-@pytest.mark.parametrize("T,D", NORM_SIZES)
+@pytest.mark.parametrize("T,D", NORM_SIZES + MANY_ROWS)
 def test_norm(rows, kind, T, D):
     for params in {kind, "fp32"}:
         x, gamma, beta, _ = norm_inputs(T, D, kind, params)
@@ -84,7 +87,7 @@ def test_norm(rows, kind, T, D):
 
 
 @pytest.mark.parametrize("kind", KINDS)
-@pytest.mark.parametrize("T,D", NORM_SIZES + [(1000, 40), (700, 600), (301, 2048)])
+@pytest.mark.parametrize("T,D", NORM_SIZES + MANY_ROWS)
 def test_norm_grad(rows, kind, T, D):
     for params in {kind, "fp32"}:
         x, gamma, _, dy = norm_inputs(T, D, kind, params, 2)
