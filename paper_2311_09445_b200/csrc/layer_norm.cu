@@ -62,6 +62,25 @@ template <typename E, bool kBroken> __device__ __forceinline__ void keep(Twos<E>
     }
 }
 
+// The bits of a word's elements [lo, hi).
+template <typename E> __device__ __forceinline__ void bits_of(uint32_t (&mask)[4], int lo, int hi)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        mask[i] = 0u;
+#pragma unroll
+        for (int k = 0; k < 4 / (int)sizeof(E); ++k) {
+            const int e = i * (4 / (int)sizeof(E)) + k;
+            if (e >= lo && e < hi) mask[i] |= sizeof(E) == 4 ? 0xFFFFFFFFu : 0xFFFFu << (k * 16);
+        }
+    }
+}
+template <typename E> __device__ __forceinline__ void mask_word(Word<E>& v, const uint32_t (&mask)[4])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v.word[i] &= mask[i];
+}
+
 // ---- parameters in shared memory, as binary32 -----------------------------------------------------------------------------
 // One behind the other where rows are whole words; else (kBroken) those of equal remainder by a word's elements, so that a warp's lanes, whose
 // words are neighbours, find theirs in neighbouring places whatever `off` is.
@@ -69,6 +88,9 @@ template <typename E> __host__ __device__ constexpr uint32_t params_room(uint32_
 template <typename E, typename P, bool kBroken> __device__ __forceinline__ void bring_params(float* to, const void* from, uint32_t D, float otherwise)
 {
     const uint32_t line = D / kN<E> + 3;
+    if (kBroken)                            // (0 beside them: that of a word's elements which are not the row's)
+        for (uint32_t e = threadIdx.x; e < kN<E>; e += blockDim.x) to[e * line] = to[e * line + (D + kN<E> - 1 - e) / kN<E> + 1] = 0.0f;
+#pragma unroll 4
     for (uint32_t e = threadIdx.x; e < D; e += blockDim.x) {
         const float v = from ? RowsElem<P>::up(((const P*)from)[e]) : otherwise;
         to[kBroken ? e % kN<E> * line + e / kN<E> + 1 : e] = v;
@@ -255,6 +277,10 @@ __global__ void __launch_bounds__(kMost, 1)
 #pragma unroll
         for (int q = 0; q < kTwos<E>; ++q) dg[j][q] = db[j][q] = LayerTwo(0.0f);
     const float part = 1.0f / (float)D;
+    uint32_t head[4], end[4];
+    const uint32_t last = (off + D - 1) / kN<E>;
+    bits_of<E>(head, (int)off, kN<E>);
+    bits_of<E>(end, last ? 0 : (int)off, (int)(off + D - last * kN<E>));
     uint32_t odd = 0, stage = 0, round = 0;
     for (; group * f.rows < T; group += step) {
         const uint32_t rows = (uint32_t)min((uint64_t)f.rows, T - group * f.rows);
@@ -272,15 +298,16 @@ __global__ void __launch_bounds__(kMost, 1)
                 const uint32_t w = j * f.threads + me;
                 const int e = (int)(w * kN<E>) - (int)off;
                 if (e >= (int)D) break;
-                a[j] = layer_read<E, kN<E>>(at_dy + w * 16);
-                layer_twos<E, kN<E>>(p, a[j]);
-                keep<E, kBroken>(p, -e, (int)D - e);
                 const int i = kPacked ? 0 : j;
+                a[j] = layer_read<E, kN<E>>(at_dy + w * 16);
                 b[kPacked ? j : 0] = layer_read<E, kN<E>>(at_x + w * 16);
+                if constexpr (kBroken) {                    // (what lies beside the row may be anything)
+                    if (j == 0 && me == 0) { mask_word<E>(a[j], head); mask_word<E>(b[kPacked ? j : 0], head); }
+                    if (w == last) { mask_word<E>(a[j], end); mask_word<E>(b[kPacked ? j : 0], end); }
+                }
+                layer_twos<E, kN<E>>(p, a[j]);
                 layer_twos<E, kN<E>>(n[i], b[kPacked ? j : 0]);
-                keep<E, kBroken>(n[i], -e, (int)D - e);
                 read_params<E, kBroken>(g, params, w, off, D);
-                keep<E, kBroken>(g, -e, (int)D - e);
 #pragma unroll
                 for (int q = 0; q < kTwos<E>; ++q) {
                     n[i][q] = (n[i][q] + LayerTwo(-m)) * LayerTwo(rs);
