@@ -334,8 +334,11 @@ __device__ __forceinline__ void arrive_with_words(uint64_t* barrier)
     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(layer_address(barrier)) : "memory");
 }
 
+// Whose rows (the first products', the second ones') are whole words: tensor copies bring them.
+constexpr int kUpWhole = 1, kDownWhole = 2, kWhole = 3;
+template <int kAlign> __device__ __forceinline__ bool whole_words(uint32_t kind) { return kind == kUp ? (kAlign & kUpWhole) != 0 : (kAlign & kDownWhole) != 0; }
 // The warps that bring weights: one thread of one; eight warps where words have to be cut out of rows.
-template <int kAlign> constexpr uint32_t kWeightWarps = kAlign ? 1 : 8;
+template <int kAlign> constexpr uint32_t kWeightWarps = kAlign == kWhole ? 1 : 8;
 // Those that bring the rows of x or h.
 constexpr uint32_t kRowWarps = 4;
 template <int kAlign> constexpr uint32_t kThreads = (kWorkers + 1 + kRowWarps + kWeightWarps<kAlign>) * 32;
@@ -365,14 +368,17 @@ __device__ void bring_weights(const Args& a, Shared& s, const Ring& r, uint32_t 
         if (it.kind == kEnd) break;
         if (it.kind == kUp || it.kind == kDown) {
             const Cut& c = it.kind == kDown ? a.down_cut : a.up_cut;
-            if constexpr (kAlign != 0) {
+            if (whole_words<kAlign>(it.kind)) {
                 const bool gated = it.kind == kUp && a.act == PEARL_ACT_SILU_GATED;
                 const uint32_t row = it.piece * c.strips * (gated ? 8 : 16), group = s.expert[it.i] * (gated ? 2 : 1);
                 const bool whole = c.row_bytes % kBlockBytes == 0;
                 const CUtensorMap* map = it.kind == kDown ? down_map : up_map;
                 for (uint32_t k = 0; k < c.chunks; ++k, at.step(r)) {
                     layer_wait(a.status, s.empty + at.stage, at.round + 1);
-                    if (lane != 0) continue;
+                    if (warp != 0 || lane != 0) {
+                        if (kAlign != kWhole) layer_arrive(s.full + at.stage);           // (as many arrive for a stage of either kind)
+                        continue;
+                    }
                     unsigned char* to = r.base + at.stage * r.bytes;
                     layer_arrive_with(s.full + at.stage, c.strips * 16 * c.chunk);
                     if (whole) {
@@ -382,7 +388,7 @@ __device__ void bring_weights(const Args& a, Shared& s, const Ring& r, uint32_t 
                             copy_block(s.full + at.stage, to, map, (k * c.across + b) * (kBlockBytes / (uint32_t)sizeof(E)), row, group);
                     }
                 }
-            } else {
+            } else if constexpr (kAlign != kWhole) {
                 // a lane has a word of a block of every 32nd row, and the first of eight lanes the word behind the chunk
                 const unsigned char *lo = it.kind == kDown ? a.down : a.up, *hi = it.kind == kDown ? a.down_end : a.up_end;
                 const uint32_t w = lane & 7u, first = warp * 4 + (lane >> 3);
@@ -447,7 +453,7 @@ template <typename E, int kAlign> __device__ void bring_rows(const Args& a, Shar
                 return it.kind == kDown ? a.h + slot * a.pitch + part * (a.pitch / 2) : a.x + (uint64_t)(slot / a.k) * a.ld_x;
             };
             const unsigned char *lo = it.kind == kDown ? a.h : a.x, *hi = it.kind == kDown ? (const unsigned char*)a.z : a.x_end;
-            if constexpr (kAlign != 0) {
+            if (whole_words<kAlign>(it.kind)) {
                 // a lane's word of a block, of its first row (of 16, the four warps have four each)
                 const uint32_t w = lane & 7u, first = warp * 4 + (lane >> 3), from_block = r.columns * parts * kBlockBytes;
                 const unsigned char* from = first < rows ? row_at(first) + w * 16 : nullptr;
@@ -470,7 +476,7 @@ template <typename E, int kAlign> __device__ void bring_rows(const Args& a, Shar
                     }
                     arrive_with_words(s.full + at.stage);
                 }
-            } else {
+            } else if constexpr (kAlign != kWhole) {
                 const uint32_t w = lane & 7u, first = warp * 4 + (lane >> 3);
                 const unsigned char* at_first = first < rows ? row_at(first) : nullptr;
                 for (uint32_t k = 0; k < c.chunks; ++k, at.step(r)) {
@@ -543,6 +549,7 @@ template <typename E, int kAlign, int NT, uint32_t kKind>
 __device__ __forceinline__ void product(const Args& a, Shared& s, const Ring& r, const Item& it, uint32_t number, Place& at, uint32_t& swaps)
 {
     constexpr bool k32 = sizeof(E) == 4, kSecond = kKind == kDown;
+    constexpr int kHow = kAlign & (kSecond ? kDownWhole : kUpWhole);
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3u;
     const Cut& c = kSecond ? a.down_cut : a.up_cut;
     const uint32_t way = warp % c.ways, strip = warp / c.ways;
@@ -552,22 +559,22 @@ __device__ __forceinline__ void product(const Args& a, Shared& s, const Ring& r,
     // the lane's rows in a stage
     const uint32_t ra = strip * (gated ? 8 : 16) + g, rb = gated ? ra + c.strips * 8 : ra + 8;
     // (and from one block to the next)
-    const uint32_t to_a = kAlign ? ra * kBlockBytes + ((2 * t) ^ g) * 16 : ra * c.pitch + t * 32, to_next = kAlign ? c.strips * 16 * kBlockBytes : kBlockBytes;
-    const uint32_t to_b = kAlign ? rb * kBlockBytes + ((2 * t) ^ g) * 16 : rb * c.pitch + t * 32;
+    const uint32_t to_a = kHow ? ra * kBlockBytes + ((2 * t) ^ g) * 16 : ra * c.pitch + t * 32, to_next = kHow ? c.strips * 16 * kBlockBytes : kBlockBytes;
+    const uint32_t to_b = kHow ? rb * kBlockBytes + ((2 * t) ^ g) * 16 : rb * c.pitch + t * 32;
     uint32_t off_a = 0, off_b = 0;
-    if constexpr (kAlign == 0) {
+    if constexpr (kHow == 0) {
         off_a = (uint32_t)(uintptr_t)weight_row<E>(a, s, c, it, ra) & 15u;
         off_b = (uint32_t)(uintptr_t)weight_row<E>(a, s, c, it, rb) & 15u;
     }
     constexpr uint32_t kParts = kSecond && !k32 ? 2 : 1;
-    const uint32_t pitch = kAlign ? kBlockBytes : c.pitch;
-    const uint32_t to_x = r.x_at + (kAlign ? g * kBlockBytes + ((2 * t) ^ g) * 16 : g * pitch + t * 32);
-    const uint32_t to_next_x = kAlign ? r.columns * kParts * kBlockBytes : kBlockBytes;
+    const uint32_t pitch = kHow ? kBlockBytes : c.pitch;
+    const uint32_t to_x = r.x_at + (kHow ? g * kBlockBytes + ((2 * t) ^ g) * 16 : g * pitch + t * 32);
+    const uint32_t to_next_x = kHow ? r.columns * kParts * kBlockBytes : kBlockBytes;
     uint32_t off_x[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const uint32_t col = n * 8 + g;
-        off_x[n] = kAlign || kSecond || col >= it.columns ? 0u : (uint32_t)(uintptr_t)(a.x + (uint64_t)(s.slot[it.first + col] / a.k) * a.ld_x) & 15u;
+        off_x[n] = kHow || kSecond || col >= it.columns ? 0u : (uint32_t)(uintptr_t)(a.x + (uint64_t)(s.slot[it.first + col] / a.k) * a.ld_x) & 15u;
     }
     float acc[NT][4], pair[NT][2][4];          // (two sums of 16-bit products, so that an instruction need not wait for the one before)
 #pragma unroll
@@ -580,9 +587,9 @@ __device__ __forceinline__ void product(const Args& a, Shared& s, const Ring& r,
             const unsigned char* stage = r.base + at.stage * r.bytes;
             const int left = (int)c.row_bytes - (int)(k * c.chunk + block * kBlockBytes);         // of the row from the block on
             if (left <= 0) break;
-            const bool tail = kAlign == 0 && left < (int)kBlockBytes;        // (else both sides have zeros there)
+            const bool tail = kHow == 0 && left < (int)kBlockBytes;        // (else both sides have zeros there)
             const int here = left - (int)(t * 32);                           // from the lane's piece on
-            const RowsRaw<32> va = piece_at<kAlign>(stage + block * to_next + to_a, off_a, here, tail), vb = piece_at<kAlign>(stage + block * to_next + to_b, off_b, here, tail);
+            const RowsRaw<32> va = piece_at<kHow>(stage + block * to_next + to_a, off_a, here, tail), vb = piece_at<kHow>(stage + block * to_next + to_b, off_b, here, tail);
             stage += block * to_next_x;
             RowsRaw<32> ah, al, bh, bl;
             if constexpr (k32) {
@@ -591,7 +598,7 @@ __device__ __forceinline__ void product(const Args& a, Shared& s, const Ring& r,
             }
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const RowsRaw<32> x = piece_at<kAlign>(stage + to_x + n * 8 * pitch, off_x[n], here, tail);
+                const RowsRaw<32> x = piece_at<kHow>(stage + to_x + n * 8 * pitch, off_x[n], here, tail);
                 if constexpr (k32) {
                     RowsRaw<32> xh, xl;
                     split(xh, xl, x);
@@ -607,7 +614,7 @@ __device__ __forceinline__ void product(const Args& a, Shared& s, const Ring& r,
                     for (int q = 0; q < 4; ++q) acc[n][q] += (part[0][q] + part[1][q]) + part[2][q];
                 } else {
                     block_product<E>(pair[n], va, vb, x);
-                    if constexpr (kSecond) block_product<E>(pair[n], va, vb, piece_at<kAlign>(stage + to_x + (r.columns + n * 8) * pitch, 0u, here, tail));
+                    if constexpr (kSecond) block_product<E>(pair[n], va, vb, piece_at<kHow>(stage + to_x + (r.columns + n * 8) * pitch, 0u, here, tail));
                 }
             }
         }
@@ -776,7 +783,7 @@ __global__ void __launch_bounds__(kThreads<kAlign>, 1) experts_kernel(const __gr
     const uint32_t warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) {
         for (uint32_t i = 0; i < kMaxStages; ++i) {
-            layer_barrier(s.full + i, 32 * kRowWarps + (kAlign ? 1 : 32 * kWeightWarps<kAlign>));
+            layer_barrier(s.full + i, 32 * kRowWarps + (kAlign == kWhole ? 1 : 32 * kWeightWarps<kAlign>));
             layer_barrier(s.empty + i, kWorkers);
         }
         for (uint32_t i = 0; i < kQueue; ++i) {
@@ -840,8 +847,9 @@ template <typename T, int kAlign> int experts_launch(const Args& a, uint32_t dty
     }
     CUtensorMap up = {}, down = {};
     const bool gated = a.act == PEARL_ACT_SILU_GATED;
-    if (kAlign && (!map_of(&up, dtype, a.up, a.D, a.H, (uint64_t)a.E * (gated ? 2 : 1), a.up_cut, a.up_cut.strips * (gated ? 8 : 16), gated ? 2 : 1) ||
-                   !map_of(&down, dtype, a.down, a.H, a.D, a.E, a.down_cut, a.down_cut.strips * 16, 1)))
+    if (((kAlign & kUpWhole) &&
+         !map_of(&up, dtype, a.up, a.D, a.H, (uint64_t)a.E * (gated ? 2 : 1), a.up_cut, a.up_cut.strips * (gated ? 8 : 16), gated ? 2 : 1)) ||
+        ((kAlign & kDownWhole) && !map_of(&down, dtype, a.down, a.H, a.D, a.E, a.down_cut, a.down_cut.strips * 16, 1)))
         return -1;
     return rows_launch(experts_kernel<T, kAlign>, dim3(rows_sm_count()), dim3(kThreads<kAlign>), kSharedBytes + kRingBytes, s, 0, a, up, down);
 }
@@ -867,17 +875,17 @@ template <typename T> int experts_as(unsigned* status, const LayerExperts& a, cu
     Args args = { a.T, a.D, a.H, a.E, a.k, a.act, Cut(), Cut(), x, x + ((uint64_t)(a.T - 1) * a.ld_x + a.D) * S, up,
                         up + matrix * (a.act == PEARL_ACT_SILU_GATED ? 2 : 1), down, down + matrix, a.ld_x * S, a.ld_y * S, l.pitch, a.w, a.ids,
                         (unsigned char*)a.y, work + l.h, (float*)(work + l.z), (Counters*)work, work + l.bytes, status };
-    const uint32_t granule = rows_granule((uintptr_t)a.x | (uintptr_t)a.up, (uintptr_t)a.down, a.ld_x * S, (uint64_t)a.D * S, (uint64_t)a.H * S);
     const bool gated = a.act == PEARL_ACT_SILU_GATED;
+    const bool up_whole = rows_granule((uintptr_t)a.x, (uintptr_t)a.up, a.ld_x * S, (uint64_t)a.D * S) >= 16, down_whole = rows_granule((uintptr_t)a.down, (uint64_t)a.H * S) >= 16;
     const uint32_t rows = gated ? a.H * 2 : a.H, slots = a.T * a.k, experts = slots < a.E ? slots : a.E;
-    const bool words = granule < 16;
-    args.up_cut = cut_of(rows, a.D * S, experts, words);
-    args.down_cut = cut_of(a.D, a.H * S, experts, words);
+    args.up_cut = cut_of(rows, a.D * S, experts, !up_whole);
+    args.down_cut = cut_of(a.D, a.H * S, experts, !down_whole);
     if (ring_of(nullptr, args.up_cut, args.down_cut, slots, S == 2 ? 2 : 1).stages < 2) {       // many rows for few experts: smaller stages
-        args.up_cut = cut_as(rows, a.D * S, 1, 1, words);
-        args.down_cut = cut_as(a.D, a.H * S, 1, 1, words);
+        args.up_cut = cut_as(rows, a.D * S, 1, 1, !up_whole);
+        args.down_cut = cut_as(a.D, a.H * S, 1, 1, !down_whole);
     }
-    m = words ? experts_launch<T, 0>(args, a.dtype, s) : experts_launch<T, 16>(args, a.dtype, s);
+    m = up_whole ? (down_whole ? experts_launch<T, kWhole>(args, a.dtype, s) : experts_launch<T, kUpWhole>(args, a.dtype, s))
+                 : (down_whole ? experts_launch<T, kDownWhole>(args, a.dtype, s) : experts_launch<T, 0>(args, a.dtype, s));
     return m < 0 ? m : n + m;
 }
 

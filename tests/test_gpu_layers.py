@@ -260,7 +260,7 @@ def run_layer(rows, x, router, up, down, w, ids, gated, chosen, work=None, y=Non
 
 LAYERS = [(1, 16, 16, 2, 1), (1, 1, 1, 1, 1), (3, 17, 5, 3, 2), (2, 64, 64, 8, 2), (9, 500, 333, 16, 4), (64, 128, 96, 4, 2), (5, 256, 40, 130, 8),
           (33, 72, 200, 5, 5), (64, 65, 63, 2, 1), (17, 1024, 128, 6, 3), (8, 40, 1000, 4, 2), (64, 32, 32, 40, 32), (1, 2048, 512, 16, 8),
-          (12, 66, 34, 7, 2), (40, 520, 264, 3, 2)]
+          (12, 66, 34, 7, 2), (40, 520, 264, 3, 2), (6, 256, 130, 5, 2), (6, 250, 128, 5, 2), (64, 512, 77, 3, 2)]
 
 
 @pytest.mark.parametrize("kind", KINDS)
