@@ -142,16 +142,17 @@ __device__ __forceinline__ void block_product(float (&c)[2][4], const RowsRaw<32
 #pragma unroll
     for (int i = 0; i < 4; ++i) mma16(c[i % 2], a.r[2 * i], b.r[2 * i], a.r[2 * i + 1], b.r[2 * i + 1], x.r[2 * i], x.r[2 * i + 1], E());
 }
-// binary32 as the sum of two numbers of 11 bits, each rounded to nearest (ties away from zero): what is left out of a product is 2^-22 of it.  By
-// additions to the bits: the conversion instruction, at a quarter of an SM's lanes, was what the products waited for (64 experts of
-// 2048 x 1408 for 64 rows 579 us).
-__device__ __forceinline__ uint32_t rounded(uint32_t bits) { return (bits + 0x1000u) & 0xFFFFE000u; }
+// binary32 as the sum of two numbers of 11 bits, the upper one rounded to nearest (ties away from zero), by an addition to the bits: the conversion
+// instruction, at a quarter of an SM's lanes, was what the products waited for (64 experts of 2048 x 1408 for 64 rows 579 us).  What is left has
+// 12 bits at most and loses the last of them: nearest would be no nearer.  So a part is off by 2^-23 of the number, and a product, with that of the
+// two lower parts left out, by 2^-21.  A NaN's upper part may be anything (the addition runs over into the sign for the largest); its lower one is a
+// NaN, as cutting off bits leaves that one which arithmetic gives, and so is an infinity's.
 __device__ __forceinline__ void split(RowsRaw<32>& high, RowsRaw<32>& low, const RowsRaw<32>& v)
 {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        high.r[i] = rounded(v.r[i]);
-        low.r[i] = rounded(__float_as_uint(__uint_as_float(v.r[i]) - __uint_as_float(high.r[i])));
+        high.r[i] = (v.r[i] + 0x1000u) & 0xFFFFE000u;
+        low.r[i] = __float_as_uint(__uint_as_float(v.r[i]) - __uint_as_float(high.r[i])) & 0xFFFFE000u;
     }
 }
 

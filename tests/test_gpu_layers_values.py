@@ -1,0 +1,69 @@
+"""A layer's operators on the GPU where values are special: NaN and infinity in what is chosen, numbers that need all of binary32, constant rows."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import layer_reference as ref
+from test_gpu_layers import KINDS, TYPES, f64, gen, layer_inputs, norm_inputs, rows, run_layer, run_norm, strided  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def given(T, k, E, *seed):
+    """Weights and experts of T rows; the last row asks for none."""
+    g = gen(*seed)
+    ids = torch.stack([torch.randperm(E, generator=g)[:k] for _ in range(T)]).to(torch.int32)
+    ids[-1] = -1
+    return torch.rand(T, k, generator=g) + 0.5, ids
+
+
+# ---- NaN and infinity in what the experts' products take -------------------------------------------------------------
+
+# (the last ones in binary32: NaNs that arithmetic on a GPU gives, with a sign, with the lowest bit alone, and next to what rounds to them)
+VALUES = {"nan": math.nan, "+inf": math.inf, "-inf": -math.inf, "all ones": 0x7FFFFFFF, "all ones and sign": 0xFFFFFFFF, "upper ones": 0x7FFFF000,
+          "lowest bit": 0x7F800001, "below the upper ones": 0x7FFFEFFF}
+
+
+def special(value, kind):
+    if isinstance(value, float):
+        return torch.tensor(value, dtype=TYPES[kind])
+    return torch.from_numpy(np.array([value], np.uint32).view(np.float32))[0].to(TYPES[kind])
+
+
+def not_finite(rows, kind, gated, where, D, H):  # noqa: F811
+    T, E, k, row, e = 7, 5, 2, 2, 3
+    x, _, up, down = layer_inputs(T, D, H, E, k, kind, gated, 50)
+    w, ids = given(T, k, E, 51)
+    ids[row, 0], ids[row, 1] = e, (e + 1) % E
+    plain = run_layer(rows, x.cuda(), None, up.cuda(), down.cuda(), w.cuda(), ids.cuda(), gated, True).cpu()
+    for name, value in VALUES.items():
+        if kind != "fp32" and not isinstance(value, float):
+            continue
+        parts = {"x": x.clone(), "up": up.clone(), "down": down.clone()}
+        at = {"x": (row, 5), "up": (e, H - 2, D - 1), "down": (e, D - 3, H - 1)}[where]
+        parts[where][at] = special(value, kind)
+        y = run_layer(rows, parts["x"].cuda(), None, parts["up"].cuda(), parts["down"].cuda(), w.cuda(), ids.cuda(), gated, True).cpu()
+        with np.errstate(all="ignore"):
+            want = ref.experts(f64(parts["x"]), f64(parts["up"]), f64(parts["down"]), f64(w), ids.numpy(), kind, gated)[0]
+        touched = torch.zeros(T, D, dtype=torch.bool)
+        meets = torch.arange(T) == row if where == "x" else (ids == e).any(1)
+        touched[meets, D - 3 if where == "down" else slice(None)] = True
+        assert touched.any() and torch.equal(y[~touched], plain[~touched]), name
+        want = torch.from_numpy(want)
+        if kind == "fp32":
+            assert y[touched].isnan().all(), (name, y[touched])
+        else:
+            assert torch.equal(y[touched].isnan(), want[touched].isnan()), name
+            infinite = touched & want.isinf()
+            assert torch.equal(y[infinite].double(), want[infinite]), name
+    assert rows.sync() == 0
+
+
+@pytest.mark.parametrize("gated", [True, False], ids=["gated", "relu"])
+@pytest.mark.parametrize("where", ["x", "up", "down"])
+@pytest.mark.parametrize("D,H", [(48, 32), (47, 31)])
+def test_expert_layer_in_binary32_keeps_what_is_not_finite(rows, gated, where, D, H):  # noqa: F811
+    """A NaN or an infinity among the factors gives NaN where it is used, and no other bit changes."""
+    not_finite(rows, "fp32", gated, where, D, H)
