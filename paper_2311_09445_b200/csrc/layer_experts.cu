@@ -19,7 +19,10 @@ namespace {
 constexpr uint32_t kWorkers = 8;              // warps that multiply
 constexpr uint32_t kBlockBytes = 128;         // of a row: what a warp takes of 16 weight rows in one step, 32 bytes a lane of each of two rows
 constexpr uint32_t kMaxSlots = PEARL_LAYER_MAX_FEW * PEARL_ROWS_MAX_CHOICES;
-constexpr uint32_t kMaxColumns = 64;          // slots of an expert that are multiplied at once
+// Slots of an expert that are multiplied at once; one with more is gone over again, its weights from L2.  In 16 bits a thread's sums for 64 and those of
+// a stage do not fit its registers: 64 rows on 8 experts of 2048 x 1408, 4 a row, binary16, 182 us, so 98; with 64 slots at each of 4 experts of
+// 4096 x 1280 in binary32, which has one sum, 315 and 358.
+template <typename E> constexpr uint32_t kMaxColumns = sizeof(E) == 4 ? 64 : 32;
 constexpr uint32_t kSpins = kLayerSpins;
 
 // The parts of the scratch, in bytes from its start.  The counters are zero between calls.
@@ -299,11 +302,12 @@ struct Ring {
     uint32_t columns;                   // rows of x (or h) that it has room for, at most
 };
 // (the lower halves of h lie behind all the upper ones)
-__host__ __device__ __forceinline__ Ring ring_of(unsigned char* base, const Cut& up, const Cut& down, uint32_t most, uint32_t parts)
+template <typename E> __host__ __device__ __forceinline__ Ring ring_of(unsigned char* base, const Cut& up, const Cut& down, uint32_t most)
 {
+    constexpr uint32_t parts = sizeof(E) == 4 ? 1 : 2;
     Ring r;
     r.base = base;
-    r.columns = most <= 8 ? 8u : most <= 16 ? 16u : most <= 32 ? 32u : kMaxColumns;
+    r.columns = most <= 8 ? 8u : most <= 16 ? 16u : most <= 32 ? 32u : kMaxColumns<E>;
     const uint32_t weights = up.strips * up.pitch > down.strips * down.pitch ? up.strips * up.pitch : down.strips * down.pitch;
     const uint32_t rows = up.pitch > parts * down.pitch ? up.pitch : parts * down.pitch;
     r.x_at = (weights * 16 + 1023) / 1024 * 1024;
@@ -584,7 +588,9 @@ __device__ __forceinline__ void product(const Args& a, Shared& s, const Ring& r,
         const uint32_t col = n * 8 + g;
         off_x[n] = kHow || kSecond || col >= it.columns ? 0u : (uint32_t)(uintptr_t)(a.x + (uint64_t)(s.slot[it.first + col] / a.k) * a.ld_x) & 15u;
     }
-    float acc[NT][4], pair[NT][2][4];          // (two sums of 16-bit products, so that an instruction need not wait for the one before)
+    // Two sums of 16-bit products over a stage, so that an instruction need not wait for the one before.  Where a sum grows the instruction cuts off, so
+    // what a stage has is added to the sum so far by additions that round.
+    float acc[NT][4], pair[NT][2][4];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -628,12 +634,15 @@ __device__ __forceinline__ void product(const Args& a, Shared& s, const Ring& r,
         }
         __syncwarp();
         if (lane == 0) layer_arrive(s.empty + at.stage);
-    }
-    if constexpr (!k32) {
+        if constexpr (!k32) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) acc[n][q] = pair[n][0][q] + pair[n][1][q];
+                for (int q = 0; q < 4; ++q) {
+                    acc[n][q] += pair[n][0][q] + pair[n][1][q];
+                    pair[n][0][q] = pair[n][1][q] = 0.0f;
+                }
+        }
     }
     // the warps that share a strip: their sums in order, 16 columns at a time
     if (c.ways > 1) {
@@ -682,8 +691,8 @@ __device__ __forceinline__ void product_of(const Args& a, Shared& s, const Ring&
 {
     if (it.columns <= 8) product<E, kAlign, 1, kKind>(a, s, r, it, number, at, swaps);
     else if (it.columns <= 16) product<E, kAlign, 2, kKind>(a, s, r, it, number, at, swaps);
-    else if (it.columns <= 32) product<E, kAlign, 4, kKind>(a, s, r, it, number, at, swaps);
-    else product<E, kAlign, 8, kKind>(a, s, r, it, number, at, swaps);
+    else if (kMaxColumns<E> == 32 || it.columns <= 32) product<E, kAlign, 4, kKind>(a, s, r, it, number, at, swaps);
+    else product<E, kAlign, kMaxColumns<E> / 8, kKind>(a, s, r, it, number, at, swaps);
 }
 
 // A part of y, of `parts`: the slots' sums in the order of the choices.
@@ -728,7 +737,7 @@ __device__ void multiply(const Args& a, Shared& s, const Ring& r, uint32_t parts
 // hands them to the others, some way ahead, and tells what is finished.  It alone fences, and it has no copies on their way, for which a fence
 // would wait.  A CTA waits only with its earlier pieces told, and each piece that it waits for is with a CTA that runs: nobody waits for
 // one that is yet to be launched.
-__device__ void keep_books(const Args& a, Shared& s, const Ring& r, uint32_t parts, uint32_t ticket)
+template <typename E> __device__ void keep_books(const Args& a, Shared& s, const Ring& r, uint32_t parts, uint32_t ticket)
 {
     const Cut &up = a.up_cut, &down = a.down_cut;
     const uint32_t ups = s.asked * up.pieces, downs = s.asked * down.pieces;
@@ -736,10 +745,10 @@ __device__ void keep_books(const Args& a, Shared& s, const Ring& r, uint32_t par
     const auto more = [&](const Item& it) { return it.kind <= kDown && it.first + it.columns < s.first[it.i + 1]; };
     const auto take = [&] {
         Item it = { kEnd, 0, 0, 0, 0 };
-        if (more(last)) {                    // an expert of more than 64 slots is gone over once for each 64
+        if (more(last)) {                    // an expert of more slots is gone over again
             it = last;
             it.first = last.first + last.columns;
-            it.columns = min(s.first[it.i + 1] - it.first, kMaxColumns);
+            it.columns = min(s.first[it.i + 1] - it.first, kMaxColumns<E>);
             return it;
         }
         const uint32_t task = ticket;
@@ -755,7 +764,7 @@ __device__ void keep_books(const Args& a, Shared& s, const Ring& r, uint32_t par
         it.i = n / pieces;
         it.piece = n - it.i * pieces;
         it.first = s.first[it.i];
-        it.columns = min(s.first[it.i + 1] - it.first, kMaxColumns);
+        it.columns = min(s.first[it.i + 1] - it.first, kMaxColumns<E>);
         return it;
     };
     const auto stages = [&](const Item& it) { return it.kind == kUp ? up.chunks : it.kind == kDown ? down.chunks : 0u; };
@@ -805,10 +814,10 @@ __global__ void __launch_bounds__(kThreads<kAlign>, 1) experts_kernel(const __gr
     uint32_t ticket = 0;
     if (threadIdx.x == kWorkers * 32) ticket = atomicAdd(&a.n->ticket, 1u);
     plan(a, s);
-    const Ring r = ring_of(memory + kSharedBytes, a.up_cut, a.down_cut, s.most, sizeof(E) == 4 ? 1 : 2);
+    const Ring r = ring_of<E>(memory + kSharedBytes, a.up_cut, a.down_cut, s.most);
     const uint32_t parts = min(gridDim.x, (uint32_t)(((uint64_t)a.T * a.D + kWorkers * 32 - 1) / (kWorkers * 32)));
     if (warp < kWorkers) multiply<E, kAlign>(a, s, r, parts);
-    else if (threadIdx.x == kWorkers * 32) keep_books(a, s, r, parts, ticket);
+    else if (threadIdx.x == kWorkers * 32) keep_books<E>(a, s, r, parts, ticket);
     else if (warp > kWorkers + kRowWarps) bring_weights<E, kAlign>(a, s, r, warp - kWorkers - kRowWarps - 1, &up_map, &down_map);
     else if (warp > kWorkers) bring_rows<E, kAlign>(a, s, r, warp - kWorkers - 1);
     __syncwarp();
@@ -888,7 +897,7 @@ template <typename T> int experts_as(unsigned* status, const LayerExperts& a, cu
     const uint32_t rows = gated ? a.H * 2 : a.H, slots = a.T * a.k, experts = slots < a.E ? slots : a.E;
     args.up_cut = cut_of(rows, a.D * S, experts, !up_whole);
     args.down_cut = cut_of(a.D, a.H * S, experts, !down_whole);
-    if (ring_of(nullptr, args.up_cut, args.down_cut, slots, S == 2 ? 2 : 1).stages < 2) {       // many rows for few experts: smaller stages
+    if (ring_of<T>(nullptr, args.up_cut, args.down_cut, slots).stages < 2) {       // many rows for few experts: smaller stages
         args.up_cut = cut_as(rows, a.D * S, 1, 1, !up_whole);
         args.down_cut = cut_as(a.D, a.H * S, 1, 1, !down_whole);
     }

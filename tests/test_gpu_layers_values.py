@@ -67,3 +67,28 @@ def not_finite(rows, kind, gated, where, D, H):  # noqa: F811
 def test_expert_layer_in_binary32_keeps_what_is_not_finite(rows, gated, where, D, H):  # noqa: F811
     """A NaN or an infinity among the factors gives NaN where it is used, and no other bit changes."""
     not_finite(rows, "fp32", gated, where, D, H)
+
+
+# ---- sums and products to the digits that binary32 has ----------------------------------------------------------------
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_expert_layer_adds_blocks_rounding_to_nearest(rows, kind):  # noqa: F811
+    """A large number and then, block after block of 64 numbers, three quarters of the last place of it.  A matrix instruction may cut off up to a place
+    where its own sum has the large number; the sums of some blocks are added with half a place each.  So most of the terms are there."""
+    T, D, H, E = 24, 2048, 520, 24                                # (enough pieces for every SM, so that one warp has a whole row)
+    large = 2.0 ** (15 if kind == "fp16" else 24)
+    place = large * 2.0 ** -23
+    x, up, down = torch.ones(T, D), torch.zeros(E, H, D), torch.zeros(E, D, H)
+    first = torch.arange(64) % 16 < 4                             # (the columns of one instruction's step, in each of a block's four parts)
+    up[:, :2, :64][:, :, first] = large / 16
+    up[:, 0, 64::64] = 0.75 * place
+    down[:, :, 0], down[:, :, 1] = 1, -1
+    ids = torch.arange(T, dtype=torch.int32).view(T, 1)
+    t = TYPES[kind]
+    y = f64(run_layer(rows, x.to(t).cuda(), None, up.to(t).cuda(), down.to(t).cuda(), torch.ones(T, 1).cuda(), ids.cuda(), False, True))
+    blocks = D // 64 - 1
+    want = 0.75 * place * blocks
+    # a place for each of three blocks beside the large number, half a place for each block, and for h's own rounding and two of the second product
+    limit = (3 + 0.5 * blocks + 1.5) * place
+    assert limit < want
+    ref.within(y, np.full_like(y, want), limit, kind)
