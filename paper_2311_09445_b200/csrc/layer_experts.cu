@@ -32,16 +32,21 @@ struct Counters {
     uint32_t up[PEARL_ROWS_MAX_EXPERTS];               // of an expert's first product
 };
 struct Layout {
-    uint64_t logits, h, z, bytes, pitch;
+    uint64_t logits, h, z, bytes, part;
 };
+// How many numbers of the rows' type an h between the products is the sum of: as many as keep it to a binary32's digits (store_h).
+constexpr uint32_t kMostParts = 3;
+template <typename E> constexpr uint32_t kParts = 1;
+template <> constexpr uint32_t kParts<__half> = 2;
+template <> constexpr uint32_t kParts<__nv_bfloat16> = 3;
 Layout layout_of(uint32_t T, uint32_t D, uint32_t H, uint32_t E, uint32_t k)
 {
     const auto up = [](uint64_t n) { return (n + 255) / 256 * 256; };
     Layout l;
-    l.pitch = 2 * ((2ull * H + 127) / 128 * 128);       // of a slot's h: two rows of 16 bits, or one of 32
+    l.part = (2ull * H + 127) / 128 * 128;              // of a slot's h: up to three rows of 16 bits, or one of 32
     l.logits = up(sizeof(Counters));
     l.h = l.logits + up((uint64_t)T * E * 4);
-    l.z = l.h + up((uint64_t)T * k * l.pitch);
+    l.z = l.h + up((uint64_t)T * k * kMostParts * l.part);
     l.bytes = l.z + up((uint64_t)T * k * D * 4);
     return l;
 }
@@ -140,10 +145,10 @@ __device__ __forceinline__ void mma8(float (&c)[4], uint32_t a0, uint32_t a1, ui
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 template <typename E>
-__device__ __forceinline__ void block_product(float (&c)[2][4], const RowsRaw<32>& a, const RowsRaw<32>& b, const RowsRaw<32>& x)
+__device__ __forceinline__ void block_product(float (&c)[4], float (&d)[4], const RowsRaw<32>& a, const RowsRaw<32>& b, const RowsRaw<32>& x)
 {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) mma16(c[i % 2], a.r[2 * i], b.r[2 * i], a.r[2 * i + 1], b.r[2 * i + 1], x.r[2 * i], x.r[2 * i + 1], E());
+    for (int i = 0; i < 4; ++i) mma16(i % 2 ? d : c, a.r[2 * i], b.r[2 * i], a.r[2 * i + 1], b.r[2 * i + 1], x.r[2 * i], x.r[2 * i + 1], E());
 }
 // binary32 as the sum of two numbers of 11 bits, the upper one rounded to nearest (ties away from zero), by an addition to the bits: the conversion
 // instruction, at a quarter of an SM's lanes, was what the products waited for (64 experts of 2048 x 1408 for 64 rows 579 us).  What is left has
@@ -195,7 +200,7 @@ struct Args {
     uint32_t T, D, H, E, k, act;
     Cut up_cut, down_cut;
     const unsigned char *x, *x_end, *up, *up_end, *down, *down_end;
-    uint64_t ld_x, ld_y, pitch;         // bytes
+    uint64_t ld_x, ld_y, part;          // bytes; of a part of a slot's h
     const float* w;
     const int32_t* ids;
     unsigned char *y, *h;
@@ -301,15 +306,14 @@ struct Ring {
     uint32_t stages, bytes, x_at;       // bytes of a stage; where the rows of x are in it
     uint32_t columns;                   // rows of x (or h) that it has room for, at most
 };
-// (the lower halves of h lie behind all the upper ones)
+// (the lower parts of h lie behind all the upper ones)
 template <typename E> __host__ __device__ __forceinline__ Ring ring_of(unsigned char* base, const Cut& up, const Cut& down, uint32_t most)
 {
-    constexpr uint32_t parts = sizeof(E) == 4 ? 1 : 2;
     Ring r;
     r.base = base;
     r.columns = most <= 8 ? 8u : most <= 16 ? 16u : most <= 32 ? 32u : kMaxColumns<E>;
     const uint32_t weights = up.strips * up.pitch > down.strips * down.pitch ? up.strips * up.pitch : down.strips * down.pitch;
-    const uint32_t rows = up.pitch > parts * down.pitch ? up.pitch : parts * down.pitch;
+    const uint32_t rows = up.pitch > kParts<E> * down.pitch ? up.pitch : kParts<E> * down.pitch;
     r.x_at = (weights * 16 + 1023) / 1024 * 1024;
     r.bytes = r.x_at + (r.columns * rows + 1023) / 1024 * 1024;
     r.stages = kRingBytes / r.bytes < kMaxStages ? kRingBytes / r.bytes : kMaxStages;
@@ -457,19 +461,21 @@ template <typename E, int kAlign> __device__ void bring_rows(const Args& a, Shar
                 known = it.i + 1;
             }
             const Cut& c = it.kind == kDown ? a.down_cut : a.up_cut;
-            const uint32_t parts = it.kind == kDown && sizeof(E) == 2 ? 2u : 1u;
+            const uint32_t parts = it.kind == kDown ? kParts<E> : 1u;
             // Rows that there are none of are not brought: a column of a product goes by its own row alone.
-            const uint32_t rows = it.columns * parts, gap = (r.columns - it.columns) * (parts - 1);        // (between the parts)
+            const uint32_t rows = it.columns * parts;
+            const auto part_of = [&](uint32_t row) { return (row >= it.columns ? 1u : 0u) + (row >= 2 * it.columns ? 1u : 0u); };
+            const auto place_of = [&](uint32_t row) { return row + part_of(row) * (r.columns - it.columns); };
             const auto row_at = [&](uint32_t row) {
-                const uint32_t part = row >= it.columns ? 1u : 0u, slot = s.slot[it.first + row - part * it.columns];
-                return it.kind == kDown ? a.h + slot * a.pitch + part * (a.pitch / 2) : a.x + (uint64_t)(slot / a.k) * a.ld_x;
+                const uint32_t part = part_of(row), slot = s.slot[it.first + row - part * it.columns];
+                return it.kind == kDown ? a.h + (slot * kMostParts + part) * a.part : a.x + (uint64_t)(slot / a.k) * a.ld_x;
             };
             const unsigned char *lo = it.kind == kDown ? a.h : a.x, *hi = it.kind == kDown ? (const unsigned char*)a.z : a.x_end;
             if (whole_words<kAlign>(it.kind)) {
                 // a lane's word of a block, of its first row (of 16, the four warps have four each)
                 const uint32_t w = lane & 7u, first = warp * 4 + (lane >> 3), from_block = r.columns * parts * kBlockBytes;
                 const unsigned char* from = first < rows ? row_at(first) + w * 16 : nullptr;
-                const uint32_t place = first + (first >= it.columns ? gap : 0u);
+                const uint32_t place = place_of(first);
                 const uint32_t to = layer_address(r.base) + r.x_at + place * kBlockBytes + ((w ^ (place & 7u)) * 16);
                 for (uint32_t k = 0; k < c.chunks; ++k, at.step(r)) {
                     layer_wait(a.status, s.empty + at.stage, at.round + 1);
@@ -480,7 +486,7 @@ template <typename E, int kAlign> __device__ void bring_rows(const Args& a, Shar
 #pragma unroll 2
                         for (uint32_t b = 0; b < c.across; ++b, p += kBlockBytes, q += from_block) copy_word(q, p, left > (int)(b * kBlockBytes) ? 16u : 0u, lo, hi, a);
                         for (uint32_t row = first + 16; row < rows; row += 16) {
-                            const uint32_t there = row + (row >= it.columns ? gap : 0u);
+                            const uint32_t there = place_of(row);
                             p = row_at(row) + w * 16 + k * c.chunk;
                             q = layer_address(r.base) + at.stage * r.bytes + r.x_at + there * kBlockBytes + ((w ^ (there & 7u)) * 16);
                             for (uint32_t b = 0; b < c.across; ++b, p += kBlockBytes, q += from_block) copy_word(q, p, left > (int)(b * kBlockBytes) ? 16u : 0u, lo, hi, a);
@@ -497,7 +503,7 @@ template <typename E, int kAlign> __device__ void bring_rows(const Args& a, Shar
                     for (uint32_t row = first; row < rows; row += 16) {
                         const unsigned char* from = row == first ? at_first : row_at(row);
                         const unsigned char *end = from + c.row_bytes, *p = from - ((uintptr_t)from & 15u) + k * c.chunk + w * 16;
-                        uint32_t q = to + (row + (row >= it.columns ? gap : 0u)) * c.pitch;
+                        uint32_t q = to + place_of(row) * c.pitch;
                         for (uint32_t b = 0; b < c.across + (w == 0); ++b, p += kBlockBytes, q += kBlockBytes)
                             if (p < end) copy_word(q, p, (uint32_t)min((long long)16, (long long)(hi - p)), lo, hi, a);
                     }
@@ -541,18 +547,28 @@ template <int kAlign> __device__ __forceinline__ RowsRaw<32> piece_at(const unsi
 
 __device__ __forceinline__ float activated(float gate, float value) { return gate / (1.0f + expf(-gate)) * value; }
 
-// h[slot][j] = v: in 16 bits as the sum of two, as a single one would be off by as much as the result's own rounding.
+// h[slot][j] = v, as the sum of parts that keeps a binary32's digits: three of bfloat16's 8 bits each, which is all of them; two of binary16's
+// 11, the second one times 2^11, so that it runs out of exponents that much later: 2^-22 of h, and 2^-36.  (With two of bfloat16 seven times as many results
+// had another last place than those of a sum in 64 bits, 2.4 in 1000 of the layer of 64 rows and 128 experts of 4096 x 1280; it took 702 us, this 735.)
+constexpr float kLowerHalf = 2048.0f;
 template <typename E> __device__ __forceinline__ void store_h(const Args& a, uint32_t slot, uint32_t j, float v)
 {
-    unsigned char* row = a.h + slot * a.pitch;
-    if (!ROWS_IN_ARRAY(a.status, row + (uint64_t)j * sizeof(E), sizeof(E), a.h, a.z)) return;
+    unsigned char* row = a.h + slot * kMostParts * a.part;
+    if (!ROWS_IN_ARRAY(a.status, row + (uint64_t)j * sizeof(E), (kParts<E> - 1) * a.part + sizeof(E), a.h, a.z)) return;
     if constexpr (sizeof(E) == 4) {
         reinterpret_cast<float*>(row)[j] = v;
     } else {
-        const E high = RowsElem<E>::down(v);
-        const float rest = v - RowsElem<E>::up(high);
-        reinterpret_cast<E*>(row)[j] = high;
-        reinterpret_cast<E*>(row + a.pitch / 2)[j] = RowsElem<E>::down(isfinite(RowsElem<E>::up(high)) ? rest : 0.0f);
+        E part = RowsElem<E>::down(v);
+        reinterpret_cast<E*>(row)[j] = part;
+        float rest = isfinite(RowsElem<E>::up(part)) ? v - RowsElem<E>::up(part) : 0.0f;
+        if constexpr (kParts<E> == 2) {
+            reinterpret_cast<E*>(row + a.part)[j] = RowsElem<E>::down(rest * kLowerHalf);
+        } else {
+            part = RowsElem<E>::down(rest);
+            reinterpret_cast<E*>(row + a.part)[j] = part;
+            rest -= RowsElem<E>::up(part);
+            reinterpret_cast<E*>(row + 2 * a.part)[j] = RowsElem<E>::down(rest);
+        }
     }
 }
 
@@ -578,18 +594,17 @@ __device__ __forceinline__ void product(const Args& a, Shared& s, const Ring& r,
         off_a = (uint32_t)(uintptr_t)weight_row<E>(a, s, c, it, ra) & 15u;
         off_b = (uint32_t)(uintptr_t)weight_row<E>(a, s, c, it, rb) & 15u;
     }
-    constexpr uint32_t kParts = kSecond && !k32 ? 2 : 1;
     const uint32_t pitch = kHow ? kBlockBytes : c.pitch;
     const uint32_t to_x = r.x_at + (kHow ? g * kBlockBytes + ((2 * t) ^ g) * 16 : g * pitch + t * 32);
-    const uint32_t to_next_x = kHow ? r.columns * kParts * kBlockBytes : kBlockBytes;
+    const uint32_t to_next_x = kHow ? r.columns * (kSecond ? kParts<E> : 1) * kBlockBytes : kBlockBytes;
     uint32_t off_x[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const uint32_t col = n * 8 + g;
         off_x[n] = kHow || kSecond || col >= it.columns ? 0u : (uint32_t)(uintptr_t)(a.x + (uint64_t)(s.slot[it.first + col] / a.k) * a.ld_x) & 15u;
     }
-    // Two sums of 16-bit products over a stage, so that an instruction need not wait for the one before.  Where a sum grows the instruction cuts off, so
-    // what a stage has is added to the sum so far by additions that round.
+    // Two sums of 16-bit products over a stage, so that an instruction need not wait for the one before (the second product's: of h's upper parts, of
+    // the others).  Where a sum grows the instruction cuts off, so what a stage has is added to the sum so far by additions that round.
     float acc[NT][4], pair[NT][2][4];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -627,8 +642,10 @@ __device__ __forceinline__ void product(const Args& a, Shared& s, const Ring& r,
 #pragma unroll
                     for (int q = 0; q < 4; ++q) acc[n][q] += (part[0][q] + part[1][q]) + part[2][q];
                 } else {
-                    block_product<E>(pair[n], va, vb, x);
-                    if constexpr (kSecond) block_product<E>(pair[n], va, vb, piece_at<kHow>(stage + to_x + (r.columns + n * 8) * pitch, 0u, here, tail));
+                    block_product<E>(pair[n][0], kSecond ? pair[n][0] : pair[n][1], va, vb, x);
+#pragma unroll
+                    for (uint32_t part = 1; kSecond && part < kParts<E>; ++part)
+                        block_product<E>(pair[n][1], pair[n][1], va, vb, piece_at<kHow>(stage + to_x + (part * r.columns + n * 8) * pitch, 0u, here, tail));
                 }
             }
         }
@@ -639,7 +656,7 @@ __device__ __forceinline__ void product(const Args& a, Shared& s, const Ring& r,
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    acc[n][q] += pair[n][0][q] + pair[n][1][q];
+                    acc[n][q] += pair[n][0][q] + (kSecond && kParts<E> == 2 ? pair[n][1][q] * (1.0f / kLowerHalf) : pair[n][1][q]);
                     pair[n][0][q] = pair[n][1][q] = 0.0f;
                 }
         }
@@ -890,7 +907,7 @@ template <typename T> int experts_as(unsigned* status, const LayerExperts& a, cu
     const unsigned char *up = (const unsigned char*)a.up, *down = (const unsigned char*)a.down;
     const uint64_t matrix = (uint64_t)a.E * a.D * a.H * S;
     Args args = { a.T, a.D, a.H, a.E, a.k, a.act, Cut(), Cut(), x, x + ((uint64_t)(a.T - 1) * a.ld_x + a.D) * S, up,
-                        up + matrix * (a.act == PEARL_ACT_SILU_GATED ? 2 : 1), down, down + matrix, a.ld_x * S, a.ld_y * S, l.pitch, a.w, a.ids,
+                        up + matrix * (a.act == PEARL_ACT_SILU_GATED ? 2 : 1), down, down + matrix, a.ld_x * S, a.ld_y * S, l.part, a.w, a.ids,
                         (unsigned char*)a.y, work + l.h, (float*)(work + l.z), (Counters*)work, work + l.bytes, status };
     const bool gated = a.act == PEARL_ACT_SILU_GATED;
     const bool up_whole = rows_granule((uintptr_t)a.x, (uintptr_t)a.up, a.ld_x * S, (uint64_t)a.D * S) >= 16, down_whole = rows_granule((uintptr_t)a.down, (uint64_t)a.H * S) >= 16;

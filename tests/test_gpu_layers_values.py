@@ -92,3 +92,54 @@ def test_expert_layer_adds_blocks_rounding_to_nearest(rows, kind):  # noqa: F811
     limit = (3 + 0.5 * blocks + 1.5) * place
     assert limit < want
     ref.within(y, np.full_like(y, want), limit, kind)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("D,H,most,most16,times", [(8, 8, 255, 90, 2), (64, 2, 255, 31, 1), (512, 256, 255, 90, 2), (501, 123, 255, 90, 2)])
+def test_expert_layer_on_whole_numbers(rows, kind, D, H, most, most16, times):  # noqa: F811
+    """Whole numbers of up to 22 bits between the products (16 in binary16) whose differences are the results: every sum is exact in binary32."""
+    g = gen(60, D, H)
+    T, E, terms, pairs = 9, 4, min(D, 64 if H == 2 else 8), min(H // 2, 4)
+    most = most16 if kind == "fp16" else most
+    x, up, down = torch.zeros(T, D), torch.zeros(E, H, D), torch.zeros(E, D, H)
+    at = torch.randperm(D, generator=g)[:terms]
+    x[:, at] = torch.randint(0, most + 1, (T, terms), generator=g).float()
+    x[:, at[0]] = 1
+    for e in range(E):
+        for i in (torch.randperm(H // 2, generator=g)[:pairs] * 2).tolist():
+            up[e, i, at] = torch.randint(0, most - 2, (terms,), generator=g).float()
+            up[e, i + 1] = up[e, i]
+            up[e, i + 1, at[0]] += int(torch.randint(1, 4, (1,), generator=g))
+            f = torch.randint(-times, times + 1, (D,), generator=g).float()
+            down[e, :, i], down[e, :, i + 1] = -f, f
+    ids = torch.randint(0, E, (T, 1), generator=g, dtype=torch.int32)
+    t = TYPES[kind]
+    y = run_layer(rows, x.to(t).cuda(), None, up.to(t).cuda(), down.to(t).cuda(), torch.ones(T, 1).cuda(), ids.cuda(), False, True)
+    want = torch.stack([down[e].double() @ (up[e].double() @ row.double()) for row, e in zip(x, ids[:, 0].tolist())])
+    assert want.abs().max() > 0 and torch.equal(y.cpu().double(), want)
+
+
+@pytest.mark.parametrize("size", [1e-2, 1e-4, 1e-6])
+def test_expert_layer_binary16_of_small_numbers_between_the_products(rows, size):  # noqa: F811
+    """An h of the given size against large weights: it is kept to 2^-22 of it, give or take 2^-36."""
+    T, D, H, E, k = 9, 64, 96, 4, 2
+    g = gen(61)
+    x = (0.05 * torch.randn(T, D, generator=g)).half()
+    up = (size / 0.05 * D ** -0.5 * torch.randn(E, H, D, generator=g)).half()
+    down = (min(0.3 / size, 2000.0) * torch.randn(E, D, H, generator=g)).half()
+    w, ids = given(T, k, E, 62)
+    y = f64(run_layer(rows, x.cuda(), None, up.cuda(), down.cuda(), w.cuda(), ids.cuda(), False, True))
+    X, U, V = f64(x), f64(up), f64(down)
+    want, off = np.zeros((T, D)), np.zeros((T, D))
+    for t in range(T):
+        for j in range(k):
+            e = int(ids[t, j])
+            if e < 0:
+                continue
+            h = np.maximum(U[e] @ X[t], 0)
+            # additions: of a product's terms at most as many, each with two half steps where an instruction cuts off
+            dh = 2 * D * ref.U * (np.abs(U[e]) @ np.abs(X[t])) + 2.0 ** -22 * h + 2.0 ** -36
+            want[t] += float(w[t, j]) * (V[e] @ h)
+            off[t] += float(w[t, j]) * (np.abs(V[e]) @ dh + 2 * (H + k + 4) * ref.U * (np.abs(V[e]) @ h))
+    ref.within(y, want, off, "fp16")
+    assert np.abs(want).mean() > 1e-4
