@@ -656,7 +656,10 @@ __device__ __forceinline__ void product(const Args& a, Shared& s, const Ring& r,
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    acc[n][q] += pair[n][0][q] + (kSecond && kParts<E> == 2 ? pair[n][1][q] * (1.0f / kLowerHalf) : pair[n][1][q]);
+                    float rest = kSecond && kParts<E> == 2 ? pair[n][1][q] * (1.0f / kLowerHalf) : pair[n][1][q];
+                    // (an infinite weight: what it makes of the upper part)
+                    if (kSecond && !isfinite(pair[n][0][q])) rest = 0.0f;
+                    acc[n][q] += pair[n][0][q] + rest;
                     pair[n][0][q] = pair[n][1][q] = 0.0f;
                 }
         }

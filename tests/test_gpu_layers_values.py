@@ -69,6 +69,15 @@ def test_expert_layer_in_binary32_keeps_what_is_not_finite(rows, gated, where, D
     not_finite(rows, "fp32", gated, where, D, H)
 
 
+@pytest.mark.parametrize("kind", ["fp16", "bf16"])
+@pytest.mark.parametrize("gated", [True, False], ids=["gated", "relu"])
+@pytest.mark.parametrize("where", ["x", "up", "down"])
+@pytest.mark.parametrize("D,H", [(48, 32), (47, 31)])
+def test_expert_layer_in_16_bits_keeps_what_is_not_finite(rows, kind, gated, where, D, H):  # noqa: F811
+    """It reaches the results as the definition has it, and no other bit changes."""
+    not_finite(rows, kind, gated, where, D, H)
+
+
 # ---- sums and products to the digits that binary32 has ----------------------------------------------------------------
 
 @pytest.mark.parametrize("kind", KINDS)
