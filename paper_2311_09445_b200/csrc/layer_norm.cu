@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(kThreads<NV>, 1) norm_kernel(uint32_t T, uint3
         fetch(t + step);
         float s[1] = { all.sum() };
         team_sums<1>(threads, team, s, sums[0]);
-        const float mean = s[0] * part;
+        const float mean = s[0] / (float)D;          // (times 1 / D it would be off by a unit of the last place, which a row that hardly differs from it shows)
         all = LayerTwo(0.0f);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
@@ -280,7 +280,6 @@ __global__ void __launch_bounds__(kMost, 1)
     for (int j = 0; j < NV; ++j)
 #pragma unroll
         for (int q = 0; q < kTwos<E>; ++q) dg[j][q] = db[j][q] = LayerTwo(0.0f);
-    const float part = 1.0f / (float)D;
     uint32_t head[4], end[4];
     const uint32_t last = (off + D - 1) / kN<E>;
     bits_of<E>(head, (int)off, kN<E>);
@@ -333,7 +332,7 @@ __global__ void __launch_bounds__(kMost, 1)
                 if (++stage == f.stages) { stage = 0; ++round; }
             }
             if (dx == nullptr) continue;
-            const LayerTwo off_row(-s[0] * part), along_row(-s[1] * part);
+            const LayerTwo off_row(-s[0] / (float)D), along_row(-s[1] / (float)D);          // (divided, as the mean is)
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
                 const uint32_t w = j * f.threads + me;

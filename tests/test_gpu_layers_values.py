@@ -152,3 +152,37 @@ def test_expert_layer_binary16_of_small_numbers_between_the_products(rows, size)
             off[t] += float(w[t, j]) * (np.abs(V[e]) @ dh + 2 * (H + k + 4) * ref.U * (np.abs(V[e]) @ h))
     ref.within(y, want, off, "fp16")
     assert np.abs(want).mean() > 1e-4
+
+
+# ---- constant rows of the norm -----------------------------------------------------------------------------------------
+
+CONSTANT = [(41, 4096.0), (83, 1000.0), (83, 30000.0), (1000, 1000.0), (2047, 1000.0), (4099, 24.0)]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("D,value", CONSTANT)
+def test_norm_of_constant_rows(rows, kind, D, value):  # noqa: F811
+    """Their sum is exact, so the mean is the value itself: the result is the bias, and 1 / sqrt(eps)."""
+    _, gamma, beta, _ = norm_inputs(3, D, kind, "fp32", 70)
+    for extra, shift, other in ((0, 0, 0), (3, 1, 1), (0, 0, 1)):          # (`other`: rows of y at another place than those of x)
+        x = torch.full((3, D), value).to(TYPES[kind])
+        y = strided(torch.zeros_like(x), extra + other, shift + other)
+        got = run_norm(rows, strided(x, extra, shift), gamma.cuda(), beta.cuda(), y=y)
+        assert torch.equal(got[1].cpu(), x[:, 0].float())
+        np.testing.assert_allclose(f64(got[2]), 1e-5 ** -0.5, rtol=4 * ref.U)
+        assert torch.equal(got[0].cpu(), beta.to(TYPES[kind]).expand(3, D))
+    assert rows.sync() == 0
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("D,value", CONSTANT)
+def test_norm_grad_of_constant_rows(rows, kind, D, value):  # noqa: F811
+    """A constant gradient of a constant row is taken out of it whole."""
+    for extra, shift, other in ((0, 0, 0), (3, 1, 1), (0, 0, 1)):
+        dy = torch.full((3, D), value).to(TYPES[kind])
+        x = torch.full((3, D), 2.0).to(TYPES[kind])
+        dx = strided(torch.ones_like(x), extra + other, shift + other)
+        rows.layer_norm_grad(strided(dy, extra, shift), strided(x, extra, shift), torch.full((3,), 2.0, device="cuda"),
+                             torch.full((3,), 300.0, device="cuda"), None, dx)
+        assert (dx == 0).all()
+    assert rows.sync() == 0
