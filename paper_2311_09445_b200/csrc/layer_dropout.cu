@@ -28,6 +28,7 @@ __device__ __forceinline__ void philox4x32_10(uint32_t (&c)[4], uint32_t k0, uin
 }
 
 struct Args {
+    unsigned* status;
     uint32_t T, D, below;
     float scale;
     uint64_t ld_x, ld_r, ld_y, seed, call;
@@ -67,9 +68,11 @@ __global__ void __launch_bounds__(kThreads) dropout_kernel(uint32_t across, uint
 #pragma unroll
         for (int j = 0; j < kGroup / N; ++j) {
             const uint64_t t = t0 + (uint64_t)k * down;
-            const int there = t < a.T ? n - j * N : 0;
-            v[k][j] = layer_load_part<E, N>(x + t * a.ld_x + col + j * N, there);
-            if (residual) r[k][j] = layer_load_part<E, N>(residual + t * a.ld_r + col + j * N, there);
+            int there = t < a.T ? n - j * N : 0;
+            const E *p = x + t * a.ld_x + col + j * N, *q = residual + t * a.ld_r + col + j * N;
+            if (!layer_in_rows<N>(a.status, p, 0, there, x, layer_end(x, a.T, a.D, a.ld_x))) there = 0;
+            v[k][j] = layer_load_part<E, N>(p, there);
+            if (residual && layer_in_rows<N>(a.status, q, 0, there, residual, layer_end(residual, a.T, a.D, a.ld_r))) r[k][j] = layer_load_part<E, N>(q, there);
             else r[k][j].clear();
         }
     const uint64_t call = a.call + (a.calls ? *a.calls : 0);
@@ -87,8 +90,11 @@ __global__ void __launch_bounds__(kThreads) dropout_kernel(uint32_t across, uint
         const uint64_t t = t0 + (uint64_t)k * down;
         if (t >= a.T) break;
 #pragma unroll
-        for (int j = 0; j < kGroup / N; ++j)
-            layer_store_part<E, N>(y + t * a.ld_y + col + j * N, dropped<E, N>(v[k][j], r[k][j], c[k], j * N, a), n - j * N);
+        for (int j = 0; j < kGroup / N; ++j) {
+            E* p = y + t * a.ld_y + col + j * N;
+            if (layer_in_rows<N, E>(a.status, p, 0, n - j * N, y, layer_end(y, a.T, a.D, a.ld_y)))
+                layer_store_part<E, N>(p, dropped<E, N>(v[k][j], r[k][j], c[k], j * N, a), n - j * N);
+        }
     }
 }
 
@@ -110,9 +116,10 @@ __global__ void __launch_bounds__(kThreads) dropout_any_kernel(uint32_t parts, u
     const bool works = lane > 0 && e < D;
     RowsVec<E, N> v[M], r[M];
     // elements [lo, hi) of the N at p
-    const auto load = [](const E* p, int lo, int hi) {
+    const auto load = [&](const E* p, int lo, int hi, const E* first, uint64_t ld) {
         RowsVec<E, N> w;
         w.clear();
+        if (!layer_in_rows<N>(a.status, p, lo, hi, first, layer_end(first, a.T, a.D, ld))) return w;
         if (lo <= 0 && hi >= N) {
             rows_load_if<false>(true, w.raw, p);
         } else {
@@ -128,8 +135,8 @@ __global__ void __launch_bounds__(kThreads) dropout_any_kernel(uint32_t parts, u
 #pragma unroll
     for (int j = 0; j < M; ++j) {
         const int lo = works ? -(e + j * N) : N, hi = D - (e + j * N);
-        v[j] = load(row + e + j * N, lo, hi);
-        if (residual) r[j] = load(residual + t * a.ld_r + e + j * N, lo, hi);
+        v[j] = load(row + e + j * N, lo, hi, x, a.ld_x);
+        if (residual) r[j] = load(residual + t * a.ld_r + e + j * N, lo, hi, residual, a.ld_r);
         else r[j].clear();
     }
     const uint64_t call = a.call + (a.calls ? *a.calls : 0);
@@ -159,6 +166,7 @@ __global__ void __launch_bounds__(kThreads) dropout_any_kernel(uint32_t parts, u
         const RowsVec<E, N> o = dropped<E, N>(v[j], r[j], bits, j * N, a);
         E* to = y + t * a.ld_y + e + j * N;
         const int lo = -(e + j * N), hi = D - (e + j * N);
+        if (!layer_in_rows<N, E>(a.status, to, lo, hi, y, layer_end(y, a.T, a.D, a.ld_y))) continue;
         if (lo <= 0 && hi >= N) {
             rows_store(to, o.raw);
         } else {
@@ -200,10 +208,10 @@ template <typename E> int dropout_of(const Args& a, const void* x, const void* r
 
 }  // namespace
 
-int layer_launch_dropout(uint32_t T, uint32_t D, uint32_t dtype, const void* x, uint64_t ld_x, const void* residual, uint64_t ld_r, uint32_t below,
+int layer_launch_dropout(unsigned* status, uint32_t T, uint32_t D, uint32_t dtype, const void* x, uint64_t ld_x, const void* residual, uint64_t ld_r, uint32_t below,
                          float scale, uint64_t seed, uint64_t call, const uint64_t* calls, void* y, uint64_t ld_y, cudaStream_t s)
 {
-    const Args a = { T, D, below, scale, ld_x, ld_r, ld_y, seed, call, calls };
+    const Args a = { status, T, D, below, scale, ld_x, ld_r, ld_y, seed, call, calls };
 #define DROP(E) return dropout_of<E>(a, x, residual, y, s)
     ROWS_WITH_TYPE(dtype, DROP);
 #undef DROP

@@ -27,7 +27,7 @@ int pearl_layer_norm(pearl_rows_t* h, uint32_t T, uint32_t D, uint32_t dtype, co
     if (misaligned(x, S) || misaligned(y, S) || misaligned(gamma, P) || misaligned(beta, P) || misaligned(mean, 4) || misaligned(rstd, 4))
         return PEARL_ERR_ALIGN;
     return enqueue(h, [&] {
-        return layer_launch_norm(T, D, dtype, x, apart(T, ld_x), ptype, gamma, beta, (float)eps, y, apart(T, ld_y), mean, rstd, h->stream);
+        return layer_launch_norm(h->status, T, D, dtype, x, apart(T, ld_x), ptype, gamma, beta, (float)eps, y, apart(T, ld_y), mean, rstd, h->stream);
     });
 }
 
@@ -78,7 +78,7 @@ int pearl_layer_dropout(pearl_rows_t* h, uint32_t T, uint32_t D, uint32_t dtype,
     const uint32_t below = (uint32_t)floor(65536.0 * p + 0.5);
     const float scale = below < 65536u ? (float)(65536.0 / (double)(65536u - below)) : 0.0f;
     return enqueue(h, [&] {
-        return layer_launch_dropout(T, D, dtype, x, apart(T, ld_x), residual, apart(T, ld_r), below, scale, seed, call, calls, y,
+        return layer_launch_dropout(h->status, T, D, dtype, x, apart(T, ld_x), residual, apart(T, ld_r), below, scale, seed, call, calls, y,
                                     apart(T, ld_y), h->stream);
     });
 }

@@ -4,14 +4,14 @@
 #include "rows_internal.cuh"
 
 // Kernel launchers; each returns the number of kernels launched (0: nothing to do), or -1 on a launch error.
-int layer_launch_norm(uint32_t T, uint32_t D, uint32_t dtype, const void* x, uint64_t ld_x, uint32_t ptype, const void* gamma, const void* beta,
-                      float eps, void* y, uint64_t ld_y, float* mean, float* rstd, cudaStream_t s);
+int layer_launch_norm(unsigned* status, uint32_t T, uint32_t D, uint32_t dtype, const void* x, uint64_t ld_x, uint32_t ptype, const void* gamma,
+                      const void* beta, float eps, void* y, uint64_t ld_y, float* mean, float* rstd, cudaStream_t s);
 int layer_launch_norm_grad(unsigned* status, uint32_t T, uint32_t D, uint32_t dtype, const void* dy, uint64_t ld_dy, const void* x, uint64_t ld_x,
                            const float* mean, const float* rstd, uint32_t ptype, const void* gamma, void* dx, uint64_t ld_dx, float* dgamma,
                            float* dbeta, float* work, uint64_t work_bytes, cudaStream_t s);
 uint64_t layer_norm_grad_work_bytes(uint32_t T, uint32_t D);
-int layer_launch_dropout(uint32_t T, uint32_t D, uint32_t dtype, const void* x, uint64_t ld_x, const void* residual, uint64_t ld_r, uint32_t below,
-                         float scale, uint64_t seed, uint64_t call, const uint64_t* calls, void* y, uint64_t ld_y, cudaStream_t s);
+int layer_launch_dropout(unsigned* status, uint32_t T, uint32_t D, uint32_t dtype, const void* x, uint64_t ld_x, const void* residual, uint64_t ld_r,
+                         uint32_t below, float scale, uint64_t seed, uint64_t call, const uint64_t* calls, void* y, uint64_t ld_y, cudaStream_t s);
 
 struct LayerExperts {
     uint32_t T, D, H, E, k, dtype, act;
@@ -26,6 +26,20 @@ int layer_launch_experts(unsigned* status, const LayerExperts& a, cudaStream_t s
 uint64_t layer_experts_work_bytes(uint32_t T, uint32_t D, uint32_t H, uint32_t E, uint32_t k);
 
 #ifdef __CUDACC__
+
+// The checked build compares with their extents: the words of rows that the norm, its gradient and dropout load and store, the bulk copies of the gradient's
+// ring (with the rest of the words that a row starts and ends in), the places of parameters in shared memory, the blocks' lines of scratch; the
+// expert layer's logits, copied words, h and results of slots.
+// The end of a matrix's last row.
+template <typename E> __device__ __forceinline__ const E* layer_end(const E* p, uint32_t T, uint32_t D, uint64_t ld) { return p + (uint64_t)(T - 1) * ld + D; }
+// Whether elements [lo, hi) of the N at p, those of them that there are, lie in a matrix.
+template <int N, typename E>
+__device__ __forceinline__ bool layer_in_rows(unsigned* status, const E* p, int lo, int hi, const E* first, const E* end)
+{
+    lo = lo > 0 ? lo : 0;
+    hi = hi < N ? hi : N;
+    return lo >= hi || ROWS_IN_ARRAY(status, p + lo, (hi - lo) * (int)sizeof(E), first, end);
+}
 
 // ---- two binary32 numbers at once (add, multiply and multiply-add take them in one instruction) ------------------------
 struct LayerTwo {

@@ -98,8 +98,9 @@ template <typename E, typename P, bool kBroken> __device__ __forceinline__ void 
     }
 }
 // Those of word w (any numbers for elements that the row does not have).
-template <typename E, bool kBroken> __device__ __forceinline__ void read_params(Twos<E>& p, const float* from, uint32_t w, uint32_t off, uint32_t D)
+template <typename E, bool kBroken> __device__ __forceinline__ void read_params(unsigned* status, Twos<E>& p, const float* from, uint32_t w, uint32_t off, uint32_t D)
 {
+    if (!ROWS_IN_BOUNDS(status, kBroken ? w <= D / kN<E> + 1 : (w + 1) * kN<E> <= D)) w = 0;
     if constexpr (kBroken) {
         const uint32_t line = D / kN<E> + 3;
         float f[kN<E>];
@@ -141,8 +142,8 @@ template <int M> __device__ __forceinline__ void team_sums(uint32_t threads, uin
 // length), 8192 of binary32 27 (5.0 TB/s).  A block a row took 44, with four words a thread and no row ahead 34.
 template <int NV> constexpr uint32_t kThreads = NV == 4 ? 768 : 1024;           // of a block: what the registers have room for
 template <typename E, typename P, int NV, bool kBroken>
-__global__ void __launch_bounds__(kThreads<NV>, 1) norm_kernel(uint32_t T, uint32_t D, uint32_t threads, const E* x, uint64_t ld_x, const void* gamma, const void* beta,
-                                                           float eps, E* y, uint64_t ld_y, float* mean_out, float* rstd_out)
+__global__ void __launch_bounds__(kThreads<NV>, 1) norm_kernel(unsigned* status, uint32_t T, uint32_t D, uint32_t threads, const E* x, uint64_t ld_x,
+                                                           const void* gamma, const void* beta, float eps, E* y, uint64_t ld_y, float* mean_out, float* rstd_out)
 {
     extern __shared__ __align__(16) float params[];
     __shared__ float sums[2][1][32];
@@ -158,7 +159,8 @@ __global__ void __launch_bounds__(kThreads<NV>, 1) norm_kernel(uint32_t T, uint3
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int e = (int)((j * threads + me) * kN<E>) - (int)off;
-            if (row < T && e < (int)D) next[j] = load_word<E, kBroken>(p + e, -e, (int)D - e);
+            if (row < T && e < (int)D && layer_in_rows<kN<E>>(status, p + e, -e, (int)D - e, x, layer_end(x, T, D, ld_x)))
+                next[j] = load_word<E, kBroken>(p + e, -e, (int)D - e);
             else next[j].clear();
         }
     };
@@ -205,18 +207,20 @@ __global__ void __launch_bounds__(kThreads<NV>, 1) norm_kernel(uint32_t T, uint3
             const int e = (int)(w * kN<E>) - (int)off;
             if (e >= (int)D) break;
             Twos<E> g, out;
-            read_params<E, kBroken>(g, params, w, off, D);
+            read_params<E, kBroken>(status, g, params, w, off, D);
 #pragma unroll
             for (int q = 0; q < kTwos<E>; ++q) out[q] = g[q] * LayerTwo(rstd);
             if (beta) {
-                read_params<E, kBroken>(g, bias, w, off, D);
+                read_params<E, kBroken>(status, g, bias, w, off, D);
 #pragma unroll
                 for (int q = 0; q < kTwos<E>; ++q) out[q] = layer_fma(v[j][q], out[q], g[q]);
             } else {
 #pragma unroll
                 for (int q = 0; q < kTwos<E>; ++q) out[q] = v[j][q] * out[q];
             }
-            store_word<E, kBroken>(y + t * ld_y + e, layer_access<E, kN<E>>(out), -e, (int)D - e);
+            E* to = y + t * ld_y + e;
+            if (layer_in_rows<kN<E>, E>(status, to, -e, (int)D - e, y, layer_end(y, T, D, ld_y)))
+                store_word<E, kBroken>(to, layer_access<E, kN<E>>(out), -e, (int)D - e);
         }
     }
 }
@@ -262,6 +266,14 @@ __global__ void __launch_bounds__(kMost, 1)
         if (t >= T) return;
         const uint32_t rows = (uint32_t)min((uint64_t)f.rows, T - t);
         const uint32_t bytes = f.rows > 1 ? rows * f.pitch : ((off + D) * (uint32_t)sizeof(E) + 15) / 16 * 16;
+        // (with the rest of the words that they start and end in)
+        const auto there = [&](const E* from, const E* first, uint64_t ld) {
+            return ROWS_IN_ARRAY(status, from, bytes, (uintptr_t)first & ~(uintptr_t)15, ((uintptr_t)layer_end(first, T, D, ld) + 15) & ~(uintptr_t)15);
+        };
+        if (!there(dy + t * ld_dy - off, dy, ld_dy) || !there(x + t * ld_x - off, x, ld_x)) {
+            layer_arrive(full + stage);
+            return;
+        }
         layer_arrive_with(full + stage, 2 * bytes);
         unsigned char* to = ring + stage * 2 * f.rows * f.pitch;
         const auto copy = [&](unsigned char* at, const E* from) {
@@ -310,7 +322,7 @@ __global__ void __launch_bounds__(kMost, 1)
                 }
                 layer_twos<E, kN<E>>(p, a[j]);
                 layer_twos<E, kN<E>>(n[i], b[kPacked ? j : 0]);
-                read_params<E, kBroken>(g, params, w, off, D);
+                read_params<E, kBroken>(status, g, params, w, off, D);
 #pragma unroll
                 for (int q = 0; q < kTwos<E>; ++q) {
                     n[i][q] = (n[i][q] + LayerTwo(-m)) * LayerTwo(rs);
@@ -344,10 +356,12 @@ __global__ void __launch_bounds__(kMost, 1)
 #pragma unroll
                     for (int q = 0; q < kTwos<E>; ++q) n[0][q] = (n[0][q] + LayerTwo(-before_m)) * LayerTwo(now);
                 }
-                read_params<E, kBroken>(g, params, w, off, D);
+                read_params<E, kBroken>(status, g, params, w, off, D);
 #pragma unroll
                 for (int q = 0; q < kTwos<E>; ++q) p[q] = layer_fma(n[kPacked ? 0 : j][q], along_row, layer_fma(p[q], g[q], off_row)) * LayerTwo(now);
-                store_word<E, kBroken>(dx + t * ld_dx + e, layer_access<E, kN<E>>(p), -e, (int)D - e);
+                E* to = dx + t * ld_dx + e;
+                if (layer_in_rows<kN<E>, E>(status, to, -e, (int)D - e, dx, layer_end(dx, T, D, ld_dx)))
+                    store_word<E, kBroken>(to, layer_access<E, kN<E>>(p), -e, (int)D - e);
             }
         }
     }
@@ -490,6 +504,7 @@ bool same_place(const void* a, uint64_t ld_a, const void* b, uint64_t ld_b, uint
 }
 
 struct NormArgs {
+    unsigned* status;
     uint32_t T, D;
     const void *x, *gamma, *beta;
     uint64_t ld_x, ld_y;
@@ -503,7 +518,7 @@ template <typename E, typename P, int NV, bool kBroken> int norm_with(const Norm
     if (!shared_memory(norm_kernel<E, P, NV, kBroken>, ready)) return -1;
     const uint32_t whole = kThreads<NV> / threads, teams = threads > 32 && whole > 15 ? 15 : whole, most = rows_sm_count();
     const uint64_t blocks = ((uint64_t)a.T + teams - 1) / teams;
-    return rows_launch(norm_kernel<E, P, NV, kBroken>, dim3((uint32_t)(blocks < most ? blocks : most)), dim3(teams * threads), shared, s, 0, a.T, a.D, threads,
+    return rows_launch(norm_kernel<E, P, NV, kBroken>, dim3((uint32_t)(blocks < most ? blocks : most)), dim3(teams * threads), shared, s, 0, a.status, a.T, a.D, threads,
                        (const E*)a.x, a.ld_x, a.gamma, a.beta, a.eps, (E*)a.y, a.ld_y, a.mean, a.rstd);
 }
 template <typename E, typename P> int norm_as(const NormArgs& a, cudaStream_t s)
@@ -613,10 +628,10 @@ template <typename E, typename P> int grad_as(const GradArgs& a, cudaStream_t s)
 
 }  // namespace
 
-int layer_launch_norm(uint32_t T, uint32_t D, uint32_t dtype, const void* x, uint64_t ld_x, uint32_t ptype, const void* gamma, const void* beta, float eps,
-                      void* y, uint64_t ld_y, float* mean, float* rstd, cudaStream_t s)
+int layer_launch_norm(unsigned* status, uint32_t T, uint32_t D, uint32_t dtype, const void* x, uint64_t ld_x, uint32_t ptype, const void* gamma, const void* beta,
+                      float eps, void* y, uint64_t ld_y, float* mean, float* rstd, cudaStream_t s)
 {
-    const NormArgs a = { T, D, x, gamma, beta, ld_x, ld_y, eps, y, mean, rstd };
+    const NormArgs a = { status, T, D, x, gamma, beta, ld_x, ld_y, eps, y, mean, rstd };
 #define NORM_AS(E, P) return norm_as<E, P>(a, s)
     WITH_TYPES(dtype, ptype, NORM_AS);
 #undef NORM_AS
