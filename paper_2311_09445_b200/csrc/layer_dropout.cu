@@ -193,8 +193,10 @@ template <typename E> int dropout_of(const Args& a, const void* x, const void* r
     constexpr int N = 16 / (int)S;
     const uint32_t granule = rows_granule((uintptr_t)x | (uintptr_t)y, residual ? (uintptr_t)residual : 0, a.ld_x * S, a.ld_y * S, residual ? a.ld_r * S : 0);
     if (S == 4 && granule >= 32) return dropout_as<E, S == 4 ? 8 : N, 1>(a, x, residual, y, s);
-    // (two rows a thread where there are rows for it: 16384 x 4096 bfloat16 elements and their gradient 115 us, one row 130)
-    if (granule >= 16) return a.T >= 2048 && S == 2 ? dropout_as<E, N, S == 2 ? 2 : 1>(a, x, residual, y, s) : dropout_as<E, N, 1>(a, x, residual, y, s);
+    // (two rows a thread from 2^20 elements on: 16384 x 4096 bfloat16 elements with a residual 62 us, with one row a thread 66; 2048 x 512 2.0 and 2.2, 256 x
+    // 4096 2.0 and 2.2; 1536 x 512 2.0 and 1.9, 64 x 4096 1.6 and 1.4)
+    if (granule >= 16) return (uint64_t)a.T * a.D >= 1u << 20 && S == 2 ? dropout_as<E, N, S == 2 ? 2 : 1>(a, x, residual, y, s) : dropout_as<E, N, 1>(a, x, residual, y, s);
+    // (rows of an even number of elements: 2^24 of them in rows of 30 to 4094 24 us, by the other kernel 29 to 55)
     if (S == 2 && granule >= 4) return dropout_as<E, S == 2 ? 2 : 1, 1>(a, x, residual, y, s);
     const auto alike = [&](const void* p, uint64_t ld) { return (((uintptr_t)p ^ (uintptr_t)x) & 15u) == 0 && ((ld - a.ld_x) * S & 15u) == 0; };
     if (alike(y, a.ld_y) && (!residual || alike(residual, a.ld_r))) {

@@ -53,14 +53,31 @@ def test_norm_of_wide_rows_in_number(rows, kind, T, D, extra, shift):  # noqa: F
     norm_both_ways(rows, T, D, kind, [(extra, shift)] * 4)
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("D,extra,shift", [(37, 3, 0), (300, 0, 0), (501, 0, 1), (1001, 7, 2)])
+@pytest.mark.parametrize("which", ["gamma", "beta"])
+def test_norm_with_one_parameter(rows, kind, D, extra, shift, which):  # noqa: F811
+    """A weight without a bias, and a bias without a weight."""
+    x, gamma, beta, _ = norm_inputs(70, D, kind, "fp32", 81)
+    gamma, beta = (gamma, None) if which == "gamma" else (None, beta)
+    on = [None if p is None else p.cuda() for p in (gamma, beta)]
+    for other in (0, 1):
+        got = run_norm(rows, strided(x, extra, shift), *on, y=strided(torch.zeros_like(x), extra, shift + other))
+        want, off = ref.norm(f64(x), None if gamma is None else f64(gamma), None if beta is None else f64(beta), 1e-5)
+        for a, b, c, k in zip(got, want, off, (kind, "fp32", "fp32")):
+            ref.within(f64(a), b, c, k)
+    assert rows.sync() == 0
+
+
 @pytest.mark.parametrize("kind,T,D", [("bf16", 700, 33000), ("fp16", 601, 25001), ("fp32", 601, 12801)])
 @pytest.mark.parametrize("dx_wanted", [True, False], ids=["all", "sums only"])
 def test_norm_of_long_rows_in_number(rows, kind, T, D, dx_wanted):  # noqa: F811
     norm_both_ways(rows, T, D, kind, [(0, 0)] * 4, dx_wanted=dx_wanted)
 
 
-@pytest.mark.parametrize("kind", ["fp16", "bf16"])
-@pytest.mark.parametrize("T,D,extra", [(2047, 40, 0), (2048, 40, 0), (2049, 40, 0), (4101, 64, 0), (2049, 44, 4), (2051, 3, 5), (2049, 2056, 0), (30001, 8, 0)])
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("T,D,extra", [(2047, 40, 0), (2048, 40, 0), (2049, 40, 0), (4101, 64, 0), (2049, 44, 4), (2051, 3, 5), (2049, 2056, 0), (30001, 8, 0), (259, 4096, 0), (4101, 264, 0), (70001, 20, 4),
+                                     (9001, 249, 0), (5003, 501, 0)])
 def test_dropout_of_many_rows(rows, kind, T, D, extra):  # noqa: F811
     x, res = torch.randn(T, D, generator=gen(90, T, D)).to(TYPES[kind]), torch.randn(T, D, generator=gen(91, T, D)).to(TYPES[kind])
     for residual in (res, None):
