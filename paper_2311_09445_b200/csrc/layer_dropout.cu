@@ -202,7 +202,10 @@ template <typename E> int dropout_of(const Args& a, const void* x, const void* r
     if (alike(y, a.ld_y) && (!residual || alike(residual, a.ld_r))) {
         const uint32_t units = (a.D + N - 1 + kGroup - 1) / kGroup, parts = (units + 30) / 31;
         const uint64_t warps = (uint64_t)a.T * parts, blocks = (warps + kThreads / 32 - 1) / (kThreads / 32);
-        if (blocks <= 0x7FFFFFFFu && 2 * units >= 31 * parts)            // (half of the lanes at least have something)
+        // Where seven tenths of the lanes have something, half of them in binary32.  2^24 bfloat16 elements in rows of 193 (eight tenths) 40 us, element by element
+        // 41; of 513 (0.70) 42 and 42, of 501 (0.69) 42 and 42, of 301 (0.63) 49 and 41, of 249 (0.53) 57 and 42.  2^23 binary32 elements in rows of 257 (0.53) 29
+        // and 30, of 301 (0.63) 26 and 29, of 65 (0.29) 56 and 28.
+        if (blocks <= 0x7FFFFFFFu && 10 * units >= (S == 4 ? 5 : 7) * 31 * parts)
             return rows_launch(dropout_any_kernel<E>, dim3((uint32_t)blocks), dim3(kThreads), 0, s, 0, parts, warps, (const E*)x, (const E*)residual, (E*)y, a);
     }
     return dropout_as<E, 1, 1>(a, x, residual, y, s);
