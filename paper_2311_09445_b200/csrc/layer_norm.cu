@@ -525,8 +525,9 @@ template <typename E, typename P> int norm_as(const NormArgs& a, cudaStream_t s)
 {
     const bool odd = (((uintptr_t)a.x | a.ld_x * sizeof(E)) & 15u) != 0, broken = odd || a.D % kN<E> != 0;
     const uint32_t words = words_of<E>(a.D, odd), shared = 2 * params_room<E>(a.D) * 4;
-    // words of a thread: as many as make a row a warp's, but few of a wide row (2000 rows of 16384 binary16 elements: 2 words 51 us, 4 61)
-    const int nv = words <= 32 ? 1 : words <= 64 ? 2 : words <= 512 ? 4 : words <= 2048 ? 2 : 4;
+    // words of a thread: as many as make a row a warp's, but few of a wide row.  2^25 bfloat16 elements in rows of 64 words: 2 of them 30 us, 4 34; of
+    // 128: 37 and 31, of 1536: 54 and 49, of 2048: 51 and 60 (and beyond that 2 are not enough)
+    const int nv = words <= 32 ? 1 : words <= 64 ? 2 : words <= 1536 ? 4 : words <= 2048 ? 2 : 4;
     const uint32_t threads = team_of(words, nv);
     if (threads <= (nv == 4 ? kThreads<4> : kThreads<2>) && shared <= kSharedBytes && same_place(a.x, a.ld_x, a.y, a.ld_y, sizeof(E))) {
 #define NORM(NV) (broken ? norm_with<E, P, NV, true>(a, threads, shared, s) : norm_with<E, P, NV, false>(a, threads, shared, s))
