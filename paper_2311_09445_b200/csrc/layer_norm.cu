@@ -237,10 +237,10 @@ struct RingShape {
     uint32_t blocks, params;                 // of the grid; bytes of gamma, before the rings
 };
 constexpr uint32_t kSharedBytes = 216 * 1024, kMaxBarriers = 128;
-template <int NV> constexpr int kMostThreads = NV == 4 ? 384 : NV == 2 ? 768 : 1024;      // of a block: what the registers have room for
+template <int NV> constexpr int kMostThreads = NV == 4 ? 384 : 1024;      // of a block: what the registers have room for
 
-template <typename E, typename P, int NV, bool kBroken, int kMost>
-__global__ void __launch_bounds__(kMost, 1)
+template <typename E, typename P, int NV, bool kBroken>
+__global__ void __launch_bounds__(kMostThreads<NV>, 1)
     norm_grad_kernel(unsigned* status, uint32_t T, uint32_t D, const E* dy, uint64_t ld_dy, const E* x, uint64_t ld_x, const float* mean, const float* rstd,
                      const void* gamma, E* dx, uint64_t ld_dx, float* work, const float* work_end, RingShape f)
 {
@@ -304,7 +304,7 @@ __global__ void __launch_bounds__(kMost, 1)
         for (uint32_t k = 0; k < rows; ++k, odd ^= 1u) {
             const uint64_t t = group * f.rows + k;
             const unsigned char *at_dy = ring + (stage * 2 * f.rows + k) * f.pitch, *at_x = at_dy + f.rows * f.pitch;
-            constexpr bool kPacked = kMost > kMostThreads<NV>;            // (fewer registers: x is kept as it is, and normed again)
+            constexpr bool kPacked = NV == 2;            // (fewer registers: x is kept as it is, and normed again)
             Word<E> a[NV], b[kPacked ? NV : 1];
             Twos<E> p, g, n[kPacked ? 1 : NV];
             LayerTwo all(0.0f), along(0.0f);
@@ -555,10 +555,11 @@ template <typename E> RingShape ring_shape(const GradArgs& a, bool odd, int* nv)
 {
     RingShape f = {};
     const uint32_t S = sizeof(E), words = words_of<E>(a.D, odd), sms = rows_sm_count() < kLines ? rows_sm_count() : kLines;
-    // words of a thread: four, so that a row's two sums are over few threads; a wide row's two, so that one block's threads have it
-    *nv = words <= 32 ? 1 : words <= 64 ? 2 : words <= 4 * 384 ? 4 : 2;
+    // words of a thread: four, so that a row's two sums are over few threads; one where a warp has a row with that, and a wide row's two, so that one
+    // block's threads have it.  2^25 bfloat16 elements in rows of 32 words: one 60 us, 4 72; of 64: one 72, 2 67, 4 62; of 1536: 4 78, 2 102
+    *nv = words <= 32 ? 1 : words <= 4 * kMostThreads<4> ? 4 : 2;
     f.threads = team_of(words, *nv);
-    const uint32_t whole = *nv == 4 ? kMostThreads<4> : words <= 64 ? kMostThreads<2> : 1024;
+    const uint32_t whole = *nv == 4 ? kMostThreads<4> : kMostThreads<1>;
     if (f.threads > whole) return f;
     f.teams = whole / f.threads;
     if (f.threads > 32 && f.teams > 15) f.teams = 15;                  // (a named barrier each)
@@ -583,11 +584,11 @@ template <typename E> RingShape ring_shape(const GradArgs& a, bool odd, int* nv)
     }
     return f;
 }
-template <typename E, typename P, int NV, bool kBroken, int kMost> int ring_with(const GradArgs& a, const RingShape& f, float* work, cudaStream_t s)
+template <typename E, typename P, int NV, bool kBroken> int ring_with(const GradArgs& a, const RingShape& f, float* work, cudaStream_t s)
 {
     static std::atomic<bool> ready[kRowsMaxDevices];
-    if (!shared_memory(norm_grad_kernel<E, P, NV, kBroken, kMost>, ready)) return -1;
-    return rows_launch(norm_grad_kernel<E, P, NV, kBroken, kMost>, dim3(f.blocks), dim3(f.teams * f.threads), kSharedBytes, s, 0, a.status, a.T, a.D,
+    if (!shared_memory(norm_grad_kernel<E, P, NV, kBroken>, ready)) return -1;
+    return rows_launch(norm_grad_kernel<E, P, NV, kBroken>, dim3(f.blocks), dim3(f.teams * f.threads), kSharedBytes, s, 0, a.status, a.T, a.D,
                        (const E*)a.dy, a.ld_dy, (const E*)a.x, a.ld_x, a.mean, a.rstd, a.gamma, (E*)a.dx, a.ld_dx, work, a.work_end, f);
 }
 template <typename E, typename P> int grad_as(const GradArgs& a, cudaStream_t s)
@@ -604,8 +605,8 @@ template <typename E, typename P> int grad_as(const GradArgs& a, cudaStream_t s)
         const RingShape f = alike ? ring_shape<E>(a, odd, &nv) : RingShape();
         if (f.stages) {
             lines = f.blocks;
-#define RING(NV, MOST) (broken ? ring_with<E, P, NV, true, MOST>(a, f, work, s) : ring_with<E, P, NV, false, MOST>(a, f, work, s))
-            n = nv == 1 ? RING(1, kMostThreads<1>) : nv == 4 ? RING(4, kMostThreads<4>) : f.threads == 32 ? RING(2, kMostThreads<2>) : RING(2, 1024);
+#define RING(NV) (broken ? ring_with<E, P, NV, true>(a, f, work, s) : ring_with<E, P, NV, false>(a, f, work, s))
+            n = nv == 1 ? RING(1) : nv == 4 ? RING(4) : RING(2);
 #undef RING
         } else {
             lines = a.T < kLines ? a.T : kLines;
