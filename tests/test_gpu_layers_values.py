@@ -1,5 +1,6 @@
 """A layer's operators on the GPU where values are special: NaN and infinity in what is chosen, numbers that need all of binary32, constant rows."""
 import math
+import time
 
 import numpy as np
 import pytest
@@ -9,6 +10,7 @@ import layer_reference as ref
 from test_gpu_layers import KINDS, TYPES, f64, gen, layer_inputs, norm_inputs, rows, run_layer, run_norm, strided  # noqa: F401
 
 pytestmark = pytest.mark.gpu
+INTERNAL = 16
 
 
 def given(T, k, E, *seed):
@@ -185,4 +187,23 @@ def test_norm_grad_of_constant_rows(rows, kind, D, value):  # noqa: F811
         rows.layer_norm_grad(strided(dy, extra, shift), strided(x, extra, shift), torch.full((3,), 2.0, device="cuda"),
                              torch.full((3,), 300.0, device="cuda"), None, dx)
         assert (dx == 0).all()
+    assert rows.sync() == 0
+
+
+# ---- a scratch that does not fit ---------------------------------------------------------------------------------------
+
+def test_expert_layer_with_a_scratch_that_was_not_zero_ends(rows):  # noqa: F811
+    """A count in it says that some first products are already in work, so nobody tells of them.  The call gives up after a limit, says so, and leaves the
+    scratch fit for the next."""
+    T, D, H, E, k = 64, 512, 256, 64, 4
+    x, router, up, down = (t.cuda() for t in layer_inputs(T, D, H, E, k, "bf16", True, 95))
+    w, ids, work = torch.zeros(T, k, device="cuda"), torch.zeros(T, k, dtype=torch.int32, device="cuda"), rows.expert_layer_work(T, D, H, E, k)
+    want = run_layer(rows, x, router, up, down, w, ids, True, True, work=work)
+    assert rows.sync() == 0
+    work[:4].view(torch.int32)[0] = 64
+    start = time.monotonic()
+    run_layer(rows, x, router, up, down, w, ids, True, True, work=work)
+    assert rows.sync() == INTERNAL
+    assert time.monotonic() - start < 20
+    assert torch.equal(run_layer(rows, x, router, up, down, w, ids, True, True, work=work), want)
     assert rows.sync() == 0
