@@ -4,7 +4,8 @@ import pytest
 import torch
 
 import layer_reference as ref
-from test_gpu_layers import KINDS, LINES, TYPES, expected_dropout, f64, gen, norm_inputs, rows, run_norm, strided, untouched_beside  # noqa: F401
+from test_gpu_layers import (KINDS, LINES, TYPES, expected_dropout, f64, gen, layer_inputs, norm_inputs, rows, run_layer, run_norm,  # noqa: F401
+                             strided, untouched_beside)
 
 pytestmark = pytest.mark.gpu
 
@@ -85,3 +86,74 @@ def test_dropout_of_many_rows(rows, kind, T, D, extra):  # noqa: F811
         rows.dropout(strided(x, extra), y, 0.3, 12, 5, residual=None if residual is None else strided(res, extra))
         assert torch.equal(y.cpu(), expected_dropout(x, residual, 0.3, 12, 5)) and untouched_beside(y, extra)
     assert rows.sync() == 0
+
+
+# ---- the expert layer's ends, and calls side by side -------------------------------------------------------------------
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("T,D,H,E,k", [(2, 65536, 24, 2, 1), (2, 65535, 9, 2, 1), (2, 24, 65536, 2, 2), (2, 9, 65535, 2, 2), (64, 16, 8, 1024, 32), (64, 24, 40, 1, 1),
+                                       (64, 200, 72, 2, 2), (64, 72, 200, 3, 2)])
+def test_expert_layer_at_the_ends_of_its_sizes(rows, kind, T, D, H, E, k):  # noqa: F811
+    """The widest rows, the most experts and choices, experts with more slots than are multiplied at once."""
+    for gated, chosen in ((True, False), (False, True)):
+        x, router, up, down = layer_inputs(T, D, H, E, k, kind, gated, 96)
+        w, ids = torch.full((T, k), 5.0, device="cuda"), torch.full((T, k), 99, dtype=torch.int32, device="cuda")
+        y = run_layer(rows, x.cuda(), router.cuda(), up.cuda(), down.cuda(), w, ids, gated, chosen)
+        want_w, want_ids, off_w = ref.choose(f64(x), f64(router), k, chosen)
+        assert (ids.cpu().numpy() == want_ids).all()
+        want, off = ref.experts(f64(x), f64(up), f64(down), want_w, want_ids, kind, gated, off_w)
+        ref.within(f64(y), want, off, kind)
+    assert rows.sync() == 0
+
+
+def test_calls_side_by_side(rows):  # noqa: F811
+    """Two streams with handles and scratch of their own, whose calls are in the GPU at the same time: each has the results that it has alone."""
+    from paper_2311_09445_b200 import RowLayers
+    T, D, H, E, k = 48, 2048, 1000, 24, 4
+    sides = []
+    for i, kind in enumerate(("bf16", "fp16")):
+        x, router, up, down = (t.cuda() for t in layer_inputs(T, D, H, E, k, kind, True, 97 + i))
+        w, ids, y = torch.zeros(T, k, device="cuda"), torch.zeros(T, k, dtype=torch.int32, device="cuda"), torch.zeros_like(x)
+        norm, mean, rstd = torch.zeros_like(x), torch.zeros(T, device="cuda"), torch.zeros(T, device="cuda")
+        dx, dg, db = torch.zeros_like(x), torch.zeros(D, device="cuda"), torch.zeros(D, device="cuda")
+        stream = torch.cuda.Stream()
+        r = RowLayers(stream=stream)
+        work, sums = r.expert_layer_work(T, D, H, E, k), r.layer_norm_grad_work(T, D)
+
+        def step(r=r, x=x, router=router, up=up, down=down, y=y, w=w, ids=ids, work=work, norm=norm, mean=mean, rstd=rstd, dx=dx, dg=dg, db=db, sums=sums):
+            r.layer_norm(x, norm, None, None, 1e-5, mean, rstd)
+            r.expert_layer(norm, router, up, down, y, w, ids, work)
+            r.layer_norm_grad(y, x, mean, rstd, None, dx, dg, db, sums)
+
+        torch.cuda.synchronize()
+        step()
+        torch.cuda.synchronize()
+        outs = (norm, mean, rstd, y, w, ids, dx, dg, db)
+        sides.append((r, stream, step, outs, [t.clone() for t in outs]))
+    for _ in range(30):
+        for _, _, step, _, _ in sides:
+            step()
+    torch.cuda.synchronize()
+    graphs = []
+    for r, stream, step, outs, alone in sides:
+        for a, b in zip(outs, alone):
+            assert torch.equal(a, b)
+            a.zero_()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            for _ in range(3):
+                step()
+        graphs.append(graph)
+    for _ in range(5):
+        for graph, (_, stream, _, _, _) in zip(graphs, sides):
+            with torch.cuda.stream(stream):
+                graph.replay()
+    torch.cuda.synchronize()
+    for r, _, _, outs, alone in sides:
+        for a, b in zip(outs, alone):
+            assert torch.equal(a, b)
+        assert r.sync() == 0
+    graphs.clear()
+    for r, *_ in sides:
+        r.close()
