@@ -34,7 +34,9 @@ extern "C" {
 /* y[t] = (x[t] - mean_t) * rstd_t * gamma + beta, mean_t the mean of row t's D elements, rstd_t = 1 / sqrt(var_t + eps), var_t the mean of
  * (x - mean_t)^2.  gamma and beta (D elements of param_dtype, which is PEARL_F32 or dtype) may each be NULL: weights of 1, a
  * bias of 0.  d_mean and d_rstd (binary32, T entries, what the gradient wants) may each be NULL.  A row with an element that is not
- * finite has NaN for results; other rows are not touched by it.  1 <= D <= PEARL_LAYER_MAX_WIDTH, eps >= 0 and finite; T < 2^31 may be 0. */
+ * finite has NaN for results; other rows are not touched by it.  Sums and squares are binary32's, too: a row whose sum passes that range has NaN, one whose
+ * squared differences do (from some 1e19 on) has a d_rstd of 0 and the bias for results.
+ * 1 <= D <= PEARL_LAYER_MAX_WIDTH, eps >= 0 and finite; T < 2^31 may be 0. */
 int pearl_layer_norm(pearl_rows_t* rows, uint32_t T, uint32_t D, uint32_t dtype, const void* d_x, uint64_t ld_x, uint32_t param_dtype,
                      const void* d_gamma, const void* d_beta, double eps, void* d_y, uint64_t ld_y, float* d_mean, float* d_rstd);
 

@@ -190,6 +190,23 @@ def test_norm_grad_of_constant_rows(rows, kind, D, value):  # noqa: F811
     assert rows.sync() == 0
 
 
+@pytest.mark.parametrize("kind", ["fp32", "bf16"])
+@pytest.mark.parametrize("D,shift", [(48, 0), (333, 1)])
+def test_norm_of_rows_beyond_the_range_of_binary32(rows, kind, D, shift):  # noqa: F811
+    """Squared differences that are infinite give the bias, an infinite sum gives NaN; other rows are as they are alone."""
+    x, gamma, beta, _ = norm_inputs(5, D, kind, "fp32", 71)
+    for other in (0, 1):
+        plain = run_norm(rows, strided(x, 0, shift), gamma.cuda(), beta.cuda(), y=strided(torch.zeros_like(x), 0, shift + other))
+        far = x.clone()
+        far[1] *= 1e25
+        far[3] = 3e38
+        got = run_norm(rows, strided(far, 0, shift), gamma.cuda(), beta.cuda(), y=strided(torch.zeros_like(x), 0, shift + other))
+        assert float(got[2][1]) == 0 and torch.equal(got[0][1].cpu(), beta.to(TYPES[kind]))
+        assert got[0][3].isnan().all()
+        for t in (0, 2, 4):
+            assert all(torch.equal(a[t], b[t]) for a, b in zip(got, plain))
+
+
 # ---- a scratch that does not fit ---------------------------------------------------------------------------------------
 
 def test_expert_layer_with_a_scratch_that_was_not_zero_ends(rows):  # noqa: F811
