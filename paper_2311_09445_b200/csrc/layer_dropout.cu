@@ -2,7 +2,7 @@
 //
 // Bound by memory, with the generator beside it: one counter is good for 8 elements of 16 bits each, some 60 instructions.  (32 bits an
 // element would be twice that, and a 16-bit element's share of an SM's cycles is 9 instructions at the memory's rate.)  The counters are made
-// while the elements are on their way.  16384 x 4096 bfloat16 elements with a residual 62 us (6.5 TB/s), without one 54 (5.0 TB/s; issue slots three
+// while the elements are on their way.  16384 x 4096 bfloat16 elements with a residual 62 us (6.5 TB/s), without one 55 (4.9 TB/s; issue slots three
 // quarters used).
 #include "layer_internal.cuh"
 

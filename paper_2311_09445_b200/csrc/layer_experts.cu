@@ -4,12 +4,12 @@
 // ask for its expert.  So the weights are streamed through shared memory once, one CTA an SM, by copies that nobody waits for but the warps
 // that multiply: these take 16 weight rows as one operand of a matrix instruction whose other operand are the expert's rows in groups of 8.
 //
-// Measured: 64 rows, 64 experts of 2048 x 1408, 6 a row, binary16: 1.1 GB in 223 us (5.0 TB/s); 128 experts of 4096 x 1280, 8 a row, bfloat16: 4 GB
-// in 706 us (5.6 TB/s).  The same without products takes 193 and 635 us, without copies of x and h 223 and 704: what is left beside the
+// Measured, in a replayed graph: 64 rows, 64 experts of 2048 x 1408, 6 a row, binary16: 1.1 GB in 212 us (5.2 TB/s); 128 experts of 4096 x 1280, 8 a row,
+// bfloat16: 4 GB in 729 us (5.4 TB/s).  The same without products takes 189 and 636 us, without copies of x and h 211 and 724: what is left beside the
 // streaming is the reading of the operands from shared memory, and ten microseconds of a call's chain of steps (choice, plan, two products, their sum).
-// With tcgen05.mma in the place of the warps' own instructions, M = 128 and N = 16 .. 128, the sums in tensor memory, 229 and 715 us: the weights
-// are read from shared memory all the same.  It was faster only for many rows an expert (8 experts, 4 a row: 93 us, so 107), which is not
-// what this call is for.
+// tcgen05.mma in the place of the warps' own instructions, M = 128 and N = 16 .. 128, the sums in tensor memory, was no faster (229 and 715 us where these
+// then took 223 and 706): the weights are read from shared memory all the same, and its sums over a whole row are cut off.  With many rows an expert
+// it was (8 experts, 4 a row: 93 us; this then took 107, now 98 to 104).
 #include <cuda.h>
 
 #include "layer_internal.cuh"
@@ -121,7 +121,8 @@ template <typename E, int V> int logits_launch(unsigned* status, const LayerExpe
 #define LOGITS(X)                                                                                                                             \
     rows_launch(logits_kernel<E, V, X>, dim3((a.E + X - 1) / X, fours), dim3(kWorkers * 32), 0, s, 0, status, a.T, a.D, a.E, (const E*)a.x, a.ld_x, \
                 (const E*)a.router, logits)
-    // (four experts a block where there are more than two blocks an SM without that)
+    // Four experts a block where there are more than two blocks an SM without that.  Whole calls, hidden 16: 64 rows and 128 experts of width 4096 52 us, with one
+    // a block 57, 28 rows and 64 experts 31 and 32; 16 rows and 64 experts 26.1 and 25.9, 4 rows and 128 experts 21.3 and 20.7
     return a.E * fours > 2 * rows_sm_count() ? LOGITS(4) : LOGITS(1);
 #undef LOGITS
 }
@@ -187,9 +188,9 @@ Cut cut_as(uint32_t rows, uint32_t row_bytes, uint32_t ways, uint32_t across, bo
     c.pieces = ((rows + 15) / 16 + c.strips - 1) / c.strips;
     return c;
 }
-// Pieces of 128 rows in stages of 32 KB stream fastest; where an SM would not get two pieces of every three, smaller ones.  Measured in
-// binary16: 64 experts of 2048 x 1408 for 64 rows 221 us, with pieces of 64 rows 270, of 32 rows 407; 2 experts of 512 x 1024 for one row 15.3,
-// 13.5 and 12.4.
+// Pieces of 128 rows in stages of 32 KB stream fastest; where an SM would not get two pieces of every three, smaller ones.  Measured with pieces of 128,
+// 64 and 32 rows: 64 experts of 2048 x 1408 for 64 rows, binary16, 211, 265 and 400 us; 24 of 2048 x 768, a row each, 45, 47 and 62; 8 of 2048 x 2048 42,
+// 39 and 51; 4 of them 31, 29 and 32; 2 of 512 x 1024 for one row 19, 17 and 16.
 Cut cut_of(uint32_t rows, uint32_t row_bytes, uint32_t experts, bool words)
 {
     uint32_t ways = 1;
@@ -357,7 +358,8 @@ __device__ __forceinline__ void arrive_with_words(uint64_t* barrier)
 // Whose rows (the first products', the second ones') are whole words: tensor copies bring them.
 constexpr int kUpWhole = 1, kDownWhole = 2, kWhole = 3;
 template <int kAlign> __device__ __forceinline__ bool whole_words(uint32_t kind) { return kind == kUp ? (kAlign & kUpWhole) != 0 : (kAlign & kDownWhole) != 0; }
-// The warps that bring weights: one thread of one; eight warps where words have to be cut out of rows.
+// The warps that bring weights: one thread of one; eight warps where words have to be cut out of rows.  (21 warps then, 80 registers a thread, of which the
+// products spill 0.8 to 1.7 KB: what such rows cost beside the cutting.)
 template <int kAlign> constexpr uint32_t kWeightWarps = kAlign == kWhole ? 1 : 8;
 // Those that bring the rows of x or h.
 constexpr uint32_t kRowWarps = 4;

@@ -138,8 +138,9 @@ template <int M> __device__ __forceinline__ void team_sums(uint32_t threads, uin
 
 // ---- forward --------------------------------------------------------------------------------------------------------------
 // A team goes over every so many rows; the next row's words are on their way while it forms the mean, then the mean of the squared differences,
-// then the results of this one.  16381 rows of 2048 bfloat16 elements 34 us (3.9 TB/s; 452 instructions a warp and row, of which 190 are there for any
-// length), 8192 of binary32 27 (5.0 TB/s).  A block a row took 44, with four words a thread and no row ahead 34.
+// then the results of this one.  16381 rows of 2048 bfloat16 elements 35 us (3.9 TB/s; 465 instructions a warp and row, of which some 200 are there for any
+// length), 8192 of binary32 27 (5.0 TB/s).  A block a row took 44, with four words a thread and no row ahead 34.  Words that rows
+// break cost more registers than there are: four a thread spill 108 bytes (8000 rows of 2047 bfloat16 elements 34 us).
 template <int NV> constexpr uint32_t kThreads = NV == 4 ? 768 : 1024;           // of a block: what the registers have room for
 template <typename E, typename P, int NV, bool kBroken>
 __global__ void __launch_bounds__(kThreads<NV>, 1) norm_kernel(unsigned* status, uint32_t T, uint32_t D, uint32_t threads, const E* x, uint64_t ld_x,
@@ -229,8 +230,9 @@ __global__ void __launch_bounds__(kThreads<NV>, 1) norm_kernel(unsigned* status,
 // One block an SM, a row a team.  Every team has a ring in shared memory that bulk copies fill, of one row or of several that lie one
 // behind the other: what is on its way (some 150 KB an SM) takes no registers.  A thread keeps to its columns -- a team's rows all start at the same
 // place in a word --, so that the columns' sums of dy * n and dy stay in its registers; they end as the block's line of `work`: [blocks][2][D].
-// 16384 rows of 4096 bfloat16 elements 102 us with the sum over the lines (3.9 TB/s; 7 of it the lines), 1000 of 500 binary32 elements 6.7.  Spilled
-// sums made it 200 us: hence 384 threads.  Wide rows (12289 elements: 106 us for 2011) do spill.
+// 16384 rows of 4096 bfloat16 elements 103 us with the sum over the lines (3.9 TB/s; 7 of it the lines), 1000 of 500 binary32 elements 6.7.  Spilled
+// sums made it 200 us: hence 384 threads.  Wide rows (12289 elements: 109 us for 2011) do spill,
+// 440 bytes a thread, and narrow ones with broken words 40.
 struct RingShape {
     uint32_t threads, teams, stages, rows;   // of a team; teams a block; stages of a team; rows of a stage
     uint32_t pitch;                          // distance of the rows of a stage
