@@ -294,7 +294,7 @@ __device__ __forceinline__ uint32_t read_acquired(const uint32_t* p)
     asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
     return v;
 }
-// Polls until *p >= count; with a limit, of a second or two.  Once it was reached -- the scratch was not zero, or two calls share it -- the polls behind it
+// Polls until *p >= count; with a limit, of more than half a second.  Once it was reached -- the scratch was not zero, or two calls share it -- the polls behind it
 // soon give up, too, so that a call does not take as many limits as it has experts.
 __device__ __forceinline__ void poll(unsigned* status, const uint32_t* p, uint32_t count)
 {
