@@ -71,8 +71,9 @@ int pearl_layer_dropout(pearl_rows_t* rows, uint32_t T, uint32_t D, uint32_t dty
  *   d_up      E x (2H or H) x D, by `act`;  d_down  E x D x H;  both dense, of the rows' type
  * Sums run in binary32 or wider.  h is held as a binary32, in 16-bit layers as the sum of numbers of the type: three of bfloat16, which are all of it; two
  * of binary16, which are it but for 2^-22 of it or 2^-36, whichever is more (an h beyond 65504 is infinite).  Infinities and NaN go by the formula in
- * 16-bit layers (but a binary16 h below 2^-25 times an infinite weight is NaN).  Products of binary32 are formed from two parts of 11 bits each, all but 2^-21 of them; an infinite factor, or one above 3.4e38,
- * gives NaN there, as a NaN does.  An expert that no row asks for is not read.  A row without experts is zero.
+ * 16-bit layers (but a binary16 h below 2^-25 times an infinite weight is NaN).  Products of binary32 are formed from two parts of 11 bits each, all but
+ * 2^-21 of them; an infinite factor, or one above 3.4e38, gives NaN there, as a NaN does.  An expert that no row asks for is not read.  A row without
+ * experts is zero.
  * d_work must be zero before its first use; every call leaves it fit for the next one, of any sizes it has room for.
  * 1 <= k <= min(E, PEARL_ROWS_MAX_CHOICES), E <= PEARL_ROWS_MAX_EXPERTS, T <= PEARL_LAYER_MAX_FEW (0: nothing to do), D and H within
  * 1 .. PEARL_LAYER_MAX_INNER. */
